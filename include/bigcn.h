@@ -563,6 +563,135 @@ bigcn_status bigcn_spmm_prescaled_rows(const int64_t *rowptr, const int32_t *col
                                        const float *Z, int64_t ldz, int32_t F, float *H,
                                        int64_t ldh, void *stream);
 
+/*
+ * Training on real-valued rows: layer normalisation, activations kept in 8 bits
+ * for the backward pass, and the weight gradient that reads them. (The paper has
+ * no counterpart: Bi-GCN's own backward keeps one bit per feature. These serve the
+ * layers whose features stay real -- BIGCN_BINARIZE_WEIGHTS, or a plain product --
+ * and deeper models that normalise between layers.)
+ *
+ * Tensors of these calls are of one of three element types; parameters (gamma,
+ * beta), statistics and the parameters' gradients are fp32 throughout, as are all
+ * sums. Pointers are aligned to their element. NaN and infinities are data here: a
+ * row that holds one gives NaN in that row's outputs (and in the gradients that sum
+ * over rows) and touches no other row.
+ */
+typedef enum bigcn_dtype {
+    BIGCN_F32 = 0,
+    BIGCN_BF16 = 1,
+    BIGCN_F16 = 2
+} bigcn_dtype;
+
+/*
+ * A checkpoint of an N x K matrix: each row in groups of 32 consecutive columns,
+ *
+ *   v[i,k] = q[i,k] * 2^(exps[i, k/32] - 127),   q in [-127, 127],
+ *
+ * exps the least byte >= 1 by which the group's largest magnitude rounds (to nearest
+ * even) to at most 127; a group that holds a NaN or an infinity has byte 255 and NaN
+ * values. |v - x| is at most half a step: 1/127.5 of the group's largest magnitude, or
+ * 2^-127 in groups below 2^-120. Values have 7 significant bits, exact in bf16.
+ *
+ * q      N rows of ldq bytes, 16-byte aligned, ldq >= K a multiple of 16.
+ * exps   N rows of lde bytes, 4-byte aligned, lde >= ceil(K/32) a multiple of 4.
+ * Calls read and write whole rows up to K rounded up to 16 and ceil(K/32) rounded up
+ * to 4 bytes; the bytes past K and past the last group are written 0 and ignored when
+ * read.
+ */
+
+/* ceil(K / 32): the groups of a checkpoint's row (0 if K <= 0). */
+int32_t bigcn_checkpoint_groups(int32_t K);
+
+/* X (N x K, row stride ldx >= K, `dtype` a bigcn_dtype) to its checkpoint.
+ * 0 <= N < 2^31, 1 <= K; q and exps must not overlap each other or X. */
+bigcn_status bigcn_checkpoint_pack(int32_t dtype, const void *X, int64_t N, int32_t K, int64_t ldx,
+                                   int8_t *q, int64_t ldq, uint8_t *exps, int64_t lde,
+                                   void *stream);
+
+/* X[i,k] = gamma[k] * v[i,k] + beta[k] (one fused multiply-add, rounded once to
+ * `dtype`); gamma and beta K fp32, each nullable (1 and 0): the layer's input again,
+ * from the checkpoint of normalised rows. X must not overlap the inputs. */
+bigcn_status bigcn_checkpoint_unpack(int32_t dtype, const int8_t *q, int64_t ldq,
+                                     const uint8_t *exps, int64_t lde, int64_t N, int32_t K,
+                                     const float *gamma, const float *beta, void *X, int64_t ldx,
+                                     void *stream);
+
+/*
+ * Layer normalisation of rows:
+ *
+ *   mean_i = (1/K) sum_k x_ik,   rstd_i = 1 / sqrt((1/K) sum_k (x_ik - mean_i)^2 + eps),
+ *   xhat_ik = (x_ik - mean_i) rstd_i,   Y_ik = gamma_k xhat_ik + beta_k
+ *
+ * X, Y   N x K of `dtype`, row strides ldx, ldy >= K; Y rounded once.
+ * gamma, beta   K fp32, each nullable (1 and 0).   eps finite, >= 0 (0 with a constant
+ *        row divides by zero: that row is NaN).
+ * mean, rstd   N fp32 each, each nullable: the backward's inputs.
+ * q, exps (nullable, both or neither)   receive the checkpoint of xhat.
+ * 0 <= N < 2^31, 1 <= K. No output may overlap another or an input.
+ */
+bigcn_status bigcn_layer_norm_forward(int32_t dtype, const void *X, int64_t N, int32_t K,
+                                      int64_t ldx, const float *gamma, const float *beta,
+                                      float eps, void *Y, int64_t ldy, float *mean, float *rstd,
+                                      int8_t *q, int64_t ldq, uint8_t *exps, int64_t lde,
+                                      void *stream);
+
+/* Bytes of device workspace bigcn_layer_norm_backward needs when it returns dgamma or
+ * dbeta; 0 on invalid sizes. */
+size_t bigcn_layer_norm_backward_workspace_bytes(int64_t N, int32_t K);
+
+/*
+ * Its gradients, from dY = dL/dY (N x K of `dtype`, row stride lddy), with
+ * g = gamma dY:
+ *
+ *   dX_ik = rstd_i (g_ik - (1/K) sum_k g_ik - xhat_ik (1/K) sum_k g_ik xhat_ik)
+ *   dgamma_k = sum_i dY_ik xhat_ik,   dbeta_k = sum_i dY_ik
+ *
+ * xhat comes from one of two places, the other NULL: from X and mean (the forward's
+ * input and its means), or from the checkpoint q, exps. rstd (N) is required.
+ * gamma nullable (1). dX (N x K of `dtype`, row stride lddx), dgamma and dbeta (K fp32)
+ * are each nullable, but not all three.
+ * workspace  >= bigcn_layer_norm_backward_workspace_bytes(N, K) bytes, 256-byte aligned,
+ *            overlapping nothing else; not needed (may be NULL) when dgamma and dbeta
+ *            are NULL. Sums over rows are added in a fixed order: results are
+ *            deterministic on one device.
+ * No output may overlap another or an input.
+ */
+bigcn_status bigcn_layer_norm_backward(int32_t dtype, const void *dY, int64_t N, int32_t K,
+                                       int64_t lddy, const float *gamma, const void *X,
+                                       int64_t ldx, const float *mean, const int8_t *q,
+                                       int64_t ldq, const uint8_t *exps, int64_t lde,
+                                       const float *rstd, void *dX, int64_t lddx, float *dgamma,
+                                       float *dbeta, void *workspace, size_t ws_bytes,
+                                       void *stream);
+
+/* Bytes of device workspace bigcn_checkpoint_weight_grad needs; 0 on invalid sizes. */
+size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_t F);
+
+/*
+ * The gradients of Z = (gamma v + beta) W + b (W K x F, b F) from dZ = dL/dZ and the
+ * checkpoint v of the product's input before its affine (gamma, beta K fp32, each
+ * nullable: 1 and 0) -- so that the checkpoint of a norm's xhat serves the norm and
+ * the product behind it:
+ *
+ *   dW_kj = gamma_k sum_i v_ik dZ_ij + beta_k sum_i dZ_ij,   db_j = sum_i dZ_ij
+ *
+ * dZ     N x F of `dtype`, row stride lddz >= F.
+ * dW     K x F fp32, row stride lddw >= F.   db  F fp32, nullable.
+ * workspace  >= bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F) bytes, 256-byte
+ *            aligned, overlapping nothing else.
+ * Both factors enter the sums exactly (fp32 gradients to within 2^-23) and the sums
+ * are fp32, over runs of rows added in a fixed order: deterministic on one device.
+ * The tensor-core product waits on shared-memory barriers a bounded number of times:
+ * where a wait runs out its part of dW is not written (bigcn_device_timeouts).
+ * 0 <= N < 2^31, 1 <= K, 1 <= F. No output may overlap another or an input.
+ */
+bigcn_status bigcn_checkpoint_weight_grad(int32_t dtype, const int8_t *q, int64_t ldq,
+                                          const uint8_t *exps, int64_t lde, int64_t N, int32_t K,
+                                          const float *gamma, const float *beta, const void *dZ,
+                                          int32_t F, int64_t lddz, float *dW, int64_t lddw,
+                                          float *db, void *workspace, size_t ws_bytes,
+                                          void *stream);
+
 /* Bytes of the device scratch array behind bigcn_layer_forward_static. */
 #define BIGCN_STATIC_SCRATCH_BYTES (((size_t)32 << 20) + 256) /* the last 256: control words */
 

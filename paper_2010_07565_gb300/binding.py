@@ -82,6 +82,18 @@ SIGNATURES = {
                                       _p, _i64, _p, _sz, _p, _i64, _p], ctypes.c_int),
     "bigcn_layer_forward_static": ([_p, _i64, _i32, _i64, _p, _p, _p, _i32, _i64, _p, _p, _i64,
                                     _p, _i64, _p], ctypes.c_int),
+    "bigcn_checkpoint_groups": ([_i32], _i32),
+    "bigcn_checkpoint_pack": ([_i32, _p, _i64, _i32, _i64, _p, _i64, _p, _i64, _p], ctypes.c_int),
+    "bigcn_checkpoint_unpack": ([_i32, _p, _i64, _p, _i64, _i64, _i32, _p, _p, _p, _i64, _p],
+                                ctypes.c_int),
+    "bigcn_layer_norm_forward": ([_i32, _p, _i64, _i32, _i64, _p, _p, ctypes.c_float, _p, _i64,
+                                  _p, _p, _p, _i64, _p, _i64, _p], ctypes.c_int),
+    "bigcn_layer_norm_backward_workspace_bytes": ([_i64, _i32], _sz),
+    "bigcn_layer_norm_backward": ([_i32, _p, _i64, _i32, _i64, _p, _p, _i64, _p, _p, _i64, _p,
+                                   _i64, _p, _p, _i64, _p, _p, _p, _sz, _p], ctypes.c_int),
+    "bigcn_checkpoint_weight_grad_workspace_bytes": ([_i64, _i32, _i32], _sz),
+    "bigcn_checkpoint_weight_grad": ([_i32, _p, _i64, _p, _i64, _i64, _i32, _p, _p, _p, _i32,
+                                      _i64, _p, _i64, _p, _p, _sz, _p], ctypes.c_int),
     "bigcn_weighted_dinv": ([_p, _p, _i64, _i64, _p, _p], ctypes.c_int),
     "bigcn_spmm_norm_weighted": ([_p, _p, _p, _p, _i64, _i64, _p, _i64, _i32, _p, _i64, _p],
                                  ctypes.c_int),
@@ -464,6 +476,118 @@ def bigcn_weighted_layer_forward(X, scale, shift, Wt, rowptr, colidx, values, wo
         _ld(H), _stream(stream)))
 
 
+# Element types of the row-wise operators (enum bigcn_dtype).
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _dtype(t, like=None):
+    """The bigcn_dtype of a tensor (which must be ``like``'s, where given)."""
+    if t.dtype not in DTYPE or (like is not None and t.dtype != like.dtype):
+        raise ValueError("expected float32, bfloat16 or float16 tensors, all of one type")
+    return DTYPE[t.dtype]
+
+
+def _vector(t, n, what):
+    """Pointer of a contiguous fp32 vector of n entries (None: NULL)."""
+    if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous float32 vector of {n} entries")
+    return _ptr(t)
+
+
+def _kept(q, exps, N, K):
+    """(q, ldq, exps, lde) of a checkpoint of N x K, or NULLs for none."""
+    if q is None or exps is None:
+        return _ptr(q), 0, _ptr(exps), 0
+    if q.dtype != torch.int8 or exps.dtype != torch.uint8 or tuple(q.shape) != (N, K) or \
+            tuple(exps.shape) != (N, (K + 31) // 32):
+        raise ValueError("a checkpoint is q (N x K int8) and exps (N x ceil(K / 32) uint8)")
+    return _ptr(q), _ld(q), _ptr(exps), _ld(exps)
+
+
+def _matrix(t, N, K, what, like=None):
+    """(pointer, row stride) of an N x K matrix (None: NULL)."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != (N, K):
+        raise ValueError(f"{what} must be {N} x {K}")
+    if like is not None:
+        _dtype(t, like)
+    return _ptr(t), _ld(t)
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def bigcn_checkpoint_groups(K: int) -> int:
+    return int(lib().bigcn_checkpoint_groups(K))
+
+
+def bigcn_checkpoint_pack(X, q, exps, stream=None):
+    """X (N x K, fp32, bf16 or fp16) to 8 bits: q (N x K int8) and exps
+    (N x ceil(K/32) uint8), views of rows of the strides that the header asks for
+    (:func:`checkpoint_buffers`)."""
+    N, K = X.shape
+    _check("bigcn_checkpoint_pack", lib().bigcn_checkpoint_pack(
+        _dtype(X), _ptr(X), N, K, _ld(X), *_kept(q, exps, N, K), _stream(stream)))
+
+
+def bigcn_checkpoint_unpack(q, exps, X, gamma=None, beta=None, stream=None):
+    """X = gamma v + beta from the checkpoint v."""
+    N, K = X.shape
+    _check("bigcn_checkpoint_unpack", lib().bigcn_checkpoint_unpack(
+        _dtype(X), *_kept(q, exps, N, K), N, K, _vector(gamma, K, "gamma"),
+        _vector(beta, K, "beta"), _ptr(X), _ld(X), _stream(stream)))
+
+
+def bigcn_layer_norm_forward(X, gamma, beta, eps, Y, mean=None, rstd=None, q=None, exps=None,
+                             stream=None):
+    """Y = gamma xhat + beta, xhat the rows of X normalised; mean and rstd (N fp32) and the
+    checkpoint of xhat where given. gamma, beta: None for 1, 0."""
+    N, K = X.shape
+    _check("bigcn_layer_norm_forward", lib().bigcn_layer_norm_forward(
+        _dtype(X), _ptr(X), N, K, _ld(X), _vector(gamma, K, "gamma"), _vector(beta, K, "beta"),
+        eps, *_matrix(Y, N, K, "Y", X), _vector(mean, N, "mean"), _vector(rstd, N, "rstd"),
+        *_kept(q, exps, N, K), _stream(stream)))
+
+
+def bigcn_layer_norm_backward_workspace_bytes(N: int, K: int) -> int:
+    return int(lib().bigcn_layer_norm_backward_workspace_bytes(N, K))
+
+
+def bigcn_layer_norm_backward(dY, gamma, rstd, workspace, X=None, mean=None, q=None, exps=None,
+                              dX=None, dgamma=None, dbeta=None, stream=None):
+    """The gradients of the norm's input and parameters (those given) from dY, with xhat from
+    X and mean or from the checkpoint q, exps. workspace: None where neither dgamma nor dbeta
+    is given."""
+    N, K = dY.shape
+    x, ldx = _matrix(X, N, K, "X", dY)
+    dx, lddx = _matrix(dX, N, K, "dX", dY)
+    _check("bigcn_layer_norm_backward", lib().bigcn_layer_norm_backward(
+        _dtype(dY), _ptr(dY), N, K, _ld(dY), _vector(gamma, K, "gamma"), x, ldx,
+        _vector(mean, N, "mean"), *_kept(q, exps, N, K), _vector(rstd, N, "rstd"), dx, lddx,
+        _vector(dgamma, K, "dgamma"), _vector(dbeta, K, "dbeta"), _ptr(workspace),
+        _bytes(workspace), _stream(stream)))
+
+
+def bigcn_checkpoint_weight_grad_workspace_bytes(N: int, K: int, F: int) -> int:
+    return int(lib().bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F))
+
+
+def bigcn_checkpoint_weight_grad(q, exps, dZ, workspace, dW, gamma=None, beta=None, db=None,
+                                 stream=None):
+    """dW (K x F fp32) and db (F) of Z = (gamma v + beta) W + b from the checkpoint v and dZ."""
+    N, F = dZ.shape
+    K = dW.shape[0]
+    if dW.dtype != torch.float32:
+        raise ValueError("dW must be float32")
+    dw, lddw = _matrix(dW, K, F, "dW")
+    _check("bigcn_checkpoint_weight_grad", lib().bigcn_checkpoint_weight_grad(
+        _dtype(dZ), *_kept(q, exps, N, K), N, K, _vector(gamma, K, "gamma"),
+        _vector(beta, K, "beta"), _ptr(dZ), F, _ld(dZ), dw, lddw, _vector(db, F, "db"),
+        _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
 # ------------------------------------------------- allocating conveniences ---
 def pack_rows(X, scale=None, shift=None, stream=None):
     N, K = X.shape
@@ -508,3 +632,58 @@ def layer_forward(X, Wt, rowptr, colidx, scale=None, shift=None, workspace=None,
     H = torch.empty((N, F), dtype=torch.float32, device=X.device)
     bigcn_layer_forward(X, scale, shift, Wt, rowptr, colidx, workspace, H, stream)
     return H
+
+
+def checkpoint_buffers(N, K, device):
+    """(q, exps) for a checkpoint of N x K: views of rows padded as the header asks."""
+    q = torch.empty((N, (K + 15) // 16 * 16), dtype=torch.int8, device=device)
+    groups = (K + 31) // 32
+    exps = torch.empty((N, (groups + 3) // 4 * 4), dtype=torch.uint8, device=device)
+    return q[:, :K], exps[:, :groups]
+
+
+def checkpoint_pack(X, stream=None):
+    q, exps = checkpoint_buffers(*X.shape, X.device)
+    bigcn_checkpoint_pack(X, q, exps, stream)
+    return q, exps
+
+
+def checkpoint_unpack(q, exps, dtype=torch.float32, gamma=None, beta=None, stream=None):
+    X = torch.empty(q.shape, dtype=dtype, device=q.device)
+    bigcn_checkpoint_unpack(q, exps, X, gamma, beta, stream)
+    return X
+
+
+def layer_norm_forward(X, gamma=None, beta=None, eps=1e-5, checkpoint=True, stream=None):
+    """(Y, mean, rstd, q, exps); without ``checkpoint`` the last two are None."""
+    N, K = X.shape
+    Y = torch.empty((N, K), dtype=X.dtype, device=X.device)
+    mean = torch.empty(N, dtype=torch.float32, device=X.device)
+    rstd = torch.empty_like(mean)
+    q, exps = checkpoint_buffers(N, K, X.device) if checkpoint else (None, None)
+    bigcn_layer_norm_forward(X, gamma, beta, eps, Y, mean, rstd, q, exps, stream)
+    return Y, mean, rstd, q, exps
+
+
+def layer_norm_backward(dY, gamma, rstd, X=None, mean=None, q=None, exps=None, stream=None):
+    """(dX, dgamma, dbeta) with xhat from X and mean or from q and exps."""
+    N, K = dY.shape
+    ws = torch.empty(bigcn_layer_norm_backward_workspace_bytes(N, K), dtype=torch.uint8,
+                     device=dY.device)
+    dX = torch.empty((N, K), dtype=dY.dtype, device=dY.device)
+    dgamma = torch.empty(K, dtype=torch.float32, device=dY.device)
+    dbeta = torch.empty_like(dgamma)
+    bigcn_layer_norm_backward(dY, gamma, rstd, ws, X, mean, q, exps, dX, dgamma, dbeta, stream)
+    return dX, dgamma, dbeta
+
+
+def checkpoint_weight_grad(q, exps, dZ, gamma=None, beta=None, stream=None):
+    """(dW, db)."""
+    N, F = dZ.shape
+    K = q.shape[1]
+    ws = torch.empty(bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F), dtype=torch.uint8,
+                     device=dZ.device)
+    dW = torch.empty((K, F), dtype=torch.float32, device=dZ.device)
+    db = torch.empty(F, dtype=torch.float32, device=dZ.device)
+    bigcn_checkpoint_weight_grad(q, exps, dZ, ws, dW, gamma, beta, db, stream)
+    return dW, db
