@@ -3,129 +3,692 @@
 //
 //   dW[k,j] = gamma_k sum_i v_ik dZ_ij + beta_k s_j,   s_j = db_j = sum_i dZ_ij.
 //
-// The rows are split into chunks whose partial sums a second kernel adds in order, so
-// that the result does not depend on scheduling.
+// The sum over the rows i runs on the tensor cores (tcgen05, bf16 operands, fp32
+// accumulators), and nothing is rounded on the way in: v = q 2^e has 7 significant bits
+// and is a bf16; dZ is one bf16 part (bf16), two (fp16: 8 + 3 bits, exact) or three (fp32,
+// within 2^-23 of it).
+//
+// Operands. M = 128 features a tile, N = the columns, the contraction over 32 rows a
+// stage. Both matrices are row-major, i.e. their features and columns lie along memory
+// rows, and the tensor core takes them that way (MN-major), so nothing is transposed: a
+// bf16 dZ goes by tensor copies from memory into its swizzled place; q (and an fp32 or
+// fp16 dZ) by tensor copies into a ring of raw slots, from which the workers expand it.
+//
+// Roles of a CTA (320 threads): warps 0-7, the workers, turn raw slots into operand
+// stages; they also keep the running sums. Warp 8 copies, warp 9 issues the MMAs. They meet
+// on mbarriers only:
+//   loaded[slot]   a slot's copies have landed         freed[slot]   it may be refilled
+//   filled[stage]  the workers have written a stage    used[stage]   its MMAs are done
+//   summed[half]   a block's MMAs are done             drained[half] its sums were taken
+//
+// Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
+// result per accumulating MMA, always towards 0; 1080 MMAs gave 2.2e-5), so an accumulator
+// takes kDrain stages, about 40 MMAs (8e-7), and is then added in fp32 to the workers'
+// registers: 256 accumulator columns in each half of tensor memory, one filling while the
+// other drains, 128 sums a thread.
+//
+// Split. A CTA holds 256 / NT feature tiles (`mt` of them, fewer in small calls), so that
+// dZ is read once for that many; the rows are split so that the grid is about one CTA per
+// SM (kGradCtas), a last group of fewer tiles into fewer parts. A second kernel adds the
+// parts in order, sums s_j, and applies gamma and beta. The columns of dZ are summed by the
+// CTA that has them in shared memory anyway: of the groups of feature tiles that read the
+// same rows, group g takes the g-th 64 columns.
+//
+// What bounds it: tensor time where dZ is fp32 (three parts: 58 us of MMAs against 39 us
+// of copies at 232,965 x 602 x 128), reading dZ once per group of tiles and the workers'
+// expansion elsewhere.
 #include "checkpoint.cuh"
 #include "launch.cuh"
+#include "tc_rows.cuh"
 
 namespace bigcn {
+
+__device__ unsigned int g_grad_timeouts;
+
 namespace {
 
-constexpr int kGradThreads = 256;
-constexpr int kTileK = 64, kTileF = 64, kTileRows = 16;
-constexpr int kMaxGradChunks = 64;
+constexpr int kGradCtas = 152;          // SMs of the card
+constexpr int kWorkers = 256;
+constexpr int kWorkerWarps = kWorkers / 32;
+constexpr int kCopyWarp = kWorkerWarps, kMmaWarp = kWorkerWarps + 1;
+constexpr int kGradThreads = kWorkers + 64;
+constexpr int kRows = kAtomRows;        // rows of a stage
+constexpr int kAccCols = 256;           // accumulator columns of half the tensor memory
+constexpr int kSumsPerThread = kAccCols / 2;
 constexpr size_t kAlign = 256;
+constexpr int kSmemMost = 227 * 1024 - 1024 - 3072;   // less alignment and static memory
 
-struct GradArgs {
-    const int8_t *q;
-    int64_t ldq;
+__host__ __device__ constexpr int round_up_to(int x, int a) { return (x + a - 1) / a * a; }
+
+// Shared memory of a variant: NT columns, PARTS bf16 parts of dZ, kTma: dZ comes by tensor
+// copies (else its rows are not 16-byte aligned and the workers load it).
+template <int NT, int PARTS, bool kTma>
+struct GradShape {
+    static constexpr int kTiles = kAccCols / NT;
+    static constexpr bool kDirect = kTma && PARTS == 1;     // copied as an operand
+    static constexpr int kElem = PARTS == 3 ? 4 : 2;
+    static constexpr int kSlotZ = kTma ? kRows * NT * kElem : 0;
+    static constexpr int kSlotQ = kTiles * kRows * 128;
+    static constexpr int kSlot = round_up_to(kSlotZ + kSlotQ + kTiles * kRows * 4, 1024);
+    static constexpr int kOpA = kTiles * 2 * kAtomBytes;
+    static constexpr int kPart = NT / 64 * kAtomBytes;
+    static constexpr int kOp = kOpA + (kDirect ? 0 : PARTS * kPart);
+    static constexpr int kStages = 3 * (kOp + kSlot) <= kSmemMost ? 3 : 2;
+    static constexpr int kFit = (kSmemMost - kStages * kOp) / kSlot;
+    static constexpr int kSlots = kFit < 8 ? kFit : 8;
+    static constexpr int kSmem = 1024 + kStages * kOp + kSlots * kSlot;
+    // About 40 accumulating MMAs (two per stage and part) between two drains.
+    static constexpr int kDrain = PARTS == 1 ? 20 : PARTS == 2 ? 10 : 7;
+    static_assert(kSlots >= 2, "shared memory per CTA");
+};
+
+struct GradParams {
+    CUtensorMap q_map;       // K rounded up to 16 bytes x N
+    CUtensorMap z_map;       // F x N of dZ (kTma)
     const uint8_t *exps;
     int64_t lde;
     int64_t N;
-    int K;
     const void *dZ;
-    int F;
     int64_t lddz;
-    float *partial;          // chunks x K x F
-    float *colsum;           // chunks x F
-    int chunks;
+    int F;
+    int nt;                  // column tiles
+    int64_t tiles;           // feature tiles
+    int mt;                  // feature tiles of a group
+    int64_t groups;
+    int parts_full, parts_last;      // runs of rows of a group, of the last group
+    float *partial;          // [nt][tiles][parts_full][NT][128]
+    float *colsum;           // [parts_full][nt * NT]
 };
 
-// A 64 x 64 tile of a chunk's partial product; 4 x 4 outputs a thread. The blocks of
-// the first feature tile also sum dZ's columns.
-template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_tile_kernel(const GradArgs a) {
-    __shared__ float sv[kTileRows][kTileK];
-    __shared__ float sz[kTileRows][kTileF];
-    const int k0 = blockIdx.x * kTileK, f0 = blockIdx.y * kTileF, c = blockIdx.z;
-    const int64_t r0 = a.N * c / a.chunks, r1 = a.N * (c + 1) / a.chunks;
-    const int tk = threadIdx.x / 16, tf = threadIdx.x % 16;
-    float acc[4][4] = {};
-    float colsum = 0.0f;
-    for (int64_t r = r0; r < r1; r += kTileRows) {
-        for (int t = threadIdx.x; t < kTileRows * kTileK; t += kGradThreads) {
-            const int64_t i = r + t / kTileK;
-            const int k = k0 + t % kTileK;
-            sv[t / kTileK][t % kTileK] =
-                i < r1 && k < a.K
-                    ? float(a.q[i * a.ldq + k]) * unpack_factor(a.exps[i * a.lde + k / kGroup])
-                    : 0.0f;
-        }
-        for (int t = threadIdx.x; t < kTileRows * kTileF; t += kGradThreads) {
-            const int64_t i = r + t / kTileF;
-            const int f = f0 + t % kTileF;
-            sz[t / kTileF][t % kTileF] =
-                i < r1 && f < a.F ? to_f32(static_cast<const T *>(a.dZ)[i * a.lddz + f]) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kTileRows; ++e)
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    acc[p][w] = fmaf(sv[e][tk + 16 * p], sz[e][tf + 16 * w], acc[p][w]);
-        if (k0 == 0 && threadIdx.x < kTileF)
-            for (int e = 0; e < kTileRows; ++e) colsum += sz[e][threadIdx.x];
-        __syncthreads();
-    }
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int k = k0 + tk + 16 * p, f = f0 + tf + 16 * w;
-            if (k < a.K && f < a.F) a.partial[(int64_t(c) * a.K + k) * a.F + f] = acc[p][w];
-        }
-    if (k0 == 0 && threadIdx.x < kTileF && f0 + threadIdx.x < a.F)
-        a.colsum[int64_t(c) * a.F + f0 + threadIdx.x] = colsum;
+template <typename T> __device__ __forceinline__ float dz_at(const GradParams &p, int64_t i, int j) {
+    return i < p.N && j < p.F ? to_f32(static_cast<const T *>(p.dZ)[i * p.lddz + j]) : 0.0f;
 }
 
-__global__ void __launch_bounds__(kGradThreads)
-grad_sum_kernel(const float *__restrict__ partial, const float *__restrict__ colsum, int chunks,
-                int K, int F, const float *__restrict__ gamma, const float *__restrict__ beta,
-                float *__restrict__ dW, int64_t lddw, float *__restrict__ db) {
-    const int64_t n = int64_t(K) * F;
-    for (int64_t t = int64_t(blockIdx.x) * kGradThreads + threadIdx.x; t < n;
-         t += int64_t(gridDim.x) * kGradThreads) {
-        const int64_t k = t / F, f = t % F;
-        float s = 0.0f, cs = 0.0f;
-        for (int c = 0; c < chunks; ++c) {
-            s += partial[int64_t(c) * n + t];
-            cs += colsum[int64_t(c) * F + f];
-        }
-        dW[k * lddw + f] = fmaf(gamma ? gamma[k] : 1.0f, s, beta ? beta[k] * cs : 0.0f);
-        if (db && k == 0) db[f] = cs;
+// Four int8 to bf16 pairs, exactly: 0x43qq is 128 + (q & 127), or 256 + q with q's sign bit
+// cleared, so that subtracting 0x43(q & 128), 128 or 256, leaves q; times 2^e.
+__device__ __forceinline__ void expand4(uint32_t w, __nv_bfloat162 factor, uint32_t &lo,
+                                        uint32_t &hi) {
+    const uint32_t x[2] = {__byte_perm(w, 0x43434343u, 0x4140), __byte_perm(w, 0x43434343u, 0x4342)};
+    uint32_t r[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t a = x[h] & 0xFF7FFF7Fu, b = x[h] & 0xFF80FF80u;
+        const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a),
+                                                 *reinterpret_cast<const __nv_bfloat162 *>(&b)),
+                                         factor);
+        r[h] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    lo = r[0];
+    hi = r[1];
+}
+
+// 2^(b - 127) in both halves, as unpack_factor.
+__device__ __forceinline__ __nv_bfloat162 bf16_factor(uint32_t b) {
+    const uint32_t f = b == kNanByte ? 0x7FC0u : b << 7, f2 = f | (f << 16);
+    return *reinterpret_cast<const __nv_bfloat162 *>(&f2);
+}
+
+template <int PARTS>
+__device__ __forceinline__ void parts_of(float v0, float v1, uint32_t (&out)[3]) {
+    if constexpr (PARTS == 1) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(v0, v1);     // bf16 already: exact
+        out[0] = *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        bf16_parts(v0, v1, out[0], out[1], out[2]);     // of 11 bits the third part is 0
     }
 }
 
-int64_t grad_chunks(int64_t N, int K, int F) {
-    const int64_t tiles = ((int64_t(K) + kTileK - 1) / kTileK) * ((F + kTileF - 1) / kTileF);
-    int64_t c = (1024 + tiles - 1) / tiles;
-    if (c > kMaxGradChunks) c = kMaxGradChunks;
-    if (c > (N + kTileRows - 1) / kTileRows) c = (N + kTileRows - 1) / kTileRows;
-    return c < 1 ? 1 : c;
+__device__ __forceinline__ float2 bf16_pair(uint32_t u) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+
+template <typename T, int NT, int PARTS, bool kTma>
+__global__ void __launch_bounds__(kGradThreads, 1)
+grad_rows_kernel(const __grid_constant__ GradParams p) {
+    using S = GradShape<NT, PARTS, kTma>;
+    constexpr int kSlots = S::kSlots, kStages = S::kStages, kDrain = S::kDrain;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t loaded[kSlots], freed[kSlots], filled[kStages], used[kStages],
+        summed[2], drained[2], done;
+    __shared__ float colpart[kWorkerWarps][64];
+    __shared__ uint32_t tmem_base, stop;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    unsigned char *const mem = smem_raw + (base - raw);
+    constexpr int kSlot0 = kStages * S::kOp;            // slots follow the stages
+
+    // This CTA's group of feature tiles, run of rows and columns.
+    const int ny = blockIdx.x % p.nt;
+    const int64_t r = blockIdx.x / p.nt, full = (p.groups - 1) * p.parts_full;
+    const int64_t group = r < full ? r % (p.groups - 1) : p.groups - 1;
+    const int run = int(r < full ? r / (p.groups - 1) : r - full);
+    const int runs = r < full ? p.parts_full : p.parts_last;
+    const int64_t tile0 = group * p.mt;
+    const int mt = int(min(int64_t(p.mt), p.tiles - tile0));
+    const int64_t stages = (p.N + kRows - 1) / kRows;
+    const int64_t st0 = stages * run / runs;
+    const int n = int(stages * (run + 1) / runs - st0);
+    const int n0 = ny * NT, cols = min(NT, p.F - n0), atoms = (cols + 63) / 64;
+    const bool sums_cols = group < NT / 64;             // of the columns n0 + 64 group ..
+
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_addr(&tmem_base)),
+                     "r"(2 * kAccCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(smem_addr(&loaded[s]), 33);       // the copy warp's lanes, and its bytes
+            mbar_init(smem_addr(&freed[s]), S::kDirect ? 1 : kWorkerWarps);
+        }
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_addr(&filled[s]), kWorkerWarps);
+            mbar_init(smem_addr(&used[s]), 1);
+        }
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(smem_addr(&summed[h]), 1);
+            mbar_init(smem_addr(&drained[h]), kWorkerWarps);
+        }
+        mbar_init(smem_addr(&done), 1);
+        stop = 0u;
+        mbar_fence_init();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    volatile uint32_t *const stopv = &stop;
+
+    float sum[kSumsPerThread];
+    float colsum[8];
+#pragma unroll
+    for (int c = 0; c < kSumsPerThread; ++c) sum[c] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) colsum[c] = 0.0f;
+
+    if (warp == kCopyWarp) {
+        const uint32_t bytes = uint32_t(mt * kRows * 128 + (kTma ? atoms * kRows * 64 * S::kElem : 0));
+        int issued = 0;
+        for (int st = 0; st < n; ++st) {
+            const int s = st % kSlots;
+            const bool go = st < kSlots || wait_unless(smem_addr(&freed[s]),
+                                                       uint32_t(st / kSlots - 1) & 1u, stopv);
+            if (!__all_sync(kFullMask, go)) {
+                *stopv = 1u;
+                break;
+            }
+            const uint32_t slot = base + uint32_t(kSlot0 + s * S::kSlot);
+            const uint32_t bar = smem_addr(&loaded[s]);
+            const int64_t row0 = (st0 + st) * kRows;
+            // Scale bytes: lane = row, four groups (128 features) a copy.
+            const bool in = row0 + lane < p.N;
+            const uint8_t *e = p.exps + (in ? (row0 + lane) * p.lde + tile0 * 4 : 0);
+            for (int t = 0; t < mt; ++t)
+                copy4(slot + uint32_t(S::kSlotZ + S::kSlotQ + (t * kRows + lane) * 4),
+                      in ? e + t * 4 : e, in ? 4u : 0u);
+            if (lane == 0) {
+                mbar_expect(bar, bytes);
+                if constexpr (kTma)
+                    for (int a = 0; a < atoms; ++a)
+                        tma_load(slot + uint32_t(a * kRows * 64 * S::kElem), &p.z_map, n0 + 64 * a,
+                                 int(row0), bar);
+                for (int t = 0; t < mt; ++t)
+                    tma_load(slot + uint32_t(S::kSlotZ + t * kRows * 128), &p.q_map,
+                             int(tile0 + t) * 128, int(row0), bar);
+            }
+            copies_arrive(bar);
+            issued = st + 1;
+            __syncwarp();
+        }
+        // What is still in flight lands before the shared memory is given up.
+        for (int st = max(0, issued - kSlots); st < issued; ++st)
+            mbar_wait(smem_addr(&loaded[st % kSlots]), uint32_t(st / kSlots) & 1u);
+    } else if (warp == kMmaWarp) {
+        if (lane == 0) {
+            const uint32_t idesc = atom_idesc(round_up_to(cols, 16));
+            bool any = false;
+            for (int st = 0; st < n; ++st) {
+                const int s = st % kSlots, o = st % kStages;
+                const int block = st / kDrain, half = block & 1, at = st % kDrain;
+                bool go = wait_unless(smem_addr(&filled[o]), uint32_t(st / kStages) & 1u, stopv);
+                if (S::kDirect)
+                    go = go && wait_unless(smem_addr(&loaded[s]), uint32_t(st / kSlots) & 1u, stopv);
+                if (at == 0 && block >= 2)
+                    go = go && wait_unless(smem_addr(&drained[half]), uint32_t(block / 2 - 1) & 1u,
+                                           stopv);
+                if (!go) {
+                    *stopv = 1u;
+                    break;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t a0 = base + uint32_t(o * S::kOp);
+                const uint32_t b0 = S::kDirect ? base + uint32_t(kSlot0 + s * S::kSlot)
+                                               : a0 + uint32_t(S::kOpA);
+#pragma unroll
+                for (int k = 0; k < kRows / 16; ++k)
+                    for (int t = 0; t < mt; ++t)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part)
+                            mma_rows(tmem + uint32_t(half * kAccCols + t * NT),
+                                     atom_desc(a0 + uint32_t(t * 2 * kAtomBytes + k * 2048)),
+                                     atom_desc(b0 + uint32_t(part * S::kPart + k * 2048)), idesc,
+                                     at > 0 || k > 0 || part > 0);
+                any = true;
+                mma_commit(smem_addr(&used[o]));
+                if (S::kDirect) mma_commit(smem_addr(&freed[s]));
+                if (at == kDrain - 1 || st == n - 1) mma_commit(smem_addr(&summed[half]));
+            }
+            if (any) mma_commit(smem_addr(&done));
+            else mbar_arrive(smem_addr(&done));
+        }
+        __syncwarp();
+    } else {
+        // Worker: row `row` of a stage, 16 features 16 c .. of each tile, 8 columns 8 c .. of
+        // each atom. Loaded without tensor copies, dZ is taken four rows a warp, a column per
+        // lane, a stage ahead.
+        const int row = tid >> 3, c = tid & 7;
+        const int quad = warp & 3, colhalf = warp >> 2;
+        constexpr int kLoadCols = kTma ? 1 : NT / 32;
+        float z[kLoadCols][4];
+        auto load = [&](int st) {
+            if constexpr (!kTma) {
+                const int64_t i = (st0 + st) * kRows + 4 * warp;
+#pragma unroll
+                for (int q = 0; q < kLoadCols; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        z[q][e] = st < n && n0 + 32 * q < p.F ? dz_at<T>(p, i + e, n0 + 32 * q + lane)
+                                                              : 0.0f;
+            }
+        };
+        // Adds the accumulators of block b to the running sums.
+        auto drain = [&](int b) -> bool {
+            const bool go = wait_unless(smem_addr(&summed[b & 1]), uint32_t(b / 2) & 1u, stopv);
+            if (!__all_sync(kFullMask, go)) return false;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = tmem + (uint32_t(32 * quad) << 16) +
+                                uint32_t((b & 1) * kAccCols + colhalf * kSumsPerThread);
+#pragma unroll
+            for (int w = 0; w < kSumsPerThread / 32; ++w) {
+                if (colhalf * kSumsPerThread + 32 * w < mt * NT) {
+                    uint32_t acc[32];
+                    tmem_ld32(at + uint32_t(32 * w), acc);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[32 * w + j] += __uint_as_float(acc[j]);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&drained[b & 1]));
+            return true;
+        };
+        int taken = 0;                  // blocks drained
+        bool ok = true;
+        load(0);
+#pragma unroll 1
+        for (int st = 0; st < n; ++st) {
+            // A block is drained kStages stages after its end: its MMAs are done by then.
+            if (st >= (taken + 1) * kDrain + kStages) {
+                ok = drain(taken);
+                if (!ok) break;
+                ++taken;
+            }
+            const int s = st % kSlots, o = st % kStages;
+            bool go = wait_unless(smem_addr(&loaded[s]), uint32_t(st / kSlots) & 1u, stopv);
+            if (st >= kStages)
+                go = go && wait_unless(smem_addr(&used[o]), uint32_t(st / kStages - 1) & 1u, stopv);
+            ok = __all_sync(kFullMask, go);
+            if (!ok) break;
+            const unsigned char *slot = mem + kSlot0 + s * S::kSlot;
+            unsigned char *op = mem + o * S::kOp;
+            // A: 16 features of a row to two 16-byte chunks. Lanes of the second atom write
+            // theirs in the other order, so that 8 lanes cover all banks.
+#pragma unroll 2
+            for (int t = 0; t < mt; ++t) {
+                const unsigned char *sq = slot + S::kSlotZ + t * kRows * 128;
+                const uint4 q = *reinterpret_cast<const uint4 *>(sq + row * 128 + c * 16);
+                const __nv_bfloat162 f =
+                    bf16_factor(slot[S::kSlotZ + S::kSlotQ + (t * kRows + row) * 4 + (c >> 1)]);
+                uint4 v[2];
+                expand4(q.x, f, v[0].x, v[0].y);
+                expand4(q.y, f, v[0].z, v[0].w);
+                expand4(q.z, f, v[1].x, v[1].y);
+                expand4(q.w, f, v[1].z, v[1].w);
+                unsigned char *atom = op + (2 * t + (c >> 2)) * kAtomBytes;
+                const bool swap = c >= 4;
+                const int ch = 2 * (c & 3);
+                *reinterpret_cast<uint4 *>(atom + atom_offset(row, ch + (swap ? 1 : 0))) =
+                    swap ? v[1] : v[0];
+                *reinterpret_cast<uint4 *>(atom + atom_offset(row, ch + (swap ? 0 : 1))) =
+                    swap ? v[0] : v[1];
+            }
+            // B: dZ's parts, and its columns' sums.
+            if constexpr (S::kDirect) {
+                if (sums_cols && int(group) < atoms) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(
+                        slot + int(group) * kAtomBytes + atom_offset(row, c));
+                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = bf16_pair(w[e]);
+                        colsum[2 * e] += f.x;
+                        colsum[2 * e + 1] += f.y;
+                    }
+                }
+            } else if constexpr (kTma) {
+#pragma unroll
+                for (int a = 0; a < NT / 64; ++a) {
+                    if (a >= atoms) break;
+                    float v[8];
+                    if constexpr (PARTS == 3) {     // 32 bytes a lane, halves in the order
+                        const unsigned char *z0 = slot + (a * kRows + row) * 256 + c * 32;
+                        const bool swap = c >= 4;   // that spreads 8 lanes over all banks
+                        const float4 x = *reinterpret_cast<const float4 *>(z0 + (swap ? 16 : 0));
+                        const float4 y = *reinterpret_cast<const float4 *>(z0 + (swap ? 0 : 16));
+                        const float4 lo = swap ? y : x, hi = swap ? x : y;
+                        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
+                        v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+                    } else {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(
+                            slot + (a * kRows + row) * 128 + c * 16);
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 f =
+                                __half22float2(*reinterpret_cast<const __half2 *>(&w[e]));
+                            v[2 * e] = f.x;
+                            v[2 * e + 1] = f.y;
+                        }
+                    }
+                    if (sums_cols && a == int(group))
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) colsum[e] += v[e];
+                    uint32_t part[4][3];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) parts_of<PARTS>(v[2 * e], v[2 * e + 1], part[e]);
+                    unsigned char *dst = op + S::kOpA + a * kAtomBytes + atom_offset(row, c);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q)
+                        *reinterpret_cast<uint4 *>(dst + q * S::kPart) =
+                            make_uint4(part[0][q], part[1][q], part[2][q], part[3][q]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kLoadCols; ++q) {
+                    if (q / 2 >= atoms) break;
+                    if (sums_cols && q / 2 == int(group))
+                        colsum[q % 2] += (z[q][0] + z[q][1]) + (z[q][2] + z[q][3]);
+                    // Neighbouring lanes exchange a row's value: the even one writes the pair
+                    // of columns of rows 0 and 2, the odd one of rows 1 and 3.
+                    const bool odd = lane & 1;
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float got =
+                            __shfl_xor_sync(kFullMask, odd ? z[q][e] : z[q][e + 1], 1);
+                        uint32_t part[3];
+                        parts_of<PARTS>(odd ? got : z[q][e], odd ? z[q][e + 1] : got, part);
+                        const int rr = 4 * warp + e + (odd ? 1 : 0);
+                        const int col = 32 * (q % 2) + (lane & ~1);
+                        unsigned char *dst = op + S::kOpA + (q / 2) * kAtomBytes +
+                                             atom_offset(rr, col >> 3) + (col & 7) * 2;
+#pragma unroll
+                        for (int w = 0; w < PARTS; ++w)
+                            *reinterpret_cast<uint32_t *>(dst + w * S::kPart) = part[w];
+                    }
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (!S::kDirect) mbar_arrive(smem_addr(&freed[s]));
+                mbar_arrive(smem_addr(&filled[o]));
+            }
+            load(st + 1);
+        }
+        for (; ok && taken * kDrain < n; ++taken) ok = drain(taken);
+        if (!ok) *stopv = 1u;
+    }
+
+    // Every MMA has ended once `done` completes. A CTA whose waits ran out writes nothing.
+    const bool ended = mbar_wait(smem_addr(&done), 0u);
+    const bool ok = __syncthreads_and(ended && *stopv == 0u) != 0;
+    if (!ok && tid == 0) atomicAdd(&g_grad_timeouts, 1u);
+    allow_dependent_launch();
+    if (ok && warp < kWorkerWarps) {
+        const int f = 32 * (warp & 3) + lane, colhalf = warp >> 2;
+#pragma unroll
+        for (int c = 0; c < kSumsPerThread; ++c) {
+            const int at = colhalf * kSumsPerThread + c, t = at / NT, col = at % NT;
+            if (t < mt && col < cols)
+                p.partial[(((int64_t(ny) * p.tiles + tile0 + t) * p.parts_full + run) * NT + col) * 128 +
+                          f] = sum[c];
+        }
+        if (sums_cols && int(group) < atoms) {
+            // Rows of a warp, then the warps in order.
+            if constexpr (kTma) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    colsum[e] += __shfl_xor_sync(kFullMask, colsum[e], 8);
+                    colsum[e] += __shfl_xor_sync(kFullMask, colsum[e], 16);
+                    if (lane < 8) colpart[warp][8 * lane + e] = colsum[e];
+                }
+            } else {
+                colpart[warp][lane] = colsum[0];
+                colpart[warp][32 + lane] = colsum[1];
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (tid < 64 && 64 * int(group) + tid < cols) {
+                float t = 0.0f;
+                for (int w = 0; w < kWorkerWarps; ++w) t += colpart[w][tid];
+                p.colsum[int64_t(run) * p.nt * NT + n0 + 64 * int(group) + tid] = t;
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == kMmaWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+                     "r"(2 * kAccCols));
+}
+
+// The runs' sums added in order, and gamma, beta: a block takes four columns of a tile of 128
+// features. A warp adds every eighth run (four features a lane), the eight sums are added in
+// order.
+constexpr int kSumThreads = 256;
+struct GradSumParams {
+    const float *partial;
+    const float *colsum;
+    int64_t tiles;
+    int64_t groups;
+    int parts_full, parts_last;
+    int mt;
+    int NT;
+    int padded;              // nt * NT
+    int K;
+    int F;
+    const float *gamma;
+    const float *beta;
+    float *dW;
+    int64_t lddw;
+    float *db;
+};
+
+__global__ void __launch_bounds__(kSumThreads) grad_sum_kernel(const GradSumParams p) {
+    __shared__ __align__(16) float part[8][4][128];
+    __shared__ float cpart[64][4];
+    __shared__ float csum[4];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t tile = blockIdx.x % p.tiles;
+    const int j0 = int(blockIdx.x / p.tiles) * 4, ny = j0 / p.NT, col0 = j0 % p.NT;
+    const int runs = tile / p.mt == p.groups - 1 ? p.parts_last : p.parts_full;
+    // The group that summed these columns.
+    const int cruns = col0 / 64 == p.groups - 1 ? p.parts_last : p.parts_full;
+    grid_dependency_wait();
+    {
+        const int c = tid & 3;
+        float t = 0.0f;
+        if (j0 + c < p.F)
+            for (int s = tid >> 2; s < cruns; s += 64) t += p.colsum[int64_t(s) * p.padded + j0 + c];
+        cpart[tid >> 2][c] = t;
+    }
+    float4 acc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float4 *src = reinterpret_cast<const float4 *>(
+                            p.partial + ((int64_t(ny) * p.tiles + tile) * p.parts_full * p.NT + col0) * 128) +
+                        lane;
+    for (int s = warp; s < runs; s += 8)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (j0 + c < p.F) {
+                const float4 v = src[(int64_t(s) * p.NT + c) * 32];
+                acc[c].x += v.x, acc[c].y += v.y, acc[c].z += v.z, acc[c].w += v.w;
+            }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) *reinterpret_cast<float4 *>(&part[warp][c][4 * lane]) = acc[c];
+    __syncthreads();
+    if (tid < 4) {
+        float t = 0.0f;
+        const int used = min(cruns, 64);
+        for (int s = 0; s < used; ++s) t += cpart[s][tid];
+        csum[tid] = t;
+        if (tile == 0 && p.db && j0 + tid < p.F) p.db[j0 + tid] = t;
+    }
+    __syncthreads();
+    for (int q = tid; q < 512; q += kSumThreads) {
+        const int f = q >> 2, c = q & 3;
+        const int64_t k = tile * 128 + f;
+        if (k >= p.K || j0 + c >= p.F) continue;
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += part[w][c][f];
+        const float g = p.gamma ? __ldg(p.gamma + k) : 1.0f;
+        p.dW[k * p.lddw + j0 + c] = p.beta ? fmaf(g, t, __ldg(p.beta + k) * csum[c]) : g * t;
+    }
+}
+
+// How a call is cut into CTAs.
+struct GradPlan {
+    int NT, nt, mt, parts_full, parts_last;
+    int64_t tiles, groups;
+    size_t partial_bytes, colsum_bytes;
+};
+
+// NT: the widest tile that F fills and for which there are as many groups of feature tiles
+// as 64-column atoms to sum (each sums one); at most `most`. mt: all the tiles that fit
+// unless runs of rows get shorter than 8 stages, where fewer tiles and longer runs mean
+// less to add up: 2708 x 1433 x 64, fp32.
+GradPlan grad_plan(int64_t N, int K, int F, int most) {
+    GradPlan g;
+    g.tiles = (int64_t(K) + 127) / 128;
+    g.NT = 64;
+    for (int NT = 128; NT <= most; NT *= 2)
+        if (F > NT / 2 && (g.tiles + kAccCols / NT - 1) / (kAccCols / NT) >= NT / 64) g.NT = NT;
+    g.nt = int((int64_t(F) + g.NT - 1) / g.NT);
+    const int64_t stages = (N + kRows - 1) / kRows;
+    const int64_t longest = stages / 4 > 1 ? stages / 4 : 1;       // runs of 4 stages or more
+    auto runs = [&](int64_t mt) {
+        int64_t s = kGradCtas * mt / (g.tiles * g.nt);
+        s = s < longest ? s : longest;
+        return s > 1 ? s : 1;
+    };
+    g.mt = kAccCols / g.NT;
+    if (g.mt > g.tiles) g.mt = int(g.tiles);
+    while (g.mt > 1 && stages / runs(g.mt) < 8) g.mt = (g.mt + 1) / 2;
+    g.groups = (g.tiles + g.mt - 1) / g.mt;
+    g.parts_full = int(runs(g.mt));
+    g.parts_last = int(runs(g.tiles - (g.groups - 1) * g.mt));
+    if (g.groups == 1) g.parts_full = g.parts_last;
+    g.partial_bytes = size_t(g.nt) * size_t(g.tiles) * size_t(g.parts_full) * size_t(g.NT) * 128 * 4;
+    g.colsum_bytes = size_t(g.parts_full) * size_t(g.nt) * size_t(g.NT) * 4;
+    return g;
 }
 
 size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+size_t plan_bytes(const GradPlan &g) { return round_up(g.partial_bytes) + round_up(g.colsum_bytes); }
 
-template <typename T>
-void launch_grad(const GradArgs &a, cudaStream_t s) {
-    grad_tile_kernel<T><<<dim3(unsigned((a.K + kTileK - 1) / kTileK),
-                               unsigned((a.F + kTileF - 1) / kTileF), unsigned(a.chunks)),
-                          kGradThreads, 0, s>>>(a);
+// dZ's widest tile: loaded by the workers it is kept in registers a stage ahead, 128
+// columns of it.
+constexpr int kMostTma = 256, kMostLoaded = 128;
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                                const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps (the library links no driver); nullptr without one.
+EncodeTiled encoder() {
+    static const EncodeTiled fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
+                                             &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// A map of `rows` rows of `width` elements, boxes of box x kRows.
+bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
+            int64_t rows, int64_t row_bytes, int box, bool swizzle) {
+    const EncodeTiled fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {cuuint64_t(width), cuuint64_t(rows)};
+    const cuuint64_t strides[1] = {cuuint64_t(row_bytes)};
+    const cuuint32_t boxes[2] = {cuuint32_t(box), cuuint32_t(kRows)};
+    const cuuint32_t steps[2] = {1, 1};
+    return fn(map, type, 2, const_cast<void *>(base), dims, strides, boxes, steps,
+              CU_TENSOR_MAP_INTERLEAVE_NONE,
+              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int NT, int PARTS, bool kTma>
+void launch_rows(const GradParams &p, unsigned grid, cudaStream_t s) {
+    using S = GradShape<NT, PARTS, kTma>;
+    cudaFuncSetAttribute(grad_rows_kernel<T, NT, PARTS, kTma>,
+                         cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    grad_rows_kernel<T, NT, PARTS, kTma><<<grid, kGradThreads, S::kSmem, s>>>(p);
+}
+
+template <typename T, int PARTS>
+void launch_type(const GradParams &p, int NT, bool tma, unsigned grid, cudaStream_t s) {
+    if (tma && NT == 256) launch_rows<T, 256, PARTS, true>(p, grid, s);
+    else if (tma && NT == 128) launch_rows<T, 128, PARTS, true>(p, grid, s);
+    else if (tma) launch_rows<T, 64, PARTS, true>(p, grid, s);
+    else if (NT == 128) launch_rows<T, 128, PARTS, false>(p, grid, s);
+    else launch_rows<T, 64, PARTS, false>(p, grid, s);
 }
 
 }  // namespace
+
+uint32_t take_grad_timeouts() {
+    unsigned int n = 0;
+    const unsigned int zero = 0;
+    if (cudaMemcpyFromSymbol(&n, g_grad_timeouts, sizeof(n)) != cudaSuccess ||
+        cudaMemcpyToSymbol(g_grad_timeouts, &zero, sizeof(zero)) != cudaSuccess) {
+        cudaGetLastError();
+        return ~0u;
+    }
+    return n;
+}
+
 }  // namespace bigcn
 
 using namespace bigcn;
 
 extern "C" size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_t F) {
-    if (N < 0 || N > int64_t(INT32_MAX) || K < 1 || F < 1 ||
-        int64_t(K) > kMaxElems / 4096 / F)
+    if (N < 0 || N > int64_t(INT32_MAX) || K < 1 || F < 1 || int64_t(K) > kMaxElems / (1 << 20) / F)
         return 0;
-    const size_t c = size_t(grad_chunks(N, K, F));
-    return round_up(c * size_t(K) * size_t(F) * 4) + round_up(c * size_t(F) * 4);
+    const size_t a = plan_bytes(grad_plan(N, K, F, kMostTma));
+    const size_t b = plan_bytes(grad_plan(N, K, F, kMostLoaded));
+    return a > b ? a : b;
 }
 
 extern "C" bigcn_status bigcn_checkpoint_weight_grad(
@@ -167,16 +730,40 @@ extern "C" bigcn_status bigcn_checkpoint_weight_grad(
         }
         return BIGCN_OK;
     }
-    const int chunks = int(grad_chunks(N, K, F));
-    float *partial = static_cast<float *>(workspace);
-    float *colsum = reinterpret_cast<float *>(static_cast<char *>(workspace) +
-                                              round_up(size_t(chunks) * size_t(K) * F * 4));
-    const GradArgs a{q, ldq, exps, lde, N, K, dZ, F, lddz, partial, colsum, chunks};
-    if (dtype == BIGCN_F32) launch_grad<float>(a, s);
-    else if (dtype == BIGCN_BF16) launch_grad<__nv_bfloat16>(a, s);
-    else launch_grad<__half>(a, s);
-    const int64_t blocks = (int64_t(K) * F + kGradThreads - 1) / kGradThreads;
-    grad_sum_kernel<<<unsigned(blocks < 4096 ? blocks : 4096), kGradThreads, 0, s>>>(
-        partial, colsum, chunks, K, F, gamma, beta, dW, lddw, db);
+
+    GradParams p;
+    const int64_t width = (int64_t(K) + 15) / 16 * 16;
+    if (!encode(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, false))
+        return BIGCN_ERR_CUDA;
+    const CUtensorMapDataType type = dtype == BIGCN_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : dtype == BIGCN_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                           : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    // Tensor copies want rows that start on 16-byte boundaries.
+    const int64_t zrow = lddz * int64_t(es);
+    const bool tma = aligned_to(dZ, 16) && zrow % 16 == 0 &&
+                     encode(&p.z_map, type, dZ, F, N, zrow, 64, dtype == BIGCN_BF16);
+    const GradPlan g = grad_plan(N, K, F, tma ? kMostTma : kMostLoaded);
+    p.exps = exps;
+    p.lde = lde;
+    p.N = N;
+    p.dZ = dZ;
+    p.lddz = lddz;
+    p.F = F;
+    p.nt = g.nt;
+    p.tiles = g.tiles;
+    p.mt = g.mt;
+    p.groups = g.groups;
+    p.parts_full = g.parts_full;
+    p.parts_last = g.parts_last;
+    p.partial = static_cast<float *>(workspace);
+    p.colsum = reinterpret_cast<float *>(static_cast<char *>(workspace) + round_up(g.partial_bytes));
+    const int64_t grid = ((g.groups - 1) * g.parts_full + g.parts_last) * g.nt;
+    if (dtype == BIGCN_F32) launch_type<float, 3>(p, g.NT, tma, unsigned(grid), s);
+    else if (dtype == BIGCN_BF16) launch_type<__nv_bfloat16, 1>(p, g.NT, tma, unsigned(grid), s);
+    else launch_type<__half, 2>(p, g.NT, tma, unsigned(grid), s);
+    const GradSumParams sum{p.partial, p.colsum, g.tiles, g.groups, g.parts_full, g.parts_last,
+                            g.mt,      g.NT,     g.nt * g.NT, K, F, gamma, beta, dW, lddw, db};
+    launch_kernel(grad_sum_kernel, dim3(unsigned(g.tiles * ((F + 3) / 4))), dim3(kSumThreads), 0, s,
+                  true, dim3(1, 1, 1), sum);
     return launch_status();
 }

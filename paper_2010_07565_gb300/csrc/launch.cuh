@@ -434,4 +434,7 @@ void launch_xnor_gemm_bucketed(const BucketGemmArgs &args, const DeviceInfo &dev
 // resets the count); ~0u on a CUDA error.
 uint32_t take_mix_timeouts();
 
+// Likewise for the checkpoints' weight gradient (checkpoint_grad.cu).
+uint32_t take_grad_timeouts();
+
 }  // namespace bigcn
