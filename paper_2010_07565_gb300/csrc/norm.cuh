@@ -20,36 +20,49 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Vec {
     T v[V];
 };
 
+// Vectors of a thread that are compiled, by V. J is the least that holds a row, so a thread's
+// vectors before the next smaller option are all within the row, and are taken without tests.
+constexpr int kOptions[4][6] = {{1, 2, 4, 8, 16, 24}, {1, 2, 4, 8, 12, 0}, {1, 2, 4, 8, 0, 0},
+                                {1, 2, 4, 0, 0, 0}};
+__host__ __device__ constexpr int options_of(int V) { return V == 1 ? 0 : V == 2 ? 1 : V == 4 ? 2 : 3; }
+__host__ __device__ constexpr int full_vectors(int V, int J) {
+    int full = 0;
+    for (int q = 0; q < 6; ++q)
+        if (kOptions[options_of(V)][q] > 0 && kOptions[options_of(V)][q] < J)
+            full = kOptions[options_of(V)][q];
+    return full;
+}
+
 // The layout of a call: tpr threads a row, J vectors a thread, V elements a vector;
 // J == 0: rows that no layout holds in registers.
 struct RowLayout {
     int tpr, J;
 };
 
-// The fewest threads that hold a row of K, with at most `warp_most` elements a thread where
-// they are a warp and `most` where they are several; and then more threads while the rows do
-// not fill the card (each has less to do then). The vectors that are compiled follow V.
-inline RowLayout row_layout(int64_t N, int K, int V, int warp_most, int most,
+// The fewest threads, `fewest` or more, that hold a row of K, with at most `warp_most`
+// elements a thread where they are a warp and `most` otherwise; and then more threads while
+// the rows do not fill the card (each has less to do then).
+inline RowLayout row_layout(int64_t N, int K, int V, int fewest, int warp_most, int most,
                             const DeviceInfo &dev) {
-    static const int kOptions[4][6] = {{1, 2, 4, 8, 16, 24}, {1, 2, 4, 8, 12, 0}, {1, 2, 4, 8, 0, 0},
-                                       {1, 2, 4, 0, 0, 0}};
-    const int *options = kOptions[V == 1 ? 0 : V == 2 ? 1 : V == 4 ? 2 : 3];
+    const int *options = kOptions[options_of(V)];
     const int64_t vecs = (int64_t(K) + V - 1) / V;
-    int tpr = 4;
-    while (tpr < 32 && tpr < vecs) tpr *= 2;
     auto fit = [&](int threads) {
         const int64_t need = (vecs + threads - 1) / threads;
         for (int q = 0; q < 6 && options[q] > 0; ++q)
-            if (options[q] >= need && options[q] * V <= (threads == 32 ? warp_most : most))
-                return options[q];
+            if (options[q] >= need)
+                return options[q] * V <= (threads == 32 ? warp_most : most) ? options[q] : 0;
         return 0;
     };
+    int tpr = fewest;
     while (fit(tpr) == 0 && tpr < kMostRowThreads) tpr *= 2;
-    while (tpr >= 32 && tpr < kRowThreads && tpr < vecs &&
-           N * tpr < int64_t(dev.sm_count) * 2 * kRowThreads)
+    while (tpr < kRowThreads && tpr < vecs && N * tpr < int64_t(dev.sm_count) * 2 * kRowThreads)
         tpr *= 2;
     return {tpr, fit(tpr)};
 }
+
+// What stands in for a gamma or a beta that is not given, read with a stride of 0.
+static __device__ __align__(32) const float kOnes[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+static __device__ __align__(32) const float kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
 // Largest V <= 16 bytes of elements by which everything in `addresses` (pointers and byte
 // strides of element size es) is aligned.

@@ -92,16 +92,20 @@ __global__ void __launch_bounds__(kRowThreads) param_any_kernel(const BackwardAr
 }
 
 // Rows in registers; a.chunks blocks, block b takes the sets of rows b, b + chunks, ...
-// kWarp: a row is one warp's. dy and the source stay as they were read and are expanded twice,
-// for the sums and for dx: the registers hold the columns' sums.
+// kWarp: a row is one warp's (tpr = 32, which makes every offset a constant), else tpr
+// threads'.
 template <typename T, int V, int J, bool kKept, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads)
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 2 : 1)
 backward_rows_kernel(const BackwardArgs a, const int row_threads) {
     __shared__ float red[2][2][kMostRowThreads / 32];
     __shared__ float part[kMostRowThreads * V];
+    constexpr int kFull = full_vectors(V, J);
+    // xhat is kept in fp32 between the two uses where that takes no more registers than what
+    // it was read as (a byte and its scale take two), else expanded twice.
+    constexpr bool kHold = V <= 2 || (!kKept && sizeof(T) == 4);
     const int tpr = kWarp ? 32 : row_threads;
     const int t = threadIdx.x & (tpr - 1), rows = blockDim.x / tpr, slot = threadIdx.x / tpr;
-    const int K = a.K, k0 = t * V, step = tpr * V;
+    const int K = a.K, k0 = t * V, step = tpr * V, left = K - k0;
     const float inv_k = 1.0f / float(K);
     using Q = typename QWord<V>::type;
     float sg[J][V], sb[J][V];
@@ -109,45 +113,36 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads) {
     for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int e = 0; e < V; ++e) sg[j][e] = sb[j][e] = 0.0f;
-    const float *gamma = a.gamma + k0;
+    const float *gamma = a.gamma ? a.gamma + k0 : kOnes;
+    const int gstep = a.gamma ? step : 0;
     int turn = 0;
     for (int64_t i0 = int64_t(blockIdx.x) * rows; i0 < a.N; i0 += int64_t(a.chunks) * rows) {
         const int64_t i = i0 + slot;
         const bool live = i < a.N;
+        if (kWarp && !live) break;
         const int64_t at = live ? i : 0;
-        const int left = live ? K - k0 : 0;
         const T *dy = static_cast<const T *>(a.dY) + at * a.lddy + k0;
         const T *x = static_cast<const T *>(a.X) + at * a.ldx + k0;
         const int8_t *q = a.q + at * a.ldq + k0;
         const uint8_t *exps = a.exps + at * a.lde;
-        const float rstd = a.rstd[at], mean = kKept ? 0.0f : a.mean[at];
-        Vec<T, V> g[J];
+        Vec<T, V> w[J];                 // dy as read
         Vec<T, V> xr[kKept ? 1 : J];
         Q qr[kKept ? J : 1];
         uint8_t er[kKept ? J : 1];
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (j * step < left) {
-                g[j] = *reinterpret_cast<const Vec<T, V> *>(dy + j * step);
+            if (j < kFull || j * step < left) {
+                w[j] = *reinterpret_cast<const Vec<T, V> *>(dy + j * step);
                 if constexpr (kKept) {
                     qr[j] = *reinterpret_cast<const Q *>(q + j * step);
-                    er[j] = exps[(k0 + j * step) / kGroup];
+                    er[j] = exps[unsigned(k0 + j * step) / kGroup];
                 } else {
                     xr[j] = *reinterpret_cast<const Vec<T, V> *>(x + j * step);
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) g[j].v[e] = from_f32<T>(0.0f);
-                if constexpr (kKept) {
-                    qr[j] = Q{};
-                    er[j] = 0;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) xr[j].v[e] = from_f32<T>(0.0f);
-                }
             }
         }
-        auto xhat = [&](int j, float (&h)[V]) {
+        const float rstd = a.rstd[at], mean = kKept ? 0.0f : a.mean[at];
+        auto expand = [&](int j, float (&h)[V]) {
             if constexpr (kKept) {
                 dequantise<V>(qr[j], unpack_factor(er[j]), h);
             } else {
@@ -155,49 +150,47 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads) {
                 for (int e = 0; e < V; ++e) h[e] = (to_f32(xr[j].v[e]) - mean) * rstd;
             }
         };
-        auto weights = [&](int j, float (&w)[V]) {
-            if (a.gamma && j * step < left) {
-                const Vec<float, V> v = *reinterpret_cast<const Vec<float, V> *>(gamma + j * step);
-#pragma unroll
-                for (int e = 0; e < V; ++e) w[e] = v.v[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) w[e] = 1.0f;
-            }
-        };
+        float g[J][V];                  // gamma dy
+        float h[kHold ? J : 1][V];
         float s[2] = {0.0f, 0.0f};
+        if (kWarp || live) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (j * step >= K) break;
-            float h[V], w[V];
-            xhat(j, h);
-            weights(j, w);
+            for (int j = 0; j < J; ++j) {
+                if (j < kFull || j * step < left) {
+                    float (&hj)[V] = h[kHold ? j : 0];
+                    expand(j, hj);
+                    const Vec<float, V> m =
+                        *reinterpret_cast<const Vec<float, V> *>(gamma + j * gstep);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float d = to_f32(g[j].v[e]), gd = d * w[e];
-                sg[j][e] = fmaf(d, h[e], sg[j][e]);
-                sb[j][e] += d;
-                s[0] += gd;
-                s[1] = fmaf(gd, h[e], s[1]);
+                    for (int e = 0; e < V; ++e) {
+                        const float d = to_f32(w[j].v[e]);
+                        sg[j][e] = fmaf(d, hj[e], sg[j][e]);
+                        sb[j][e] += d;
+                        g[j][e] = d * m.v[e];
+                        s[0] += g[j][e];
+                        s[1] = fmaf(g[j][e], hj[e], s[1]);
+                    }
+                }
             }
         }
         if (!a.dX) continue;
         // Two sets of sums in turn: a set is written again only after the next one's barrier.
         row_sum<kWarp>(s, tpr, red[turn]);
         turn ^= 1;
+        if (!kWarp && !live) continue;
         const float c0 = s[0] * inv_k, c1 = s[1] * inv_k;
         T *dx = static_cast<T *>(a.dX) + at * a.lddx + k0;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (j * step >= left) break;
-            float h[V], w[V];
-            xhat(j, h);
-            weights(j, w);
-            Vec<T, V> o;
+            if (j < kFull || j * step < left) {
+                float (&hj)[V] = h[kHold ? j : 0];
+                if (!kHold) expand(j, hj);
+                Vec<T, V> o;
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                o.v[e] = from_f32<T>(rstd * (fmaf(to_f32(g[j].v[e]), w[e], -c0) - h[e] * c1));
-            *reinterpret_cast<Vec<T, V> *>(dx + j * step) = o;
+                for (int e = 0; e < V; ++e)
+                    o.v[e] = from_f32<T>(rstd * (g[j][e] - c0 - hj[e] * c1));
+                *reinterpret_cast<Vec<T, V> *>(dx + j * step) = o;
+            }
         }
     }
     allow_dependent_launch();
@@ -258,9 +251,15 @@ template <typename T, int V, int J, bool kKept, bool kWarp>
 void launch_kept(BackwardArgs &a, int tpr, const DeviceInfo &dev, cudaStream_t s) {
     const auto kernel = backward_rows_kernel<T, V, J, kKept, kWarp>;
     const int threads = tpr > kRowThreads ? tpr : kRowThreads, rows = threads / tpr;
-    int per_sm = 1;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess)
-        per_sm = 1;
+    static const auto blocks_per_sm = [](int n) {
+        int per = 1;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(
+                &per, backward_rows_kernel<T, V, J, kKept, kWarp>, n, 0) != cudaSuccess)
+            cudaGetLastError();
+        return per > 1 ? per : 1;
+    };
+    static const int with[2] = {blocks_per_sm(kRowThreads), blocks_per_sm(kMostRowThreads)};
+    const int per_sm = with[threads > kRowThreads];
     const int64_t sets = (a.N + rows - 1) / rows;
     int64_t blocks = int64_t(dev.sm_count) * per_sm;
     if (blocks > kMaxChunks) blocks = kMaxChunks;
@@ -281,7 +280,7 @@ void launch_rows(BackwardArgs &a, int tpr, const DeviceInfo &dev, cudaStream_t s
 
 template <typename T, int V>
 bool launch_width(BackwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
-    const RowLayout r = row_layout(a.N, a.K, V, 24, 16, dev);
+    const RowLayout r = row_layout(a.N, a.K, V, 8, 24, 16, dev);
     if (r.J == 1) launch_rows<T, V, 1>(a, r.tpr, dev, s);
     else if (r.J == 2) launch_rows<T, V, 2>(a, r.tpr, dev, s);
     else if (V <= 4 && r.J == 4) launch_rows<T, V, V <= 4 ? 4 : 1>(a, r.tpr, dev, s);

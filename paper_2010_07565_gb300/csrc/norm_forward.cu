@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
 // Rows in registers. kWarp: a row is one warp's (tpr = 32, which makes every offset a constant),
 // else tpr threads'. Rows past N take part in the sums over threads and store nothing.
 template <typename T, int V, int J, bool kKeep, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads)
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 4 : 2)
 forward_rows_kernel(const ForwardArgs a, const int row_threads) {
     __shared__ float red[2][1][kMostRowThreads / 32];
     const int tpr = kWarp ? 32 : row_threads;
@@ -86,16 +86,18 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads) {
     const int64_t i = int64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
     const bool live = i < a.N;
     if (kWarp && !live) return;
-    // Columns k0 + j step; those of this thread from `left` on are past the row.
-    const int K = a.K, k0 = t * V, step = tpr * V, left = live ? K - k0 : 0;
+    // Columns k0 + j step; those of this thread from `left` on are past the row. The first
+    // kFull vectors are within it.
+    constexpr int kFull = full_vectors(V, J);
+    const int K = a.K, k0 = t * V, step = tpr * V, left = K - k0;
     const float inv_k = 1.0f / float(K);
     // The row as it was read: 16-bit elements take half the registers that way, and are
     // converted where they are used.
     Vec<T, V> x[J];
-    const T *row = static_cast<const T *>(a.X) + (live ? i * a.ldx + k0 : 0);
+    const T *row = static_cast<const T *>(a.X) + (live ? i : 0) * a.ldx + k0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        if (j * step < left) x[j] = *reinterpret_cast<const Vec<T, V> *>(row + j * step);
+        if (j < kFull || j * step < left) x[j] = *reinterpret_cast<const Vec<T, V> *>(row + j * step);
         else
 #pragma unroll
             for (int e = 0; e < V; ++e) x[j].v[e] = from_f32<T>(0.0f);
@@ -110,27 +112,29 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads) {
     s[0] = 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-        if (j * step < left)
+        if (j < kFull || j * step < left)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = to_f32(x[j].v[e]) - mean;
                 s[0] = fmaf(d, d, s[0]);
             }
     row_sum<kWarp>(s, tpr, red[1]);
+    if (!kWarp && !kKeep && !live) return;      // (with a checkpoint lanes still meet below)
     const float rstd = 1.0f / sqrtf(s[0] * inv_k + a.eps);
     if (live && t == 0) {
         if (a.mean) a.mean[i] = mean;
         if (a.rstd) a.rstd[i] = rstd;
     }
-    T *out = static_cast<T *>(a.Y) + (live ? i * a.ldy + k0 : 0);
+    T *out = static_cast<T *>(a.Y) + i * a.ldy + k0;
     using Q = typename QWord<V>::type;
-    int8_t *qrow = kKeep && live ? a.q + i * a.ldq : nullptr;
-    uint8_t *erow = kKeep && live ? a.exps + i * a.lde : nullptr;
-    const float *gamma = a.gamma + k0, *beta = a.beta + k0;
+    int8_t *qrow = a.q + i * a.ldq;
+    uint8_t *erow = a.exps + i * a.lde;
+    const float *gamma = a.gamma ? a.gamma + k0 : kOnes, *beta = a.beta ? a.beta + k0 : kZeros;
+    const int gstep = a.gamma ? step : 0, bstep = a.beta ? step : 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        if (j * step >= K) break;           // the same for the whole row's threads
-        const bool in = j * step < left;
+        if (j >= kFull && j * step >= K) break;     // the same for the whole row's threads
+        const bool in = (kWarp || live) && (j < kFull || j * step < left);
         uint32_t top = 0;
         float v[V];
 #pragma unroll
@@ -138,17 +142,10 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads) {
             v[e] = (to_f32(x[j].v[e]) - mean) * rstd;
             if (kKeep) top = max(top, abs_bits(v[e]));
         }
-        if (kKeep) top = in ? top : 0u;
+        if (kKeep && j >= kFull) top = in ? top : 0u;
         if (in) {
-            Vec<float, V> g, b;
-            if (a.gamma) g = *reinterpret_cast<const Vec<float, V> *>(gamma + j * step);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e) g.v[e] = 1.0f;
-            if (a.beta) b = *reinterpret_cast<const Vec<float, V> *>(beta + j * step);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e) b.v[e] = 0.0f;
+            const Vec<float, V> g = *reinterpret_cast<const Vec<float, V> *>(gamma + j * gstep);
+            const Vec<float, V> b = *reinterpret_cast<const Vec<float, V> *>(beta + j * bstep);
             Vec<T, V> w;
 #pragma unroll
             for (int e = 0; e < V; ++e) w.v[e] = from_f32<T>(fmaf(v[e], g.v[e], b.v[e]));
@@ -158,8 +155,9 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads) {
             const uint32_t b = group_byte<V, kWarp>(top, tpr);
             if (in) {
                 *reinterpret_cast<Q *>(qrow + k0 + j * step) = quantise<V>(v, pack_factor(b));
-                if (k0 % kGroup == 0 || !kWarp)
-                    if ((k0 + j * step) % kGroup == 0) erow[(k0 + j * step) / kGroup] = uint8_t(b);
+                // A warp's step is a whole number of groups.
+                if (kWarp ? (k0 & (kGroup - 1)) == 0 : ((k0 + j * step) & (kGroup - 1)) == 0)
+                    erow[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
             }
         }
     }
@@ -182,12 +180,12 @@ void launch_kind(const ForwardArgs &a, int tpr, cudaStream_t s) {
 template <typename T, int V, int J>
 void launch_rows(const ForwardArgs &a, int tpr, cudaStream_t s) {
     if (tpr == 32) launch_kind<T, V, J, true>(a, tpr, s);
-    else if constexpr (V * J <= 16) launch_kind<T, V, J, false>(a, tpr, s);
+    else if constexpr (V * J <= 16 || V == 8) launch_kind<T, V, J, false>(a, tpr, s);
 }
 
 template <typename T, int V>
 bool launch_width(const ForwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
-    const RowLayout r = row_layout(a.N, a.K, V, 32, 16, dev);
+    const RowLayout r = row_layout(a.N, a.K, V, a.q ? 32 / V : 8, 32, V == 8 ? 32 : 16, dev);
     if (r.J == 1) launch_rows<T, V, 1>(a, r.tpr, s);
     else if (r.J == 2) launch_rows<T, V, 2>(a, r.tpr, s);
     else if (r.J == 4) launch_rows<T, V, 4>(a, r.tpr, s);
