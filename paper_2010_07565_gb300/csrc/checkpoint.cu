@@ -6,141 +6,27 @@ namespace {
 
 constexpr int kCkThreads = 256;
 
-// Both directions lay a row over `tpr` threads (a power of two, 4 to 256) in vectors of V
-// elements, as layer norm does (norm.cuh): a group of 32 columns lies in 32 / V
-// neighbouring lanes (or in the row's, where it is shorter). A thread takes four vectors, J of a
-// row by R rows, all loaded before the first is used; a row longer than tpr J V columns
-// goes over several blocks. Bound by memory.
+// Both directions lay a row over `tpr` threads (a power of two, 8 to 256) in pieces of 16
+// bytes of X, as layer norm does (norm.cuh). A thread takes four pieces, J of a row by R rows,
+// all loaded before the first is used; a row longer than tpr J pieces goes over several blocks.
+// Bound by memory.
 template <int V, int J, int R>
 struct Place {
     int64_t i[R];            // rows
-    int k0;                  // column of vector 0
-    int step;                // columns from one vector to the next
-    __device__ __forceinline__ Place(int tpr, unsigned pieces) {
+    int k0;                  // column of piece 0
+    int step;                // columns from one piece to the next
+    __device__ __forceinline__ Place(int tpr, unsigned parts) {
         const int t = threadIdx.x & (tpr - 1), rows = kCkThreads / tpr;
-        const int64_t set = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+        const unsigned set = blockIdx.x / parts, part = blockIdx.x % parts;
 #pragma unroll
-        for (int r = 0; r < R; ++r) i[r] = (set * R + r) * rows + threadIdx.x / tpr;
+        for (int r = 0; r < R; ++r) i[r] = (int64_t(set) * R + r) * rows + threadIdx.x / tpr;
         step = tpr * V;
-        k0 = int(piece) * step * J + t * V;
+        k0 = int(part) * step * J + t * V;
     }
 };
 
-template <typename T, int V, int J, int R, bool kWhole>
-__global__ void __launch_bounds__(kCkThreads)
-pack_kernel(const T *__restrict__ X, int64_t N, int K, int64_t ldx, int8_t *__restrict__ q,
-            int64_t ldq, uint8_t *__restrict__ exps, int64_t lde, int tpr, unsigned pieces) {
-    const Place<V, J, R> at(tpr, pieces);
-    Vec<T, V> x[R][J];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = at.k0 + j * at.step;
-            if (at.i[r] < N && k < K)
-                x[r][j] = *reinterpret_cast<const Vec<T, V> *>(X + at.i[r] * ldx + k);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e) x[r][j].v[e] = from_f32<T>(0.0f);
-        }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = at.k0 + j * at.step;
-            const bool in = at.i[r] < N && k < K;
-            uint32_t top = 0;
-            float v[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                v[e] = to_f32(x[r][j].v[e]);
-                top = max(top, abs_bits(v[e]));
-            }
-            const uint32_t b = group_byte<V, kWhole>(in ? top : 0u, tpr);
-            if (in) {
-                *reinterpret_cast<typename QWord<V>::type *>(q + at.i[r] * ldq + k) =
-                    quantise<V>(v, pack_factor(b));
-                if (k % kGroup == 0) exps[at.i[r] * lde + k / kGroup] = uint8_t(b);
-            }
-        }
-    // The padding of the rows that end in this block's columns.
-    const int t = threadIdx.x & (tpr - 1), groups = int(checkpoint_groups(K));
-    if (int64_t(blockIdx.x % pieces) + 1 == pieces)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (at.i[r] < N) {
-                for (int k = K + t; k < (K + 15) / 16 * 16; k += tpr) q[at.i[r] * ldq + k] = 0;
-                for (int g = groups + t; g < (groups + 3) / 4 * 4; g += tpr)
-                    exps[at.i[r] * lde + g] = 0;
-            }
-}
-
-template <typename T, int V, int J, int R>
-__global__ void __launch_bounds__(kCkThreads)
-unpack_kernel(const int8_t *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ exps,
-              int64_t lde, int64_t N, int K, const float *__restrict__ gamma,
-              const float *__restrict__ beta, T *__restrict__ X, int64_t ldx, int tpr,
-              unsigned pieces) {
-    const Place<V, J, R> at(tpr, pieces);
-    using Q = typename QWord<V>::type;
-    Q w[R][J];
-    uint8_t b[R][J];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = at.k0 + j * at.step;
-            if (at.i[r] < N && k < K) {
-                w[r][j] = *reinterpret_cast<const Q *>(q + at.i[r] * ldq + k);
-                b[r][j] = exps[at.i[r] * lde + k / kGroup];
-            }
-        }
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int k = at.k0 + j * at.step;
-        if (k >= K) continue;
-        Vec<float, V> g, c;
-        if (gamma) g = *reinterpret_cast<const Vec<float, V> *>(gamma + k);
-        if (beta) c = *reinterpret_cast<const Vec<float, V> *>(beta + k);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (at.i[r] >= N) continue;
-            Vec<T, V> x;
-            float v[V];
-            dequantise<V>(w[r][j], unpack_factor(b[r][j]), v);
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                x.v[e] = from_f32<T>(gamma || beta
-                                         ? fmaf(gamma ? g.v[e] : 1.0f, v[e], beta ? c.v[e] : 0.0f)
-                                         : v[e]);
-            *reinterpret_cast<Vec<T, V> *>(X + at.i[r] * ldx + k) = x;
-        }
-    }
-}
-
-// Threads of a row and the call's grid: the fewest threads (a warp, or fewer for short rows)
-// that hold a row in at most four vectors, else all 256 and several blocks.
-struct CkGrid {
-    int tpr, J;
-    unsigned pieces, blocks;
-};
-inline CkGrid ck_grid(int64_t N, int K, int V) {
-    const int64_t vecs = (int64_t(K) + V - 1) / V;
-    CkGrid g;
-    g.tpr = 4;
-    while (g.tpr < 32 && g.tpr < vecs) g.tpr *= 2;
-    while (g.tpr < kCkThreads && int64_t(g.tpr) * 4 < vecs) g.tpr *= 2;
-    g.J = vecs <= g.tpr ? 1 : vecs <= 2 * g.tpr ? 2 : 4;
-    const int64_t pieces = (vecs + int64_t(g.tpr) * g.J - 1) / (int64_t(g.tpr) * g.J);
-    const int64_t rows = kCkThreads / g.tpr * (4 / g.J);
-    g.pieces = unsigned(pieces);
-    g.blocks = unsigned((N + rows - 1) / rows * pieces);
-    return g;
-}
-
-template <typename T>
-struct PackArgs {
-    T *X;                    // read by the packing, written by the unpacking
+struct CkArgs {
+    void *X;                 // read by the packing, written by the unpacking
     int64_t N;
     int K;
     int64_t ldx;
@@ -150,53 +36,131 @@ struct PackArgs {
     int64_t lde;
     const float *gamma;
     const float *beta;
+    bool aligned;            // gamma and beta to 16 bytes
 };
 
-template <typename T, int V, int J>
-void launch_vectors(const PackArgs<T> &a, bool pack, const CkGrid &g, cudaStream_t s) {
-    if (pack && g.tpr >= 32)
-        pack_kernel<T, V, J, 4 / J, true><<<g.blocks, kCkThreads, 0, s>>>(
-            a.X, a.N, a.K, a.ldx, a.q, a.ldq, a.exps, a.lde, g.tpr, g.pieces);
-    else if (pack)
-        pack_kernel<T, V, J, 4 / J, false><<<g.blocks, kCkThreads, 0, s>>>(
-            a.X, a.N, a.K, a.ldx, a.q, a.ldq, a.exps, a.lde, g.tpr, g.pieces);
-    else
-        unpack_kernel<T, V, J, 4 / J><<<g.blocks, kCkThreads, 0, s>>>(
-            a.q, a.ldq, a.exps, a.lde, a.N, a.K, a.gamma, a.beta, a.X, a.ldx, g.tpr, g.pieces);
+template <typename T, int A, int J, int R>
+__global__ void __launch_bounds__(kCkThreads)
+pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
+    constexpr int V = kPiece<T>, H = V / 2;
+    const Place<V, J, R> at(tpr, parts);
+    const int K = a.K, left = K - at.k0;
+    uint4 w[R][J];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            w[r][j] = make_uint4(0u, 0u, 0u, 0u);
+            if (at.i[r] < a.N && left > j * at.step)
+                w[r][j] = load_piece<T, A>(static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0 +
+                                               j * at.step,
+                                           left - j * at.step);
+        }
+    // Past K a piece is zeros and so is its q.
+    const int kq = (K + 15) / 16 * 16 - at.k0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float2 x[J][H];
+        uint32_t own[J], top[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            unpack16<T>(w[r][j], x[j]);
+            own[j] = top_bits(x[j]);
+        }
+        group_tops<32 / V>(own, top);
+        if (at.i[r] >= a.N) continue;
+        int8_t *q = a.q + at.i[r] * a.ldq + at.k0;
+        uint8_t *exps = a.exps + at.i[r] * a.lde;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (j * at.step >= kq) break;
+            const uint32_t b = scale_byte(top[j]);
+            *reinterpret_cast<QPiece<H> *>(q + j * at.step) = quantise_piece(x[j], pack_factor(b));
+            if ((threadIdx.x & (32 / V - 1)) == 0 && j * at.step < left)
+                exps[unsigned(at.k0 + j * at.step) / kGroup] = uint8_t(b);
+        }
+        const int groups = int(checkpoint_groups(K)), t = threadIdx.x & (tpr - 1);
+        if (blockIdx.x % parts + 1 == parts && groups + t < (groups + 3) / 4 * 4) exps[groups + t] = 0;
+    }
 }
 
-template <typename T, int V>
-void launch_width(const PackArgs<T> &a, bool pack, cudaStream_t s) {
-    const CkGrid g = ck_grid(a.N, a.K, V);
-    if (g.J == 1) launch_vectors<T, V, 1>(a, pack, g, s);
-    else if (g.J == 2) launch_vectors<T, V, 2>(a, pack, g, s);
-    else launch_vectors<T, V, 4>(a, pack, g, s);
+template <typename T, int A, int J, int R>
+__global__ void __launch_bounds__(kCkThreads)
+unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
+    constexpr int V = kPiece<T>, H = V / 2;
+    const Place<V, J, R> at(tpr, parts);
+    const int left = a.K - at.k0;
+    QPiece<H> w[R][J];
+    uint8_t b[R][J];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (at.i[r] < a.N && left > j * at.step) {
+                const int k = at.k0 + j * at.step;
+                w[r][j] = *reinterpret_cast<const QPiece<H> *>(a.q + at.i[r] * a.ldq + k);
+                b[r][j] = a.exps[at.i[r] * a.lde + unsigned(k) / kGroup];
+            }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int n = left - j * at.step;
+        if (n <= 0) break;
+        const int k = at.k0 + j * at.step;
+        float2 g[H], c[H];
+        if (a.gamma) load_params(a.gamma + k, a.aligned, n, g);
+        if (a.beta) load_params(a.beta + k, a.aligned, n, c);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (at.i[r] >= a.N) continue;
+            float2 v[H];
+            dequantise_piece<H>(w[r][j], unpack_factor(b[r][j]), v);
+            if (a.gamma || a.beta)
+#pragma unroll
+                for (int e = 0; e < H; ++e)
+                    v[e] = __ffma2_rn(v[e], a.gamma ? g[e] : both(1.0f), a.beta ? c[e] : both(0.0f));
+            store_piece<T, A>(static_cast<T *>(a.X) + at.i[r] * a.ldx + k, pack16<T>(v), n);
+        }
+    }
+}
+
+// Threads of a row and the call's grid: the fewest threads (8, or more) that hold a row in at
+// most four pieces, else all 256 and several blocks.
+template <typename T, int A>
+void launch_checkpoint_rows(const CkArgs &a, bool pack, cudaStream_t s) {
+    const int64_t pieces = (int64_t(a.K) + kPiece<T> - 1) / kPiece<T>;
+    int tpr = 8;
+    while (tpr < kCkThreads && int64_t(tpr) * 4 < pieces) tpr *= 2;
+    const int J = pieces <= tpr ? 1 : pieces <= 2 * tpr ? 2 : 4;
+    const unsigned parts = unsigned((pieces + int64_t(tpr) * J - 1) / (int64_t(tpr) * J));
+    const int64_t rows = kCkThreads / tpr * (4 / J);
+    const unsigned blocks = unsigned((a.N + rows - 1) / rows * parts);
+    if (J == 1 && pack) pack_kernel<T, A, 1, 4><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else if (J == 2 && pack) pack_kernel<T, A, 2, 2><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else if (pack) pack_kernel<T, A, 4, 1><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else if (J == 1) unpack_kernel<T, A, 1, 4><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else if (J == 2) unpack_kernel<T, A, 2, 2><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else unpack_kernel<T, A, 4, 1><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
 }
 
 template <typename T>
-void launch_type(const PackArgs<T> &a, bool pack, cudaStream_t s) {
-    const uint64_t es = sizeof(T), f = 4 / es;
-    const uint64_t where[] = {uint64_t(uintptr_t(a.X)), uint64_t(a.ldx) * es, uint64_t(a.K) * es,
-                              uint64_t(uintptr_t(a.gamma)) / f, uint64_t(uintptr_t(a.beta)) / f};
-    const int V = vector_width(es, where, 5);
-    if (V == 1) launch_width<T, 1>(a, pack, s);
-    else if (V == 2) launch_width<T, 2>(a, pack, s);
-    else if (V == 4) launch_width<T, 4>(a, pack, s);
-    else launch_width<T, es == 2 ? 8 : 4>(a, pack, s);
+void launch_type(const CkArgs &a, bool pack, cudaStream_t s) {
+    const uint64_t es = sizeof(T);
+    const uint64_t where[] = {uint64_t(uintptr_t(a.X)), uint64_t(a.ldx) * es};
+    const int A = alignment_of(where, 2);
+    if (A == 16) launch_checkpoint_rows<T, 16>(a, pack, s);
+    else if (A == 8) launch_checkpoint_rows<T, 8>(a, pack, s);
+    else if (A == 4) launch_checkpoint_rows<T, 4>(a, pack, s);
+    else launch_checkpoint_rows<T, es == 2 ? 2 : 4>(a, pack, s);
 }
 
 void launch_checkpoint(int32_t dtype, void *X, int64_t N, int K, int64_t ldx, int8_t *q,
                        int64_t ldq, uint8_t *exps, int64_t lde, const float *gamma,
                        const float *beta, bool pack, cudaStream_t s) {
-    if (dtype == BIGCN_F32)
-        launch_type(PackArgs<float>{static_cast<float *>(X), N, K, ldx, q, ldq, exps, lde, gamma,
-                                    beta}, pack, s);
-    else if (dtype == BIGCN_BF16)
-        launch_type(PackArgs<__nv_bfloat16>{static_cast<__nv_bfloat16 *>(X), N, K, ldx, q, ldq, exps,
-                                            lde, gamma, beta}, pack, s);
-    else
-        launch_type(PackArgs<__half>{static_cast<__half *>(X), N, K, ldx, q, ldq, exps, lde, gamma,
-                                     beta}, pack, s);
+    const CkArgs a{X,    N,   K,     ldx,  q, ldq, exps, lde, gamma, beta,
+                   aligned_to(gamma, 16) && aligned_to(beta, 16)};
+    if (dtype == BIGCN_F32) launch_type<float>(a, pack, s);
+    else if (dtype == BIGCN_BF16) launch_type<__nv_bfloat16>(a, pack, s);
+    else launch_type<__half>(a, pack, s);
 }
 
 }  // namespace

@@ -46,55 +46,12 @@ __device__ __forceinline__ float unpack_factor(uint32_t b) {
     return __uint_as_float(b == kNanByte ? 0x7FC00000u : b << 23);
 }
 
-// V bytes of q as one word or two.
-template <int V> struct QWord {
-    using type = uint8_t;
-};
-template <> struct QWord<2> {
-    using type = uint16_t;
-};
-template <> struct QWord<4> {
-    using type = uint32_t;
-};
-template <> struct QWord<8> {
-    using type = uint2;
-};
-
-// V values times a group's factor to int8, rounded to nearest even. v f + 1.5 2^23, rounded
-// once, has the two's complement of the nearest integer in its low bits (v f is exact, the
-// factor a power of two): one multiply-add instead of a conversion, which has a sixteenth of
+// v times a group's factor to int8, rounded to nearest even, in the low byte: v f + 1.5 2^23,
+// rounded once, has the two's complement of the nearest integer in its low bits (v f is exact,
+// the factor a power of two). One multiply-add instead of a conversion, which has an eighth of
 // its rate.
 __device__ __forceinline__ uint32_t q_low(float v, float f) {
     return __float_as_uint(fmaf(v, f, 12582912.0f));
-}
-__device__ __forceinline__ uint32_t q_four(const float *v, float f) {
-    return __byte_perm(__byte_perm(q_low(v[0], f), q_low(v[1], f), 0x0040),
-                       __byte_perm(q_low(v[2], f), q_low(v[3], f), 0x0040), 0x5410);
-}
-template <int V>
-__device__ __forceinline__ typename QWord<V>::type quantise(const float (&v)[V], float f) {
-    if constexpr (V == 1) return uint8_t(q_low(v[0], f));
-    else if constexpr (V == 2)
-        return uint16_t(__byte_perm(q_low(v[0], f), q_low(v[1], f), 0x0040));
-    else if constexpr (V == 4) return q_four(v, f);
-    else return make_uint2(q_four(v, f), q_four(v + 4, f));
-}
-
-// And back: q + 128 in the low byte of 2^23, less 2^23 + 128, times the factor.
-__device__ __forceinline__ float q_value(uint32_t flipped, int byte) {
-    return __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7440u + uint32_t(byte))) - 8388736.0f;
-}
-template <int V>
-__device__ __forceinline__ void dequantise(typename QWord<V>::type w, float f, float (&v)[V]) {
-    if constexpr (V == 8) {
-        const uint32_t u[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = q_value(u[e >> 2], e & 3) * f;
-    } else {
-        const uint32_t u = uint32_t(w) ^ 0x80808080u;
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = q_value(u, e) * f;
-    }
 }
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }

@@ -1,12 +1,18 @@
-// What the row-wise kernels of layer norm share: how a row is laid over threads, vectors of
-// elements, sums over a row's threads.
+// What the row-wise kernels of layer norm and the checkpoints share: how a row is laid over
+// threads, 16 bytes of columns at a time, packed arithmetic, sums over a row's threads.
 //
-// A row lies in the registers of `tpr` threads (a power of two), J vectors of V elements each:
-// vector j of thread t holds columns (j tpr + t) V .. + V - 1, so that a warp's loads are
-// contiguous and a group of 32 columns lies in 32 / V neighbouring lanes. V follows from the
-// alignment of everything that is read or written in such vectors (16 bytes where it can). A
-// row is read once.
+// A row lies in the registers of `tpr` threads (a power of two), J pieces of V elements each
+// (16 bytes: 4 fp32 or 8 16-bit columns): piece j of thread t holds columns (j tpr + t) V ..
+// + V - 1, whatever the rows' alignment, so that a group of 32 columns lies in 32 / V lanes. Rows
+// that are aligned to A < 16 bytes only are read and written in 16 / A accesses a piece, which
+// share their sectors in L1.
+//
+// These kernels are bound by memory only if they issue few instructions (16 an element and
+// SM cycle at 5 bytes an element fill all issue slots): elements go through packed fp32
+// arithmetic in pairs, and maxima of two groups share a word.
 #pragma once
+
+#include <type_traits>
 
 #include "checkpoint.cuh"
 #include "launch.cuh"
@@ -16,66 +22,251 @@ namespace bigcn {
 constexpr int kRowThreads = 256;        // threads of a block, or of a row where that is more
 constexpr int kMostRowThreads = 512;
 
-template <typename T, int V> struct alignas(sizeof(T) * V) Vec {
-    T v[V];
-};
+template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 
-// Vectors of a thread that are compiled, by V. J is the least that holds a row, so a thread's
-// vectors before the next smaller option are all within the row, and are taken without tests.
-constexpr int kOptions[4][6] = {{1, 2, 4, 8, 16, 24}, {1, 2, 4, 8, 12, 0}, {1, 2, 4, 8, 0, 0},
-                                {1, 2, 4, 0, 0, 0}};
-__host__ __device__ constexpr int options_of(int V) { return V == 1 ? 0 : V == 2 ? 1 : V == 4 ? 2 : 3; }
-__host__ __device__ constexpr int full_vectors(int V, int J) {
+// ---- 16 bytes of a row --------------------------------------------------------------------
+template <int A> __device__ __forceinline__ uint4 load16(const void *p) {
+    if constexpr (A == 16) {
+        return *static_cast<const uint4 *>(p);
+    } else if constexpr (A == 8) {
+        const uint2 *q = static_cast<const uint2 *>(p);
+        const uint2 a = q[0], b = q[1];
+        return make_uint4(a.x, a.y, b.x, b.y);
+    } else if constexpr (A == 4) {
+        const uint32_t *q = static_cast<const uint32_t *>(p);
+        return make_uint4(q[0], q[1], q[2], q[3]);
+    } else {
+        const uint16_t *q = static_cast<const uint16_t *>(p);
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = uint32_t(q[2 * e]) | (uint32_t(q[2 * e + 1]) << 16);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <int A> __device__ __forceinline__ void store16(void *p, uint4 v) {
+    if constexpr (A == 16) {
+        *static_cast<uint4 *>(p) = v;
+    } else if constexpr (A == 8) {
+        static_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
+        static_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (A == 4) {
+                static_cast<uint32_t *>(p)[e] = w[e];
+            } else {
+                static_cast<uint16_t *>(p)[2 * e] = uint16_t(w[e]);
+                static_cast<uint16_t *>(p)[2 * e + 1] = uint16_t(w[e] >> 16);
+            }
+        }
+    }
+}
+
+// The first n < V elements of a piece (zeros behind them), and their store.
+template <typename T> __device__ __forceinline__ uint4 load_some(const T *p, int n) {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < kPiece<T>; ++e)
+        if (e < n) {
+            if constexpr (sizeof(T) == 4) w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+            else
+                w[e / 2] |= uint32_t(reinterpret_cast<const uint16_t *>(p)[e]) << (16 * (e % 2));
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T> __device__ __forceinline__ void store_some(T *p, uint4 v, int n) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < kPiece<T>; ++e)
+        if (e < n) {
+            if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(p)[e] = w[e];
+            else reinterpret_cast<uint16_t *>(p)[e] = uint16_t(w[e / 2] >> (16 * (e % 2)));
+        }
+}
+template <typename T, int A> __device__ __forceinline__ uint4 load_piece(const T *p, int n) {
+    return n >= kPiece<T> ? load16<A>(p) : load_some(p, n);
+}
+template <typename T, int A> __device__ __forceinline__ void store_piece(T *p, uint4 v, int n) {
+    if (n >= kPiece<T>) store16<A>(p, v);
+    else store_some(p, v, n);
+}
+
+// ---- pairs of fp32 ------------------------------------------------------------------------
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+template <typename T>
+__device__ __forceinline__ void unpack16(uint4 w, float2 (&v)[kPiece<T> / 2]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            v[e] = make_float2(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (std::is_same<T, __half>::value)
+                v[e] = __half22float2(*reinterpret_cast<const __half2 *>(&u[e]));
+            else v[e] = make_float2(__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xFFFF0000u));
+        }
+    }
+}
+// Rounded to T once, to nearest even.
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float2 (&v)[kPiece<T> / 2]) {
+    uint32_t u[4];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            u[2 * e] = __float_as_uint(v[e].x);
+            u[2 * e + 1] = __float_as_uint(v[e].y);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __floats2half2_rn(v[e].x, v[e].y);
+                u[e] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[e].x, v[e].y);
+                u[e] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// Zeros in the elements of a piece from n on.
+template <int H> __device__ __forceinline__ void clear_from(float2 (&v)[H], int n) {
+#pragma unroll
+    for (int e = 0; e < H; ++e) {
+        v[e].x = 2 * e < n ? v[e].x : 0.0f;
+        v[e].y = 2 * e + 1 < n ? v[e].y : 0.0f;
+    }
+}
+
+// V entries of gamma or beta at p, of which n lie in the row; `aligned`: p to 16 bytes.
+template <int H>
+__device__ __forceinline__ void load_params(const float *p, bool aligned, int n, float2 (&v)[H]) {
+    if (aligned && n >= 2 * H) {
+#pragma unroll
+        for (int w = 0; w < H / 2; ++w) {
+            const float4 f = __ldg(reinterpret_cast<const float4 *>(p) + w);
+            v[2 * w] = make_float2(f.x, f.y);
+            v[2 * w + 1] = make_float2(f.z, f.w);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+            v[e].x = 2 * e < n ? __ldg(p + 2 * e) : 0.0f;
+            v[e].y = 2 * e + 1 < n ? __ldg(p + 2 * e + 1) : 0.0f;
+        }
+    }
+}
+
+// What stands in for a gamma or a beta that is not given, read with a stride of 0.
+static __device__ __align__(16) const float kOnes[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+static __device__ __align__(16) const float kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+
+// The largest magnitude of a piece as bits (a NaN is larger than an infinity).
+template <int H> __device__ __forceinline__ uint32_t top_bits(const float2 (&v)[H]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < H; ++e)
+        asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(v[e].x), "f"(v[e].y));
+    return __float_as_uint(m);
+}
+
+// Largest magnitudes of the groups of 32 columns that this lane's pieces belong to (kLanes
+// neighbouring lanes each), two to a word: a scale byte needs the upper 16 bits only.
+template <int kLanes, int J>
+__device__ __forceinline__ void group_tops(const uint32_t (&own)[J], uint32_t (&top)[J]) {
+#pragma unroll
+    for (int j = 0; j < J; j += 2) {
+        uint32_t w = __byte_perm(own[j], j + 1 < J ? own[j + 1 < J ? j + 1 : j] : 0u, 0x7632);
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1)
+            w = __vmaxu2(w, __shfl_xor_sync(kFullMask, w, o));
+        top[j] = w << 16;
+        if (j + 1 < J) top[j + 1 < J ? j + 1 : j] = w & 0xFFFF0000u;
+    }
+}
+
+// A piece to int8 and back (checkpoint.cuh has the rounding): V bytes as one word or two.
+template <int H> using QPiece = typename std::conditional<H == 4, uint2, uint32_t>::type;
+__device__ __forceinline__ uint32_t quantise4(float2 a, float2 b, float f) {
+    const float2 x = __ffma2_rn(a, both(f), both(12582912.0f)), y = __ffma2_rn(b, both(f), both(12582912.0f));
+    return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
+                       __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
+}
+template <int H> __device__ __forceinline__ QPiece<H> quantise_piece(const float2 (&v)[H], float f) {
+    if constexpr (H == 2) return quantise4(v[0], v[1], f);
+    else return make_uint2(quantise4(v[0], v[1], f), quantise4(v[2], v[3], f));
+}
+__device__ __forceinline__ void dequantise4(uint32_t w, float f, float2 &a, float2 &b) {
+    const uint32_t u = w ^ 0x80808080u;
+    float m[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        m[e] = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440u + uint32_t(e)));
+    a = __fmul2_rn(__fadd2_rn(make_float2(m[0], m[1]), both(-8388736.0f)), both(f));
+    b = __fmul2_rn(__fadd2_rn(make_float2(m[2], m[3]), both(-8388736.0f)), both(f));
+}
+template <int H> __device__ __forceinline__ void dequantise_piece(QPiece<H> w, float f, float2 (&v)[H]) {
+    if constexpr (H == 2) {
+        dequantise4(w, f, v[0], v[1]);
+    } else {
+        dequantise4(w.x, f, v[0], v[1]);
+        dequantise4(w.y, f, v[2], v[3]);
+    }
+}
+
+// ---- layouts ------------------------------------------------------------------------------
+// Pieces of a thread that are compiled, by V. The least that holds a row is taken, so a
+// thread's pieces before the next smaller option are all within the row.
+constexpr int kOptions[2][7] = {{1, 2, 3, 4, 5, 6, 8}, {1, 2, 3, 4, 0, 0, 0}};
+__host__ __device__ constexpr int full_pieces(int V, int J) {
     int full = 0;
-    for (int q = 0; q < 6; ++q)
-        if (kOptions[options_of(V)][q] > 0 && kOptions[options_of(V)][q] < J)
-            full = kOptions[options_of(V)][q];
+    for (int q = 0; q < 7; ++q)
+        if (kOptions[V == 8][q] > 0 && kOptions[V == 8][q] < J) full = kOptions[V == 8][q];
     return full;
 }
 
-// The layout of a call: tpr threads a row, J vectors a thread, V elements a vector;
-// J == 0: rows that no layout holds in registers.
+// tpr threads a row, J pieces a thread; J == 0: rows that no layout holds in registers.
 struct RowLayout {
     int tpr, J;
 };
 
-// The fewest threads, `fewest` or more, that hold a row of K, with at most `warp_most`
-// elements a thread where they are a warp and `most` otherwise; and then more threads while
-// the rows do not fill the card (each has less to do then).
-inline RowLayout row_layout(int64_t N, int K, int V, int fewest, int warp_most, int most,
-                            const DeviceInfo &dev) {
-    const int *options = kOptions[options_of(V)];
-    const int64_t vecs = (int64_t(K) + V - 1) / V;
+// The fewest threads (8 or more, so that a group of 32 columns lies in one row's lanes) that hold a row of K, with at most `most` elements each,
+// `warp_most` where they are a warp; and then more threads while the rows do not fill the card
+// (each has less to do then).
+inline RowLayout row_layout(int64_t N, int K, int V, int most, int warp_most, const DeviceInfo &dev) {
+    const int *options = kOptions[V == 8];
+    const int64_t pieces = (int64_t(K) + V - 1) / V;
     auto fit = [&](int threads) {
-        const int64_t need = (vecs + threads - 1) / threads;
-        for (int q = 0; q < 6 && options[q] > 0; ++q)
+        const int64_t need = (pieces + threads - 1) / threads;
+        for (int q = 0; q < 7 && options[q] > 0; ++q)
             if (options[q] >= need)
                 return options[q] * V <= (threads == 32 ? warp_most : most) ? options[q] : 0;
         return 0;
     };
-    int tpr = fewest;
+    int tpr = 8;
     while (fit(tpr) == 0 && tpr < kMostRowThreads) tpr *= 2;
-    while (tpr < kRowThreads && tpr < vecs && N * tpr < int64_t(dev.sm_count) * 2 * kRowThreads)
+    while (tpr < kRowThreads && tpr < pieces && N * tpr < int64_t(dev.sm_count) * 2 * kRowThreads)
         tpr *= 2;
     return {tpr, fit(tpr)};
 }
 
-// What stands in for a gamma or a beta that is not given, read with a stride of 0.
-static __device__ __align__(32) const float kOnes[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-static __device__ __align__(32) const float kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-
-// Largest V <= 16 bytes of elements by which everything in `addresses` (pointers and byte
-// strides of element size es) is aligned.
-inline int vector_width(size_t es, const uint64_t *addresses, int n) {
+// The alignment in bytes, at most 16, of everything in `addresses` (pointers and byte strides).
+inline int alignment_of(const uint64_t *addresses, int n) {
     uint64_t all = 16;
     for (int q = 0; q < n; ++q) all |= addresses[q];
-    const uint64_t bytes = all & (~all + 1);        // the lowest set bit, at most 16
-    return bytes <= es ? 1 : int(bytes / es);
+    return int(all & (~all + 1));
 }
 
-// Sums over a row's threads, the same value for all of them. kWarp: the row is one warp;
-// else `red` holds a float per warp and sum (unused where a row is within a warp), and every
-// thread of the block calls it.
+// ---- sums over a row's threads ------------------------------------------------------------
+// The same value for all of them. kWarp: the row is one warp; else `red` holds a float per warp
+// and sum (unused where a row is within a warp), and every thread of the block calls it.
 template <bool kWarp, int kN>
 __device__ __forceinline__ void row_sum(float (&v)[kN], int tpr, float (*red)[kMostRowThreads / 32]) {
     if constexpr (kWarp) {
@@ -118,23 +309,6 @@ __device__ __forceinline__ void block_sum(float (&v)[kN]) {
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) v[n] += part[n][w];
     }
-}
-
-// The scale byte of the group of 32 columns that this lane's vector belongs to, from the
-// vector's own largest magnitude. kWhole: a group lies in 32 / V lanes; else in the tpr lanes of
-// a shorter row.
-template <int V, bool kWhole>
-__device__ __forceinline__ uint32_t group_byte(uint32_t own, int tpr) {
-    if constexpr (kWhole && V == 1) {
-        own = __reduce_max_sync(kFullMask, own);
-    } else if constexpr (kWhole) {
-#pragma unroll
-        for (int o = 16 / V; o > 0; o >>= 1) own = max(own, __shfl_xor_sync(kFullMask, own, o));
-    } else {
-        for (int o = min(32 / V, tpr) >> 1; o > 0; o >>= 1)
-            own = max(own, __shfl_xor_sync(kFullMask, own, o));
-    }
-    return scale_byte(own);
 }
 
 }  // namespace bigcn

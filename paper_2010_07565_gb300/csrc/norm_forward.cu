@@ -31,8 +31,8 @@ struct ForwardArgs {
     int64_t lde;
 };
 
-// Rows that do not fit registers (more than 8192 columns): a block per row, which walks it
-// three times; the later walks find it in L1 or L2.
+// Rows that do not fit registers (more than 8192 fp32 or 16384 16-bit columns): a block per
+// row, which walks it three times; the later walks find it in L1 or L2.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardArgs a) {
     const int K = a.K, lane = threadIdx.x & 31;
@@ -75,144 +75,134 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
     }
 }
 
-// Rows in registers. kWarp: a row is one warp's (tpr = 32, which makes every offset a constant),
-// else tpr threads'. Rows past N take part in the sums over threads and store nothing.
-template <typename T, int V, int J, bool kKeep, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 4 : 2)
-forward_rows_kernel(const ForwardArgs a, const int row_threads) {
+// Rows in registers (norm.cuh). kWarp: a row is one warp's (tpr = 32, which makes every offset a
+// constant), else tpr threads'. Rows past N take part in the sums over threads and store
+// nothing.
+template <typename T, int A, int J, bool kKeep, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? (J * kPiece<T> <= 16 ? 4 : 3) : 2)
+forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool aligned) {
+    constexpr int V = kPiece<T>, H = V / 2, kFull = full_pieces(V, J);
     __shared__ float red[2][1][kMostRowThreads / 32];
     const int tpr = kWarp ? 32 : row_threads;
     const int t = threadIdx.x & (tpr - 1);
     const int64_t i = int64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
     const bool live = i < a.N;
     if (kWarp && !live) return;
-    // Columns k0 + j step; those of this thread from `left` on are past the row. The first
-    // kFull vectors are within it.
-    constexpr int kFull = full_vectors(V, J);
+    // Piece j holds columns k0 + j step ..; left - j step of them are in the row, all V where
+    // j < kFull.
     const int K = a.K, k0 = t * V, step = tpr * V, left = K - k0;
     const float inv_k = 1.0f / float(K);
-    // The row as it was read: 16-bit elements take half the registers that way, and are
-    // converted where they are used.
-    Vec<T, V> x[J];
     const T *row = static_cast<const T *>(a.X) + (live ? i : 0) * a.ldx + k0;
+    float2 x[J][H];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        if (j < kFull || j * step < left) x[j] = *reinterpret_cast<const Vec<T, V> *>(row + j * step);
-        else
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[j].v[e] = from_f32<T>(0.0f);
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (j < kFull) w = load16<A>(row + j * step);
+        else if (left > j * step) w = load_piece<T, A>(row + j * step, left - j * step);
+        unpack16<T>(w, x[j]);
     }
-    float s[1] = {0.0f};
+    float2 s2 = both(0.0f);
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[0] += to_f32(x[j].v[e]);
+        for (int e = 0; e < H; ++e) s2 = __fadd2_rn(s2, x[j][e]);
+    float s[1] = {s2.x + s2.y};
     row_sum<kWarp>(s, tpr, red[0]);
     const float mean = s[0] * inv_k;
-    s[0] = 0.0f;
+    s2 = both(0.0f);
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-        if (j < kFull || j * step < left)
+    for (int j = 0; j < J; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float d = to_f32(x[j].v[e]) - mean;
-                s[0] = fmaf(d, d, s[0]);
-            }
+        for (int e = 0; e < H; ++e) x[j][e] = __fadd2_rn(x[j][e], both(-mean));
+        if (j >= kFull && left < j * step + V) clear_from(x[j], left - j * step);
+#pragma unroll
+        for (int e = 0; e < H; ++e) s2 = __ffma2_rn(x[j][e], x[j][e], s2);
+    }
+    s[0] = s2.x + s2.y;
     row_sum<kWarp>(s, tpr, red[1]);
-    if (!kWarp && !kKeep && !live) return;      // (with a checkpoint lanes still meet below)
     const float rstd = 1.0f / sqrtf(s[0] * inv_k + a.eps);
     if (live && t == 0) {
         if (a.mean) a.mean[i] = mean;
         if (a.rstd) a.rstd[i] = rstd;
     }
     T *out = static_cast<T *>(a.Y) + i * a.ldy + k0;
-    using Q = typename QWord<V>::type;
-    int8_t *qrow = a.q + i * a.ldq;
-    uint8_t *erow = a.exps + i * a.lde;
     const float *gamma = a.gamma ? a.gamma + k0 : kOnes, *beta = a.beta ? a.beta + k0 : kZeros;
     const int gstep = a.gamma ? step : 0, bstep = a.beta ? step : 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        if (j >= kFull && j * step >= K) break;     // the same for the whole row's threads
-        const bool in = (kWarp || live) && (j < kFull || j * step < left);
-        uint32_t top = 0;
-        float v[V];
+        const int n = j < kFull ? V : left - j * step;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            v[e] = (to_f32(x[j].v[e]) - mean) * rstd;
-            if (kKeep) top = max(top, abs_bits(v[e]));
-        }
-        if (kKeep && j >= kFull) top = in ? top : 0u;
-        if (in) {
-            const Vec<float, V> g = *reinterpret_cast<const Vec<float, V> *>(gamma + j * gstep);
-            const Vec<float, V> b = *reinterpret_cast<const Vec<float, V> *>(beta + j * bstep);
-            Vec<T, V> w;
+        for (int e = 0; e < H; ++e) x[j][e] = __fmul2_rn(x[j][e], both(rstd));
+        if (n <= 0 || (!kWarp && !live)) continue;
+        float2 g[H], b[H], y[H];
+        load_params(gamma + j * gstep, aligned, n, g);
+        load_params(beta + j * bstep, aligned, n, b);
 #pragma unroll
-            for (int e = 0; e < V; ++e) w.v[e] = from_f32<T>(fmaf(v[e], g.v[e], b.v[e]));
-            *reinterpret_cast<Vec<T, V> *>(out + j * step) = w;
-        }
-        if constexpr (kKeep) {
-            const uint32_t b = group_byte<V, kWarp>(top, tpr);
-            if (in) {
-                *reinterpret_cast<Q *>(qrow + k0 + j * step) = quantise<V>(v, pack_factor(b));
-                // A warp's step is a whole number of groups.
-                if (kWarp ? (k0 & (kGroup - 1)) == 0 : ((k0 + j * step) & (kGroup - 1)) == 0)
-                    erow[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
-            }
-        }
+        for (int e = 0; e < H; ++e) y[e] = __ffma2_rn(x[j][e], g[e], b[e]);
+        store_piece<T, A>(out + j * step, pack16<T>(y), n);
     }
-    if constexpr (kKeep)
-        if (live) {
-            const int groups = int(checkpoint_groups(K));
-            for (int k = K + t; k < (K + 15) / 16 * 16; k += tpr) qrow[k] = 0;
-            for (int g = groups + t; g < (groups + 3) / 4 * 4; g += tpr) erow[g] = 0;
+    if constexpr (kKeep) {
+        uint32_t own[J], top[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) own[j] = top_bits(x[j]);
+        group_tops<32 / V>(own, top);
+        if (!kWarp && !live) return;
+        int8_t *q = a.q + i * a.ldq + k0;
+        uint8_t *exps = a.exps + i * a.lde;
+        const int kq = (K + 15) / 16 * 16 - k0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (j >= kFull && j * step >= kq) break;
+            const uint32_t b = scale_byte(top[j]);
+            *reinterpret_cast<QPiece<H> *>(q + j * step) = quantise_piece(x[j], pack_factor(b));
+            if ((t & (32 / V - 1)) == 0 && j * step < left)
+                exps[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
         }
+        const int groups = int(checkpoint_groups(K));
+        if (groups + t < (groups + 3) / 4 * 4) exps[groups + t] = 0;
+    }
 }
 
-template <typename T, int V, int J, bool kWarp>
-void launch_kind(const ForwardArgs &a, int tpr, cudaStream_t s) {
+template <typename T, int A, int J>
+void launch_rows(const ForwardArgs &a, int tpr, bool aligned, cudaStream_t s) {
     const int threads = tpr > kRowThreads ? tpr : kRowThreads, rows = threads / tpr;
     const unsigned grid = unsigned((a.N + rows - 1) / rows);
-    if (a.q) forward_rows_kernel<T, V, J, true, kWarp><<<grid, threads, 0, s>>>(a, tpr);
-    else forward_rows_kernel<T, V, J, false, kWarp><<<grid, threads, 0, s>>>(a, tpr);
+    if (tpr == 32) {
+        if (a.q) forward_rows_kernel<T, A, J, true, true><<<grid, threads, 0, s>>>(a, tpr, aligned);
+        else forward_rows_kernel<T, A, J, false, true><<<grid, threads, 0, s>>>(a, tpr, aligned);
+    } else if constexpr (J <= 4) {
+        if (a.q) forward_rows_kernel<T, A, J, true, false><<<grid, threads, 0, s>>>(a, tpr, aligned);
+        else forward_rows_kernel<T, A, J, false, false><<<grid, threads, 0, s>>>(a, tpr, aligned);
+    }
 }
 
-template <typename T, int V, int J>
-void launch_rows(const ForwardArgs &a, int tpr, cudaStream_t s) {
-    if (tpr == 32) launch_kind<T, V, J, true>(a, tpr, s);
-    else if constexpr (V * J <= 16 || V == 8) launch_kind<T, V, J, false>(a, tpr, s);
-}
-
-template <typename T, int V>
-bool launch_width(const ForwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
-    const RowLayout r = row_layout(a.N, a.K, V, a.q ? 32 / V : 8, 32, V == 8 ? 32 : 16, dev);
-    if (r.J == 1) launch_rows<T, V, 1>(a, r.tpr, s);
-    else if (r.J == 2) launch_rows<T, V, 2>(a, r.tpr, s);
-    else if (r.J == 4) launch_rows<T, V, 4>(a, r.tpr, s);
-    else if (V <= 4 && r.J == 8) launch_rows<T, V, V <= 4 ? 8 : 1>(a, r.tpr, s);
-    else if (V == 2 && r.J == 12) launch_rows<T, V, V == 2 ? 12 : 1>(a, r.tpr, s);
-    else if (V == 1 && r.J == 16) launch_rows<T, V, V == 1 ? 16 : 1>(a, r.tpr, s);
-    else if (V == 1 && r.J == 24) launch_rows<T, V, V == 1 ? 24 : 1>(a, r.tpr, s);
-    else return false;
-    return true;
+template <typename T, int A>
+bool launch_aligned(const ForwardArgs &a, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
+    constexpr bool kWide = sizeof(T) == 4;      // pieces of four columns: up to eight of them
+    const RowLayout r = row_layout(a.N, a.K, kPiece<T>, kWide ? 16 : 32, 32, dev);
+    switch (r.J) {
+    case 1: launch_rows<T, A, 1>(a, r.tpr, aligned, s); return true;
+    case 2: launch_rows<T, A, 2>(a, r.tpr, aligned, s); return true;
+    case 3: launch_rows<T, A, 3>(a, r.tpr, aligned, s); return true;
+    case 4: launch_rows<T, A, 4>(a, r.tpr, aligned, s); return true;
+    case 5: launch_rows<T, A, kWide ? 5 : 1>(a, r.tpr, aligned, s); return true;
+    case 6: launch_rows<T, A, kWide ? 6 : 1>(a, r.tpr, aligned, s); return true;
+    case 8: launch_rows<T, A, kWide ? 8 : 1>(a, r.tpr, aligned, s); return true;
+    }
+    return false;
 }
 
 template <typename T>
 void launch_forward(const ForwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
-    // Vectors of x and y; those of gamma and beta are fp32, q's are V bytes of 16-byte rows.
-    const uint64_t es = sizeof(T), f = 4 / es;
-    const uint64_t where[] = {uint64_t(uintptr_t(a.X)),
-                              uint64_t(uintptr_t(a.Y)),
-                              uint64_t(a.ldx) * es,
-                              uint64_t(a.ldy) * es,
-                              uint64_t(a.K) * es,
-                              uint64_t(uintptr_t(a.gamma)) / f,
-                              uint64_t(uintptr_t(a.beta)) / f};
-    const int V = vector_width(es, where, 7);
-    const bool done = V == 1   ? launch_width<T, 1>(a, dev, s)
-                      : V == 2 ? launch_width<T, 2>(a, dev, s)
-                      : V == 4 ? launch_width<T, 4>(a, dev, s)
-                               : launch_width<T, es == 2 ? 8 : 4>(a, dev, s);
+    const uint64_t es = sizeof(T);
+    const uint64_t rows[] = {uint64_t(uintptr_t(a.X)), uint64_t(a.ldx) * es, uint64_t(uintptr_t(a.Y)),
+                             uint64_t(a.ldy) * es};
+    const bool aligned = aligned_to(a.gamma, 16) && aligned_to(a.beta, 16);
+    const int A = alignment_of(rows, 4);
+    const bool done = A == 16  ? launch_aligned<T, 16>(a, aligned, dev, s)
+                      : A == 8 ? launch_aligned<T, 8>(a, aligned, dev, s)
+                      : A == 4 ? launch_aligned<T, 4>(a, aligned, dev, s)
+                               : launch_aligned<T, es == 2 ? 2 : 4>(a, aligned, dev, s);
     if (done) return;
     const int64_t most = int64_t(dev.sm_count) * 64;
     forward_any_kernel<T><<<unsigned(a.N < most ? a.N : most), kRowThreads, 0, s>>>(a);

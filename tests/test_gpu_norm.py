@@ -398,3 +398,95 @@ def test_binding_refusals(cuda_device):
         B.bigcn_layer_norm_forward(X, None, None, EPS, X)
     with pytest.raises(B.BigcnError):
         B.bigcn_checkpoint_pack(X, torch.empty((4, 40), dtype=torch.int8, device=cuda_device), exps)
+
+
+# Enough rows for the kernels that stage them in shared memory: widths whose rows start at
+# every multiple of their element's size, several rows a stage, a last set that is not full,
+# matrices that begin and end off 16-byte boundaries.
+MANY = [("float32", 20011, 602, 0, 0), ("float32", 39001, 128, 0, 0), ("float32", 10007, 603, 0, 0),
+        ("float32", 9999, 1024, 0, 0), ("float32", 10001, 601, 2, 3), ("float32", 5003, 1433, 0, 0),
+        ("float32", 12000, 300, 4, 4), ("float32", 9973, 997, 0, 1), ("float32", 20000, 140, 1, 2),
+        ("bfloat16", 40007, 256, 0, 0), ("bfloat16", 20001, 601, 0, 0),
+        ("bfloat16", 20003, 602, 0, 2), ("bfloat16", 10005, 1000, 4, 4),
+        ("bfloat16", 10005, 1021, 3, 7), ("float16", 39999, 260, 0, 0),
+        ("float16", 10003, 513, 0, 5), ("float16", 5001, 2050, 0, 0), ("float16", 10111, 770, 2, 6)]
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("dtype,N,K,pad,offset", MANY)
+def test_forward_many_rows(cuda_device, dtype, N, K, pad, offset, keep):
+    x = rows(N, K, N + K, dtype)
+    gamma, beta = params(K, K)
+    X, _ = strided(x, pad, offset, cuda_device)
+    Yv, buf = strided(torch.zeros_like(x), pad, offset, cuda_device, fill=7.0)
+    mean, rstd = torch.empty(N, device=cuda_device), torch.empty(N, device=cuda_device)
+    q, exps = B.checkpoint_buffers(N, K, cuda_device) if keep else (None, None)
+    t = lambda a: torch.from_numpy(a).to(cuda_device)
+    B.bigcn_layer_norm_forward(X, t(gamma), t(beta), EPS, Yv, mean, rstd, q, exps)
+    ry, rm, rr, rx = R.forward(f64(x), gamma, beta, EPS)
+    ey, em, er, ex = R.forward_bounds(f64(x), gamma, beta, EPS, dtype)
+    within(Yv, ry, ey, "Y")
+    within(mean, rm, em, "mean")
+    within(rstd, rr, er, "rstd")
+    if keep:
+        en = exps.cpu().numpy()
+        step = np.repeat(2.0 ** (en.astype(float) - 127), 32, axis=1)[:, :K]
+        within(R.values(q.cpu().numpy(), en), rx, step / 2 + ex, "checkpoint")
+        if dtype == "float32":
+            B.bigcn_layer_norm_forward(X, None, None, EPS, Yv, None, None, q, exps)
+            q2, e2 = B.checkpoint_pack(Yv)
+            assert torch.equal(q, q2) and torch.equal(exps, e2)
+    Yv.fill_(7.0)
+    assert (buf == 7.0).all()
+    assert B.device_timeouts() == 0
+
+
+@pytest.mark.parametrize("source", ["input", "checkpoint"])
+@pytest.mark.parametrize("dtype,N,K,pad,offset", MANY)
+def test_backward_many_rows(cuda_device, dtype, N, K, pad, offset, source):
+    x = rows(N, K, 2 * N + K, dtype)
+    dy = (0.1 * rows(N, K, 7 * N + K, "float32", level=0.2)).to(DTYPES[dtype])
+    gamma, _ = params(K, K + 1)
+    _, rm, rr, rx = R.forward(f64(x), gamma, np.zeros(K), EPS)
+    t = lambda a: torch.from_numpy(a.astype(np.float32)).to(cuda_device)
+    mean, rstd = t(rm), t(rr)
+    if source == "input":
+        X, _ = strided(x, pad, offset, cuda_device)
+        xhat = (f64(x) - f64(mean)[:, None]) * f64(rstd)[:, None]
+        kw, ex = dict(X=X, mean=mean), 2 * R.U * np.abs(xhat)
+    else:
+        q, exps = B.checkpoint_pack(t(rx))
+        xhat, ex = R.values(q.cpu().numpy(), exps.cpu().numpy()), np.zeros((N, K))
+        kw = dict(q=q, exps=exps)
+    dY, _ = strided(dy, pad, offset, cuda_device)
+    dX, buf = strided(torch.zeros_like(dy), pad, offset, cuda_device, fill=7.0)
+    ws = torch.empty(B.bigcn_layer_norm_backward_workspace_bytes(N, K), dtype=torch.uint8,
+                     device=cuda_device)
+    dg, db = torch.empty(K, device=cuda_device), torch.empty(K, device=cuda_device)
+    B.bigcn_layer_norm_backward(dY, t(gamma), rstd, ws, dX=dX, dgamma=dg, dbeta=db, **kw)
+    rdx, rdg, rdb = R.backward(f64(dy), gamma, xhat, f64(rstd))
+    e, eg, eb = R.backward_bounds(f64(dy), gamma, xhat, f64(rstd), dtype, ex)
+    within(dX, rdx, e, "dX")
+    within(dg, rdg, eg, "dgamma")
+    within(db, rdb, eb, "dbeta")
+    again = [torch.empty_like(dg), torch.empty_like(db)]
+    B.bigcn_layer_norm_backward(dY, t(gamma), rstd, ws, dgamma=again[0], dbeta=again[1], **kw)
+    assert torch.equal(again[0], dg) and torch.equal(again[1], db)
+    dX.fill_(7.0)
+    assert (buf == 7.0).all()
+    assert B.device_timeouts() == 0
+
+
+def test_many_rows_with_nan_and_infinite_rows(cuda_device):
+    N, K = 20000, 602
+    x = rows(N, K, 5, "float32")
+    x[11, 600], x[12, 0], x[N - 1, K - 1] = float("nan"), float("inf"), float("nan")
+    bad = torch.zeros(N, dtype=torch.bool)
+    bad[[11, 12, N - 1]] = True
+    X = x.to(cuda_device)
+    Y, mean, rstd, q, exps = B.layer_norm_forward(X)
+    assert torch.equal(torch.isnan(Y).all(1).cpu(), bad) and torch.equal(torch.isnan(Y).any(1).cpu(), bad)
+    assert torch.equal((exps == 255).all(1).cpu(), bad)
+    dX, dg, db = B.layer_norm_backward(torch.ones_like(X), None, rstd, q=q, exps=exps)
+    assert torch.equal(torch.isnan(dX).any(1).cpu(), bad)
+    assert torch.isnan(dg).all() and torch.isfinite(db).all()
