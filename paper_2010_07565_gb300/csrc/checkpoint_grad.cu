@@ -8,35 +8,32 @@
 // and is a bf16; dZ is one bf16 part (bf16), two (fp16: 8 + 3 bits, exact) or three (fp32,
 // within 2^-23 of it).
 //
-// Operands. M = 128 features a tile, N = the columns, the contraction over 32 rows a
+// Operands. M = 128 features a tile, N = the columns, the contraction over 32 or 64 rows a
 // stage. Both matrices are row-major, i.e. their features and columns lie along memory
 // rows, and the tensor core takes them that way (MN-major), so nothing is transposed: a
 // bf16 dZ goes by tensor copies from memory into its swizzled place; q (and an fp32 or
 // fp16 dZ) by tensor copies into a ring of raw slots, from which the workers expand it.
 //
-// Roles of a CTA (320 threads): warps 0-7, the workers, turn raw slots into operand
-// stages; they also keep the running sums. Warp 8 copies, warp 9 issues the MMAs. They meet
+// Roles of a CTA (576 threads): warps 0-15, the workers, turn raw slots into operand
+// stages and take the running sums. Warp 16 copies, warp 17 issues the MMAs. They meet
 // on mbarriers only:
 //   loaded[slot]   a slot's copies have landed         freed[slot]   it may be refilled
 //   filled[stage]  the workers have written a stage    used[stage]   its MMAs are done
-//   summed[half]   a block's MMAs are done             drained[half] its sums were taken
+//   summed         a block's MMAs are done             drained       its sums were taken
 //
 // Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
 // result per accumulating MMA, always towards 0; 1080 MMAs gave 2.2e-5), so an accumulator
-// takes kDrain stages, about 40 MMAs (8e-7), and is then added in fp32 to the workers'
-// registers: 256 accumulator columns in each half of tensor memory, one filling while the
-// other drains, 128 sums a thread.
+// takes kDrain stages, about 40 MMAs (8e-7), and is then added, in fp32, to the running sums:
+// 256 accumulator columns of tensor memory and 256 of sums. (Sums in registers, with two
+// accumulators in turn, left room for 8 worker warps: 236 us at 232,965 x 602 x 128 fp32, the
+// workers' instructions at 1.7 a cycle being the limit.)
 //
 // Split. A CTA holds 256 / NT feature tiles (`mt` of them, fewer in small calls), so that
-// dZ is read once for that many; the rows are split so that the grid is about one CTA per
-// SM (kGradCtas), a last group of fewer tiles into fewer parts. A second kernel adds the
-// parts in order, sums s_j, and applies gamma and beta. The columns of dZ are summed by the
-// CTA that has them in shared memory anyway: of the groups of feature tiles that read the
+// dZ is read and split into parts once for that many; the rows are split so that the grid is
+// about one CTA per SM (kGradCtas), a last group of fewer tiles into fewer runs. A second kernel
+// adds the runs in order, sums s_j, and applies gamma and beta. The columns of dZ are summed by
+// the CTA that has them in shared memory anyway: of the groups of feature tiles that read the
 // same rows, group g takes the g-th 64 columns.
-//
-// What bounds it: tensor time where dZ is fp32 (three parts: 58 us of MMAs against 39 us
-// of copies at 232,965 x 602 x 128), reading dZ once per group of tiles and the workers'
-// expansion elsewhere.
 #include "checkpoint.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -48,15 +45,13 @@ __device__ unsigned int g_grad_timeouts;
 namespace {
 
 constexpr int kGradCtas = 152;          // SMs of the card
-constexpr int kWorkers = 256;
+constexpr int kWorkers = 512;
 constexpr int kWorkerWarps = kWorkers / 32;
 constexpr int kCopyWarp = kWorkerWarps, kMmaWarp = kWorkerWarps + 1;
 constexpr int kGradThreads = kWorkers + 64;
-constexpr int kRows = kAtomRows;        // rows of a stage
-constexpr int kAccCols = 256;           // accumulator columns of half the tensor memory
-constexpr int kSumsPerThread = kAccCols / 2;
+constexpr int kAccCols = 256;           // accumulator columns; as many of running sums
 constexpr size_t kAlign = 256;
-constexpr int kSmemMost = 227 * 1024 - 1024 - 3072;   // less alignment and static memory
+constexpr int kSmemMost = 227 * 1024 - 1024 - 5120;   // less alignment and static memory
 
 __host__ __device__ constexpr int round_up_to(int x, int a) { return (x + a - 1) / a * a; }
 
@@ -66,19 +61,23 @@ template <int NT, int PARTS, bool kTma>
 struct GradShape {
     static constexpr int kTiles = kAccCols / NT;
     static constexpr bool kDirect = kTma && PARTS == 1;     // copied as an operand
+    // Rows of a stage: 64 where the stages' B needs no room of its own, which halves what the
+    // workers spend on barriers.
+    static constexpr int kRows = kDirect ? 64 : 32;
+    static constexpr int kAtom = kRows * 128;
     static constexpr int kElem = PARTS == 3 ? 4 : 2;
     static constexpr int kSlotZ = kTma ? kRows * NT * kElem : 0;
     static constexpr int kSlotQ = kTiles * kRows * 128;
     static constexpr int kSlot = round_up_to(kSlotZ + kSlotQ + kTiles * kRows * 4, 1024);
-    static constexpr int kOpA = kTiles * 2 * kAtomBytes;
-    static constexpr int kPart = NT / 64 * kAtomBytes;
+    static constexpr int kOpA = kTiles * 2 * kAtom;
+    static constexpr int kPart = NT / 64 * kAtom;
     static constexpr int kOp = kOpA + (kDirect ? 0 : PARTS * kPart);
     static constexpr int kStages = 3 * (kOp + kSlot) <= kSmemMost ? 3 : 2;
     static constexpr int kFit = (kSmemMost - kStages * kOp) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
     static constexpr int kSmem = 1024 + kStages * kOp + kSlots * kSlot;
-    // About 40 accumulating MMAs (two per stage and part) between two drains.
-    static constexpr int kDrain = PARTS == 1 ? 20 : PARTS == 2 ? 10 : 7;
+    // About 40 accumulating MMAs (kRows / 16 per stage and part) between two drains.
+    static constexpr int kDrain = kDirect ? 10 : PARTS == 1 ? 20 : PARTS == 2 ? 10 : 7;
     static_assert(kSlots >= 2, "shared memory per CTA");
 };
 
@@ -91,6 +90,7 @@ struct GradParams {
     const void *dZ;
     int64_t lddz;
     int F;
+    int64_t stages;          // of kRows rows
     int nt;                  // column tiles
     int64_t tiles;           // feature tiles
     int mt;                  // feature tiles of a group
@@ -146,10 +146,11 @@ template <typename T, int NT, int PARTS, bool kTma>
 __global__ void __launch_bounds__(kGradThreads, 1)
 grad_rows_kernel(const __grid_constant__ GradParams p) {
     using S = GradShape<NT, PARTS, kTma>;
-    constexpr int kSlots = S::kSlots, kStages = S::kStages, kDrain = S::kDrain;
+    constexpr int kSlots = S::kSlots, kStages = S::kStages, kDrain = S::kDrain, kRows = S::kRows;
+    constexpr int kAtom = S::kAtom;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t loaded[kSlots], freed[kSlots], filled[kStages], used[kStages],
-        summed[2], drained[2], done;
+        summed, drained, done;
     __shared__ float colpart[kWorkerWarps][64];
     __shared__ uint32_t tmem_base, stop;
 
@@ -166,11 +167,11 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     const int runs = r < full ? p.parts_full : p.parts_last;
     const int64_t tile0 = group * p.mt;
     const int mt = int(min(int64_t(p.mt), p.tiles - tile0));
-    const int64_t stages = (p.N + kRows - 1) / kRows;
-    const int64_t st0 = stages * run / runs;
-    const int n = int(stages * (run + 1) / runs - st0);
+    const int64_t st0 = p.stages * run / runs;
+    const int n = int(p.stages * (run + 1) / runs - st0);
     const int n0 = ny * NT, cols = min(NT, p.F - n0), atoms = (cols + 63) / 64;
-    const bool sums_cols = group < NT / 64;             // of the columns n0 + 64 group ..
+    const bool sums_cols = group < atoms;               // of the columns n0 + 64 group ..
+    const int own = sums_cols ? int(group) : -1;
 
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -187,10 +188,8 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             mbar_init(smem_addr(&filled[s]), kWorkerWarps);
             mbar_init(smem_addr(&used[s]), 1);
         }
-        for (int h = 0; h < 2; ++h) {
-            mbar_init(smem_addr(&summed[h]), 1);
-            mbar_init(smem_addr(&drained[h]), kWorkerWarps);
-        }
+        mbar_init(smem_addr(&summed), 1);
+        mbar_init(smem_addr(&drained), kWorkerWarps);
         mbar_init(smem_addr(&done), 1);
         stop = 0u;
         mbar_fence_init();
@@ -201,12 +200,7 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     const uint32_t tmem = tmem_base;
     volatile uint32_t *const stopv = &stop;
 
-    float sum[kSumsPerThread];
-    float colsum[8];
-#pragma unroll
-    for (int c = 0; c < kSumsPerThread; ++c) sum[c] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) colsum[c] = 0.0f;
+    float colsum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 
     if (warp == kCopyWarp) {
         const uint32_t bytes = uint32_t(mt * kRows * 128 + (kTma ? atoms * kRows * 64 * S::kElem : 0));
@@ -223,11 +217,15 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             const uint32_t bar = smem_addr(&loaded[s]);
             const int64_t row0 = (st0 + st) * kRows;
             // Scale bytes: lane = row, four groups (128 features) a copy.
-            const bool in = row0 + lane < p.N;
-            const uint8_t *e = p.exps + (in ? (row0 + lane) * p.lde + tile0 * 4 : 0);
-            for (int t = 0; t < mt; ++t)
-                copy4(slot + uint32_t(S::kSlotZ + S::kSlotQ + (t * kRows + lane) * 4),
-                      in ? e + t * 4 : e, in ? 4u : 0u);
+#pragma unroll
+            for (int h = 0; h < kRows / 32; ++h) {
+                const int row = 32 * h + lane;
+                const bool in = row0 + row < p.N;
+                const uint8_t *e = p.exps + (in ? (row0 + row) * p.lde + tile0 * 4 : 0);
+                for (int t = 0; t < mt; ++t)
+                    copy4(slot + uint32_t(S::kSlotZ + S::kSlotQ + (t * kRows + row) * 4),
+                          in ? e + t * 4 : e, in ? 4u : 0u);
+            }
             if (lane == 0) {
                 mbar_expect(bar, bytes);
                 if constexpr (kTma)
@@ -251,13 +249,12 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             bool any = false;
             for (int st = 0; st < n; ++st) {
                 const int s = st % kSlots, o = st % kStages;
-                const int block = st / kDrain, half = block & 1, at = st % kDrain;
+                const int block = st / kDrain, at = st % kDrain;
                 bool go = wait_unless(smem_addr(&filled[o]), uint32_t(st / kStages) & 1u, stopv);
                 if (S::kDirect)
                     go = go && wait_unless(smem_addr(&loaded[s]), uint32_t(st / kSlots) & 1u, stopv);
-                if (at == 0 && block >= 2)
-                    go = go && wait_unless(smem_addr(&drained[half]), uint32_t(block / 2 - 1) & 1u,
-                                           stopv);
+                if (at == 0 && block > 0)
+                    go = go && wait_unless(smem_addr(&drained), uint32_t(block - 1) & 1u, stopv);
                 if (!go) {
                     *stopv = 1u;
                     break;
@@ -271,57 +268,61 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                     for (int t = 0; t < mt; ++t)
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part)
-                            mma_rows(tmem + uint32_t(half * kAccCols + t * NT),
-                                     atom_desc(a0 + uint32_t(t * 2 * kAtomBytes + k * 2048)),
-                                     atom_desc(b0 + uint32_t(part * S::kPart + k * 2048)), idesc,
+                            mma_rows(tmem + uint32_t(t * NT),
+                                     atom_desc<kRows>(a0 + uint32_t(t * 2 * kAtom + k * 2048)),
+                                     atom_desc<kRows>(b0 + uint32_t(part * S::kPart + k * 2048)), idesc,
                                      at > 0 || k > 0 || part > 0);
                 any = true;
                 mma_commit(smem_addr(&used[o]));
                 if (S::kDirect) mma_commit(smem_addr(&freed[s]));
-                if (at == kDrain - 1 || st == n - 1) mma_commit(smem_addr(&summed[half]));
+                if (at == kDrain - 1 || st == n - 1) mma_commit(smem_addr(&summed));
             }
             if (any) mma_commit(smem_addr(&done));
             else mbar_arrive(smem_addr(&done));
         }
         __syncwarp();
     } else {
-        // Worker: row `row` of a stage, 16 features 16 c .. of each tile, 8 columns 8 c .. of
-        // each atom. Loaded without tensor copies, dZ is taken four rows a warp, a column per
+        // Worker: row `row` of 32 of a stage, 8 features 8 c .. of each tile, 4 columns 4 c .. of
+        // each atom. Loaded without tensor copies, dZ is taken two rows a warp, a column per
         // lane, a stage ahead.
-        const int row = tid >> 3, c = tid & 7;
-        const int quad = warp & 3, colhalf = warp >> 2;
+        const int row = tid >> 4, c = tid & 15;
+        const int quad = warp & 3, quarter = warp >> 2;
         constexpr int kLoadCols = kTma ? 1 : NT / 32;
-        float z[kLoadCols][4];
+        float z[kLoadCols][2];
         auto load = [&](int st) {
             if constexpr (!kTma) {
-                const int64_t i = (st0 + st) * kRows + 4 * warp;
+                const int64_t i = (st0 + st) * kRows + 2 * warp;
 #pragma unroll
                 for (int q = 0; q < kLoadCols; ++q)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 2; ++e)
                         z[q][e] = st < n && n0 + 32 * q < p.F ? dz_at<T>(p, i + e, n0 + 32 * q + lane)
                                                               : 0.0f;
             }
         };
-        // Adds the accumulators of block b to the running sums.
+        // Adds the accumulators of block b to the running sums: this warp's lanes, 64 columns.
         auto drain = [&](int b) -> bool {
-            const bool go = wait_unless(smem_addr(&summed[b & 1]), uint32_t(b / 2) & 1u, stopv);
+            const bool go = wait_unless(smem_addr(&summed), uint32_t(b) & 1u, stopv);
             if (!__all_sync(kFullMask, go)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = tmem + (uint32_t(32 * quad) << 16) +
-                                uint32_t((b & 1) * kAccCols + colhalf * kSumsPerThread);
+            const uint32_t at = tmem + (uint32_t(32 * quad) << 16) + uint32_t(64 * quarter);
+#pragma unroll 1
+            for (int w = 0; w < 2; ++w) {
+                if (64 * quarter + 32 * w >= mt * NT) break;
+                uint32_t acc[32], sum[32];
+                tmem_ld32(at + uint32_t(32 * w), acc);
+                if (b > 0) {
+                    tmem_ld32(at + uint32_t(kAccCols + 32 * w), sum);
 #pragma unroll
-            for (int w = 0; w < kSumsPerThread / 32; ++w) {
-                if (colhalf * kSumsPerThread + 32 * w < mt * NT) {
-                    uint32_t acc[32];
-                    tmem_ld32(at + uint32_t(32 * w), acc);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[32 * w + j] += __uint_as_float(acc[j]);
+                    for (int j = 0; j < 32; ++j)
+                        acc[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(acc[j]));
                 }
+                tmem_st32(at + uint32_t(kAccCols + 32 * w), acc);
             }
+            tmem_wait_st();
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&drained[b & 1]));
+            if (lane == 0) mbar_arrive(smem_addr(&drained));
             return true;
         };
         int taken = 0;                  // blocks drained
@@ -329,8 +330,9 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
         load(0);
 #pragma unroll 1
         for (int st = 0; st < n; ++st) {
-            // A block is drained kStages stages after its end: its MMAs are done by then.
-            if (st >= (taken + 1) * kDrain + kStages) {
+            // A block is drained one stage after its end: its MMAs are done by then, and the
+            // next one's first stage is filled.
+            if (st > (taken + 1) * kDrain) {
                 ok = drain(taken);
                 if (!ok) break;
                 ++taken;
@@ -343,100 +345,81 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             if (!ok) break;
             const unsigned char *slot = mem + kSlot0 + s * S::kSlot;
             unsigned char *op = mem + o * S::kOp;
-            // A: 16 features of a row to two 16-byte chunks. Lanes of the second atom write
-            // theirs in the other order, so that 8 lanes cover all banks.
-#pragma unroll 2
+            // A: 8 features of a row to a 16-byte chunk.
             for (int t = 0; t < mt; ++t) {
-                const unsigned char *sq = slot + S::kSlotZ + t * kRows * 128;
-                const uint4 q = *reinterpret_cast<const uint4 *>(sq + row * 128 + c * 16);
-                const __nv_bfloat162 f =
-                    bf16_factor(slot[S::kSlotZ + S::kSlotQ + (t * kRows + row) * 4 + (c >> 1)]);
-                uint4 v[2];
-                expand4(q.x, f, v[0].x, v[0].y);
-                expand4(q.y, f, v[0].z, v[0].w);
-                expand4(q.z, f, v[1].x, v[1].y);
-                expand4(q.w, f, v[1].z, v[1].w);
-                unsigned char *atom = op + (2 * t + (c >> 2)) * kAtomBytes;
-                const bool swap = c >= 4;
-                const int ch = 2 * (c & 3);
-                *reinterpret_cast<uint4 *>(atom + atom_offset(row, ch + (swap ? 1 : 0))) =
-                    swap ? v[1] : v[0];
-                *reinterpret_cast<uint4 *>(atom + atom_offset(row, ch + (swap ? 0 : 1))) =
-                    swap ? v[0] : v[1];
+#pragma unroll
+                for (int h = 0; h < kRows / 32; ++h) {
+                    const int rr = row + 32 * h;
+                    const uint2 q = *reinterpret_cast<const uint2 *>(slot + S::kSlotZ +
+                                                                     (t * kRows + rr) * 128 + c * 8);
+                    const __nv_bfloat162 f = bf16_factor(
+                        slot[S::kSlotZ + S::kSlotQ + (t * kRows + rr) * 4 + (c >> 2)]);
+                    uint4 v;
+                    expand4(q.x, f, v.x, v.y);
+                    expand4(q.y, f, v.z, v.w);
+                    *reinterpret_cast<uint4 *>(op + (2 * t + (c >> 3)) * kAtom +
+                                               atom_offset(rr, c & 7)) = v;
+                }
             }
             // B: dZ's parts, and its columns' sums.
             if constexpr (S::kDirect) {
-                if (sums_cols && int(group) < atoms) {
-                    const uint4 u = *reinterpret_cast<const uint4 *>(
-                        slot + int(group) * kAtomBytes + atom_offset(row, c));
-                    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                if (sums_cols)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 f = bf16_pair(w[e]);
-                        colsum[2 * e] += f.x;
-                        colsum[2 * e + 1] += f.y;
+                    for (int h = 0; h < kRows / 32; ++h) {
+                        const uint2 u = *reinterpret_cast<const uint2 *>(
+                            slot + own * kAtom + atom_offset(row + 32 * h, c >> 1) + (c & 1) * 8);
+                        const float2 f0 = bf16_pair(u.x), f1 = bf16_pair(u.y);
+                        colsum[0] += f0.x;
+                        colsum[1] += f0.y;
+                        colsum[2] += f1.x;
+                        colsum[3] += f1.y;
                     }
-                }
             } else if constexpr (kTma) {
 #pragma unroll
                 for (int a = 0; a < NT / 64; ++a) {
                     if (a >= atoms) break;
-                    float v[8];
-                    if constexpr (PARTS == 3) {     // 32 bytes a lane, halves in the order
-                        const unsigned char *z0 = slot + (a * kRows + row) * 256 + c * 32;
-                        const bool swap = c >= 4;   // that spreads 8 lanes over all banks
-                        const float4 x = *reinterpret_cast<const float4 *>(z0 + (swap ? 16 : 0));
-                        const float4 y = *reinterpret_cast<const float4 *>(z0 + (swap ? 0 : 16));
-                        const float4 lo = swap ? y : x, hi = swap ? x : y;
-                        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
-                        v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+                    float v[4];
+                    if constexpr (PARTS == 3) {
+                        const float4 x = *reinterpret_cast<const float4 *>(
+                            slot + (a * kRows + row) * 256 + c * 16);
+                        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
                     } else {
-                        const uint4 u = *reinterpret_cast<const uint4 *>(
-                            slot + (a * kRows + row) * 128 + c * 16);
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 f =
-                                __half22float2(*reinterpret_cast<const __half2 *>(&w[e]));
-                            v[2 * e] = f.x;
-                            v[2 * e + 1] = f.y;
-                        }
+                        const uint2 u = *reinterpret_cast<const uint2 *>(
+                            slot + (a * kRows + row) * 128 + c * 8);
+                        const float2 f0 = __half22float2(*reinterpret_cast<const __half2 *>(&u.x));
+                        const float2 f1 = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
+                        v[0] = f0.x, v[1] = f0.y, v[2] = f1.x, v[3] = f1.y;
                     }
-                    if (sums_cols && a == int(group))
+                    if (a == own)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) colsum[e] += v[e];
-                    uint32_t part[4][3];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) parts_of<PARTS>(v[2 * e], v[2 * e + 1], part[e]);
-                    unsigned char *dst = op + S::kOpA + a * kAtomBytes + atom_offset(row, c);
+                        for (int e = 0; e < 4; ++e) colsum[e] += v[e];
+                    uint32_t x[3], y[3];
+                    parts_of<PARTS>(v[0], v[1], x);
+                    parts_of<PARTS>(v[2], v[3], y);
+                    unsigned char *dst =
+                        op + S::kOpA + a * kAtom + atom_offset(row, c >> 1) + (c & 1) * 8;
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q)
-                        *reinterpret_cast<uint4 *>(dst + q * S::kPart) =
-                            make_uint4(part[0][q], part[1][q], part[2][q], part[3][q]);
+                        *reinterpret_cast<uint2 *>(dst + q * S::kPart) = make_uint2(x[q], y[q]);
                 }
             } else {
 #pragma unroll
                 for (int q = 0; q < kLoadCols; ++q) {
                     if (q / 2 >= atoms) break;
-                    if (sums_cols && q / 2 == int(group))
-                        colsum[q % 2] += (z[q][0] + z[q][1]) + (z[q][2] + z[q][3]);
+                    if (q / 2 == own) colsum[q % 2] += z[q][0] + z[q][1];
                     // Neighbouring lanes exchange a row's value: the even one writes the pair
-                    // of columns of rows 0 and 2, the odd one of rows 1 and 3.
+                    // of columns of the first row, the odd one of the second.
                     const bool odd = lane & 1;
+                    const float got = __shfl_xor_sync(kFullMask, odd ? z[q][0] : z[q][1], 1);
+                    uint32_t part[3];
+                    parts_of<PARTS>(odd ? got : z[q][0], odd ? z[q][1] : got, part);
+                    const int col = 32 * (q % 2) + (lane & ~1);
+                    unsigned char *dst = op + S::kOpA + (q / 2) * kAtom +
+                                         atom_offset(2 * warp + (odd ? 1 : 0), col >> 3) +
+                                         (col & 7) * 2;
 #pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        const float got =
-                            __shfl_xor_sync(kFullMask, odd ? z[q][e] : z[q][e + 1], 1);
-                        uint32_t part[3];
-                        parts_of<PARTS>(odd ? got : z[q][e], odd ? z[q][e + 1] : got, part);
-                        const int rr = 4 * warp + e + (odd ? 1 : 0);
-                        const int col = 32 * (q % 2) + (lane & ~1);
-                        unsigned char *dst = op + S::kOpA + (q / 2) * kAtomBytes +
-                                             atom_offset(rr, col >> 3) + (col & 7) * 2;
-#pragma unroll
-                        for (int w = 0; w < PARTS; ++w)
-                            *reinterpret_cast<uint32_t *>(dst + w * S::kPart) = part[w];
-                    }
+                    for (int w = 0; w < PARTS; ++w)
+                        *reinterpret_cast<uint32_t *>(dst + w * S::kPart) = part[w];
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -457,32 +440,37 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     if (!ok && tid == 0) atomicAdd(&g_grad_timeouts, 1u);
     allow_dependent_launch();
     if (ok && warp < kWorkerWarps) {
-        const int f = 32 * (warp & 3) + lane, colhalf = warp >> 2;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int quad = warp & 3, quarter = warp >> 2, f = 32 * quad + lane;
+#pragma unroll 1
+        for (int w = 0; w < 2; ++w) {
+            const int at = 64 * quarter + 32 * w, t = at / NT, col = at % NT;
+            if (t >= mt) break;
+            uint32_t sum[32];
+            tmem_ld32(tmem + (uint32_t(32 * quad) << 16) + uint32_t(kAccCols + at), sum);
+            float *dst = p.partial +
+                         (((int64_t(ny) * p.tiles + tile0 + t) * p.parts_full + run) * NT + col) * 128 + f;
 #pragma unroll
-        for (int c = 0; c < kSumsPerThread; ++c) {
-            const int at = colhalf * kSumsPerThread + c, t = at / NT, col = at % NT;
-            if (t < mt && col < cols)
-                p.partial[(((int64_t(ny) * p.tiles + tile0 + t) * p.parts_full + run) * NT + col) * 128 +
-                          f] = sum[c];
+            for (int j = 0; j < 32; ++j)
+                if (col + j < cols) dst[j * 128] = __uint_as_float(sum[j]);
         }
-        if (sums_cols && int(group) < atoms) {
+        if (sums_cols) {
             // Rows of a warp, then the warps in order.
             if constexpr (kTma) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    colsum[e] += __shfl_xor_sync(kFullMask, colsum[e], 8);
+                for (int e = 0; e < 4; ++e) {
                     colsum[e] += __shfl_xor_sync(kFullMask, colsum[e], 16);
-                    if (lane < 8) colpart[warp][8 * lane + e] = colsum[e];
+                    if (lane < 16) colpart[warp][4 * lane + e] = colsum[e];
                 }
             } else {
                 colpart[warp][lane] = colsum[0];
                 colpart[warp][32 + lane] = colsum[1];
             }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (tid < 64 && 64 * int(group) + tid < cols) {
+            asm volatile("bar.sync 1, 512;" ::: "memory");
+            if (tid < 64 && 64 * own + tid < cols) {
                 float t = 0.0f;
                 for (int w = 0; w < kWorkerWarps; ++w) t += colpart[w][tid];
-                p.colsum[int64_t(run) * p.nt * NT + n0 + 64 * int(group) + tid] = t;
+                p.colsum[int64_t(run) * p.nt * NT + n0 + 64 * own + tid] = t;
             }
         }
     }
@@ -578,8 +566,9 @@ struct GradPlan {
 
 // NT: the widest tile that F fills and for which there are as many groups of feature tiles
 // as 64-column atoms to sum (each sums one); at most `most`. mt: all the tiles that fit
-// unless runs of rows get shorter than 8 stages, where fewer tiles and longer runs mean
-// less to add up: 2708 x 1433 x 64, fp32.
+// unless runs of rows get shorter than 256, where fewer tiles and longer runs mean
+// less to add up: 2708 x 1433 x 64, fp32. A stage costs a CTA about mt + 3 (the workers' time:
+// a tile of A, against dZ's parts and the barriers), by which the last group's runs are longer.
 GradPlan grad_plan(int64_t N, int K, int F, int most) {
     GradPlan g;
     g.tiles = (int64_t(K) + 127) / 128;
@@ -587,20 +576,23 @@ GradPlan grad_plan(int64_t N, int K, int F, int most) {
     for (int NT = 128; NT <= most; NT *= 2)
         if (F > NT / 2 && (g.tiles + kAccCols / NT - 1) / (kAccCols / NT) >= NT / 64) g.NT = NT;
     g.nt = int((int64_t(F) + g.NT - 1) / g.NT);
-    const int64_t stages = (N + kRows - 1) / kRows;
-    const int64_t longest = stages / 4 > 1 ? stages / 4 : 1;       // runs of 4 stages or more
-    auto runs = [&](int64_t mt) {
-        int64_t s = kGradCtas * mt / (g.tiles * g.nt);
-        s = s < longest ? s : longest;
-        return s > 1 ? s : 1;
+    const int64_t longest = N / 128 > 1 ? N / 128 : 1;             // runs of 128 rows or more
+    auto cut = [&](int mt) {
+        g.mt = mt;
+        g.groups = (g.tiles + mt - 1) / mt;
+        const int rest = int(g.tiles - (g.groups - 1) * mt);
+        const int64_t cost = (g.groups - 1) * (mt + 3) + rest + 3;
+        auto runs = [&](int tiles) {
+            int64_t s = int64_t(kGradCtas / g.nt) * (tiles + 3) / cost;
+            s = s < longest ? s : longest;
+            return int(s > 1 ? s : 1);
+        };
+        g.parts_last = runs(rest);
+        g.parts_full = g.groups > 1 ? runs(mt) : g.parts_last;
     };
-    g.mt = kAccCols / g.NT;
-    if (g.mt > g.tiles) g.mt = int(g.tiles);
-    while (g.mt > 1 && stages / runs(g.mt) < 8) g.mt = (g.mt + 1) / 2;
-    g.groups = (g.tiles + g.mt - 1) / g.mt;
-    g.parts_full = int(runs(g.mt));
-    g.parts_last = int(runs(g.tiles - (g.groups - 1) * g.mt));
-    if (g.groups == 1) g.parts_full = g.parts_last;
+    int mt = kAccCols / g.NT;
+    if (mt > g.tiles) mt = int(g.tiles);
+    for (cut(mt); mt > 1 && N / g.parts_full < 256; cut(mt)) mt = (mt + 1) / 2;
     g.partial_bytes = size_t(g.nt) * size_t(g.tiles) * size_t(g.parts_full) * size_t(g.NT) * 128 * 4;
     g.colsum_bytes = size_t(g.parts_full) * size_t(g.nt) * size_t(g.NT) * 4;
     return g;
@@ -634,14 +626,14 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// A map of `rows` rows of `width` elements, boxes of box x kRows.
+// A map of `rows` rows of `width` elements, boxes of box x box_rows.
 bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
-            int64_t rows, int64_t row_bytes, int box, bool swizzle) {
+            int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle) {
     const EncodeTiled fn = encoder();
     if (!fn) return false;
     const cuuint64_t dims[2] = {cuuint64_t(width), cuuint64_t(rows)};
     const cuuint64_t strides[1] = {cuuint64_t(row_bytes)};
-    const cuuint32_t boxes[2] = {cuuint32_t(box), cuuint32_t(kRows)};
+    const cuuint32_t boxes[2] = {cuuint32_t(box), cuuint32_t(box_rows)};
     const cuuint32_t steps[2] = {1, 1};
     return fn(map, type, 2, const_cast<void *>(base), dims, strides, boxes, steps,
               CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -732,16 +724,21 @@ extern "C" bigcn_status bigcn_checkpoint_weight_grad(
     }
 
     GradParams p;
-    const int64_t width = (int64_t(K) + 15) / 16 * 16;
-    if (!encode(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, false))
-        return BIGCN_ERR_CUDA;
     const CUtensorMapDataType type = dtype == BIGCN_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                      : dtype == BIGCN_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    // Tensor copies want rows that start on 16-byte boundaries.
+    // Tensor copies want rows that start on 16-byte boundaries. A bf16 dZ is copied as an operand,
+    // in stages of 64 rows (GradShape).
     const int64_t zrow = lddz * int64_t(es);
+    const bool direct = dtype == BIGCN_BF16;
     const bool tma = aligned_to(dZ, 16) && zrow % 16 == 0 &&
-                     encode(&p.z_map, type, dZ, F, N, zrow, 64, dtype == BIGCN_BF16);
+                     encode(&p.z_map, type, dZ, F, N, zrow, 64, direct ? 64 : 32, direct);
+    const int rows = tma && direct ? 64 : 32;
+    const int64_t width = (int64_t(K) + 15) / 16 * 16;
+    if (!encode(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, rows,
+                false))
+        return BIGCN_ERR_CUDA;
+    p.stages = (N + rows - 1) / rows;
     const GradPlan g = grad_plan(N, K, F, tma ? kMostTma : kMostLoaded);
     p.exps = exps;
     p.lde = lde;

@@ -13,22 +13,20 @@
 
 namespace bigcn {
 
-// A tile is built of atoms of 64 columns (128 bytes) by kAtomRows contraction rows, one
+// A tile is built of atoms of 64 columns (128 bytes) by the contraction rows of a stage, one
 // atom after the other; within an atom 8 rows of 128 bytes make a swizzle unit.
-constexpr int kAtomRows = 32;
-constexpr int kAtomBytes = kAtomRows * 128;
 
 // Byte offset of the 16-byte chunk c (8 columns) of row r in an atom.
 __device__ __forceinline__ uint32_t atom_offset(int r, int c) {
     return uint32_t(r * 128 + ((c ^ (r & 7)) << 4));
 }
 
-// Shared-memory matrix descriptor, MN-major, 128B swizzle: atoms kAtomBytes apart along
-// the columns (leading byte offset), groups of 8 rows 1024 bytes apart along the
+// Shared-memory matrix descriptor, MN-major, 128B swizzle: atoms of kRows rows one after the
+// other along the columns (leading byte offset), groups of 8 rows 1024 bytes apart along the
 // contraction (stride byte offset), descriptor version 1.
-__device__ __forceinline__ uint64_t atom_desc(uint32_t saddr) {
+template <int kRows> __device__ __forceinline__ uint64_t atom_desc(uint32_t saddr) {
     uint64_t d = uint64_t((saddr >> 4) & 0x3FFFu);
-    d |= uint64_t(kAtomBytes >> 4) << 16;
+    d |= uint64_t((kRows * 128) >> 4) << 16;
     d |= uint64_t(1024 >> 4) << 32;
     d |= uint64_t(1) << 46;
     d |= uint64_t(2) << 61;
@@ -56,18 +54,36 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
         : "memory");
 }
 
+// 32 columns of this warp's lanes, loaded when it returns (one statement with the wait, so that
+// nothing that uses them is moved between).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
           "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
           "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
           "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
           "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 // Two values as three bf16 parts each, in pairs: the upper halves of v, of what is left
