@@ -15,10 +15,11 @@
 // fp16 dZ) by tensor copies into a ring of raw slots, from which the workers expand it.
 //
 // Roles of a CTA (576 threads): warps 0-15, the workers, turn raw slots into operand
-// stages and take the running sums. Warp 16 copies, warp 17 issues the MMAs. They meet
-// on mbarriers only:
+// stages, in two teams that take every second stage each (one's latencies pass under the
+// other's instructions), and take the running sums. Warp 16 copies, warp 17 issues the MMAs.
+// They meet on mbarriers only:
 //   loaded[slot]   a slot's copies have landed         freed[slot]   it may be refilled
-//   filled[stage]  the workers have written a stage    used[stage]   its MMAs are done
+//   filled[stage]  a team has written a stage          used[stage]   its MMAs are done
 //   summed         a block's MMAs are done             drained       its sums were taken
 //
 // Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
@@ -47,6 +48,8 @@ namespace {
 constexpr int kGradCtas = 152;          // SMs of the card
 constexpr int kWorkers = 512;
 constexpr int kWorkerWarps = kWorkers / 32;
+constexpr int kTeams = 2;               // of workers, which take stages in turn
+constexpr int kTeamWarps = kWorkerWarps / kTeams;
 constexpr int kCopyWarp = kWorkerWarps, kMmaWarp = kWorkerWarps + 1;
 constexpr int kGradThreads = kWorkers + 64;
 constexpr int kAccCols = 256;           // accumulator columns; as many of running sums
@@ -78,7 +81,7 @@ struct GradShape {
     static constexpr int kSmem = 1024 + kStages * kOp + kSlots * kSlot;
     // About 40 accumulating MMAs (kRows / 16 per stage and part) between two drains.
     static constexpr int kDrain = kDirect ? 10 : PARTS == 1 ? 20 : PARTS == 2 ? 10 : 7;
-    static_assert(kSlots >= 2, "shared memory per CTA");
+    static_assert(kSlots >= kTeams && kStages >= kTeams, "shared memory per CTA");
 };
 
 struct GradParams {
@@ -124,7 +127,7 @@ __device__ __forceinline__ void expand4(uint32_t w, __nv_bfloat162 factor, uint3
 
 // 2^(b - 127) in both halves, as unpack_factor.
 __device__ __forceinline__ __nv_bfloat162 bf16_factor(uint32_t b) {
-    const uint32_t f = b == kNanByte ? 0x7FC0u : b << 7, f2 = f | (f << 16);
+    const uint32_t f2 = b == kNanByte ? 0x7FC07FC0u : b * 0x00800080u;
     return *reinterpret_cast<const __nv_bfloat162 *>(&f2);
 }
 
@@ -182,10 +185,10 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     if (tid == 0) {
         for (int s = 0; s < kSlots; ++s) {
             mbar_init(smem_addr(&loaded[s]), 33);       // the copy warp's lanes, and its bytes
-            mbar_init(smem_addr(&freed[s]), S::kDirect ? 1 : kWorkerWarps);
+            mbar_init(smem_addr(&freed[s]), S::kDirect ? 1 : kTeamWarps);
         }
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&filled[s]), kWorkerWarps);
+            mbar_init(smem_addr(&filled[s]), kTeamWarps);
             mbar_init(smem_addr(&used[s]), 1);
         }
         mbar_init(smem_addr(&summed), 1);
@@ -282,20 +285,21 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
         }
         __syncwarp();
     } else {
-        // Worker: row `row` of 32 of a stage, 8 features 8 c .. of each tile, 4 columns 4 c .. of
-        // each atom. Loaded without tensor copies, dZ is taken two rows a warp, a column per
-        // lane, a stage ahead.
-        const int row = tid >> 4, c = tid & 15;
+        // Worker of the team that takes every second stage: of 16 rows in turn row `row`, 8
+        // features 8 c .. of each tile, 4 columns 4 c .. of each atom. Loaded without tensor
+        // copies, dZ is taken four rows a warp, a column per lane, the team's next stage ahead.
+        const int team = warp / kTeamWarps, tw = warp % kTeamWarps;
+        const int row = (tid >> 4) & 15, c = tid & 15;
         const int quad = warp & 3, quarter = warp >> 2;
         constexpr int kLoadCols = kTma ? 1 : NT / 32;
-        float z[kLoadCols][2];
+        float z[kLoadCols][4];
         auto load = [&](int st) {
             if constexpr (!kTma) {
-                const int64_t i = (st0 + st) * kRows + 2 * warp;
+                const int64_t i = (st0 + st) * kRows + 4 * tw;
 #pragma unroll
                 for (int q = 0; q < kLoadCols; ++q)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
+                    for (int e = 0; e < 4; ++e)
                         z[q][e] = st < n && n0 + 32 * q < p.F ? dz_at<T>(p, i + e, n0 + 32 * q + lane)
                                                               : 0.0f;
             }
@@ -325,49 +329,57 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             if (lane == 0) mbar_arrive(smem_addr(&drained));
             return true;
         };
-        int taken = 0;                  // blocks drained
+        int taken = 0, next_drain = kDrain;         // blocks drained, the next one's end
         bool ok = true;
-        load(0);
+        load(team);
+        // Slot and stage of st, and the parities of their phases.
+        int s = team % kSlots, o = team % kStages;
+        uint32_t sp = uint32_t(team / kSlots) & 1u, op_parity = uint32_t(team / kStages) & 1u;
+        const uint32_t a_at = uint32_t((c >> 3) * kAtom) + atom_offset(row, c & 7);
+        const uint32_t b_at = atom_offset(row, c >> 1) + (c & 1) * 8;
 #pragma unroll 1
-        for (int st = 0; st < n; ++st) {
-            // A block is drained one stage after its end: its MMAs are done by then, and the
-            // next one's first stage is filled.
-            if (st > (taken + 1) * kDrain) {
+        for (int st = team; st < n; st += kTeams) {
+            // A block is drained a stage after its end: its MMAs are done by then, and the
+            // next one's first stage is filled or under way.
+            if (st > next_drain) {
                 ok = drain(taken);
                 if (!ok) break;
                 ++taken;
+                next_drain += kDrain;
             }
-            const int s = st % kSlots, o = st % kStages;
-            bool go = wait_unless(smem_addr(&loaded[s]), uint32_t(st / kSlots) & 1u, stopv);
-            if (st >= kStages)
-                go = go && wait_unless(smem_addr(&used[o]), uint32_t(st / kStages - 1) & 1u, stopv);
+            // (A stage's first use waits for the phase before the first, which is complete.)
+            bool go = wait_unless(smem_addr(&loaded[s]), sp, stopv);
+            go = go && wait_unless(smem_addr(&used[o]), op_parity ^ 1u, stopv);
             ok = __all_sync(kFullMask, go);
             if (!ok) break;
             const unsigned char *slot = mem + kSlot0 + s * S::kSlot;
             unsigned char *op = mem + o * S::kOp;
-            // A: 8 features of a row to a 16-byte chunk.
-            for (int t = 0; t < mt; ++t) {
+            // A: 8 features of a row to a 16-byte chunk. (16 rows on, a chunk is 2048 bytes on:
+            // the swizzle repeats every 8.)
 #pragma unroll
-                for (int h = 0; h < kRows / 32; ++h) {
-                    const int rr = row + 32 * h;
-                    const uint2 q = *reinterpret_cast<const uint2 *>(slot + S::kSlotZ +
-                                                                     (t * kRows + rr) * 128 + c * 8);
-                    const __nv_bfloat162 f = bf16_factor(
-                        slot[S::kSlotZ + S::kSlotQ + (t * kRows + rr) * 4 + (c >> 2)]);
+            for (int t = 0; t < S::kTiles; ++t) {
+                if (t >= mt) break;
+                const unsigned char *sq = slot + S::kSlotZ + t * kRows * 128 + row * 128 + c * 8;
+                const unsigned char *se =
+                    slot + S::kSlotZ + S::kSlotQ + (t * kRows + row) * 4 + (c >> 2);
+                unsigned char *dst = op + 2 * t * kAtom + a_at;
+#pragma unroll
+                for (int h = 0; h < kRows / 16; ++h) {
+                    const uint2 q = *reinterpret_cast<const uint2 *>(sq + h * 2048);
+                    const __nv_bfloat162 f = bf16_factor(se[h * 64]);
                     uint4 v;
                     expand4(q.x, f, v.x, v.y);
                     expand4(q.y, f, v.z, v.w);
-                    *reinterpret_cast<uint4 *>(op + (2 * t + (c >> 3)) * kAtom +
-                                               atom_offset(rr, c & 7)) = v;
+                    *reinterpret_cast<uint4 *>(dst + h * 2048) = v;
                 }
             }
             // B: dZ's parts, and its columns' sums.
             if constexpr (S::kDirect) {
                 if (sums_cols)
 #pragma unroll
-                    for (int h = 0; h < kRows / 32; ++h) {
-                        const uint2 u = *reinterpret_cast<const uint2 *>(
-                            slot + own * kAtom + atom_offset(row + 32 * h, c >> 1) + (c & 1) * 8);
+                    for (int h = 0; h < kRows / 16; ++h) {
+                        const uint2 u =
+                            *reinterpret_cast<const uint2 *>(slot + own * kAtom + b_at + h * 2048);
                         const float2 f0 = bf16_pair(u.x), f1 = bf16_pair(u.y);
                         colsum[0] += f0.x;
                         colsum[1] += f0.y;
@@ -378,48 +390,55 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
 #pragma unroll
                 for (int a = 0; a < NT / 64; ++a) {
                     if (a >= atoms) break;
-                    float v[4];
-                    if constexpr (PARTS == 3) {
-                        const float4 x = *reinterpret_cast<const float4 *>(
-                            slot + (a * kRows + row) * 256 + c * 16);
-                        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-                    } else {
-                        const uint2 u = *reinterpret_cast<const uint2 *>(
-                            slot + (a * kRows + row) * 128 + c * 8);
-                        const float2 f0 = __half22float2(*reinterpret_cast<const __half2 *>(&u.x));
-                        const float2 f1 = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
-                        v[0] = f0.x, v[1] = f0.y, v[2] = f1.x, v[3] = f1.y;
+#pragma unroll
+                    for (int h = 0; h < kRows / 16; ++h) {
+                        float v[4];
+                        if constexpr (PARTS == 3) {
+                            const float4 x = *reinterpret_cast<const float4 *>(
+                                slot + (a * kRows + row) * 256 + c * 16 + h * 4096);
+                            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                        } else {
+                            const uint2 u = *reinterpret_cast<const uint2 *>(
+                                slot + (a * kRows + row) * 128 + c * 8 + h * 2048);
+                            const float2 f0 = __half22float2(*reinterpret_cast<const __half2 *>(&u.x));
+                            const float2 f1 = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
+                            v[0] = f0.x, v[1] = f0.y, v[2] = f1.x, v[3] = f1.y;
+                        }
+                        if (a == own)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) colsum[e] += v[e];
+                        uint32_t x[3], y[3];
+                        parts_of<PARTS>(v[0], v[1], x);
+                        parts_of<PARTS>(v[2], v[3], y);
+                        unsigned char *dst = op + S::kOpA + a * kAtom + b_at + h * 2048;
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q)
+                            *reinterpret_cast<uint2 *>(dst + q * S::kPart) = make_uint2(x[q], y[q]);
                     }
-                    if (a == own)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) colsum[e] += v[e];
-                    uint32_t x[3], y[3];
-                    parts_of<PARTS>(v[0], v[1], x);
-                    parts_of<PARTS>(v[2], v[3], y);
-                    unsigned char *dst =
-                        op + S::kOpA + a * kAtom + atom_offset(row, c >> 1) + (c & 1) * 8;
-#pragma unroll
-                    for (int q = 0; q < PARTS; ++q)
-                        *reinterpret_cast<uint2 *>(dst + q * S::kPart) = make_uint2(x[q], y[q]);
                 }
             } else {
 #pragma unroll
                 for (int q = 0; q < kLoadCols; ++q) {
                     if (q / 2 >= atoms) break;
-                    if (q / 2 == own) colsum[q % 2] += z[q][0] + z[q][1];
-                    // Neighbouring lanes exchange a row's value: the even one writes the pair
-                    // of columns of the first row, the odd one of the second.
+                    if (q / 2 == own)
+                        colsum[q % 2] += (z[q][0] + z[q][1]) + (z[q][2] + z[q][3]);
+                    // Neighbouring lanes exchange a row's value: the even one writes the pair of
+                    // columns of rows 0 and 2, the odd one of rows 1 and 3.
                     const bool odd = lane & 1;
-                    const float got = __shfl_xor_sync(kFullMask, odd ? z[q][0] : z[q][1], 1);
-                    uint32_t part[3];
-                    parts_of<PARTS>(odd ? got : z[q][0], odd ? z[q][1] : got, part);
                     const int col = 32 * (q % 2) + (lane & ~1);
-                    unsigned char *dst = op + S::kOpA + (q / 2) * kAtom +
-                                         atom_offset(2 * warp + (odd ? 1 : 0), col >> 3) +
-                                         (col & 7) * 2;
 #pragma unroll
-                    for (int w = 0; w < PARTS; ++w)
-                        *reinterpret_cast<uint32_t *>(dst + w * S::kPart) = part[w];
+                    for (int e = 0; e < 4; e += 2) {
+                        const float got =
+                            __shfl_xor_sync(kFullMask, odd ? z[q][e] : z[q][e + 1], 1);
+                        uint32_t part[3];
+                        parts_of<PARTS>(odd ? got : z[q][e], odd ? z[q][e + 1] : got, part);
+                        unsigned char *dst = op + S::kOpA + (q / 2) * kAtom +
+                                             atom_offset(4 * tw + e + (odd ? 1 : 0), col >> 3) +
+                                             (col & 7) * 2;
+#pragma unroll
+                        for (int w = 0; w < PARTS; ++w)
+                            *reinterpret_cast<uint32_t *>(dst + w * S::kPart) = part[w];
+                    }
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -428,7 +447,11 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                 if (!S::kDirect) mbar_arrive(smem_addr(&freed[s]));
                 mbar_arrive(smem_addr(&filled[o]));
             }
-            load(st + 1);
+            load(st + kTeams);
+            s += kTeams;
+            if (s >= kSlots) s -= kSlots, sp ^= 1u;
+            o += kTeams;
+            if (o >= kStages) o -= kStages, op_parity ^= 1u;
         }
         for (; ok && taken * kDrain < n; ++taken) ok = drain(taken);
         if (!ok) *stopv = 1u;
