@@ -24,7 +24,7 @@
 //
 // Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
 // result per accumulating MMA, always towards 0; 1080 MMAs gave 2.2e-5), so an accumulator
-// takes kDrain stages, about 40 MMAs (8e-7), and is then added, in fp32, to the running sums:
+// takes kDrain stages, 48 or 64 MMAs (about 1e-6), and is then added, in fp32, to the running sums:
 // 256 accumulator columns of tensor memory and 256 of sums. (Sums in registers, with two
 // accumulators in turn, left room for 8 worker warps: 236 us at 232,965 x 602 x 128 fp32, the
 // workers' instructions at 1.7 a cycle being the limit.)
@@ -79,8 +79,9 @@ struct GradShape {
     static constexpr int kFit = (kSmemMost - kStages * kOp) / kSlot;
     static constexpr int kSlots = kFit < 8 ? kFit : 8;
     static constexpr int kSmem = 1024 + kStages * kOp + kSlots * kSlot;
-    // About 40 accumulating MMAs (kRows / 16 per stage and part) between two drains.
-    static constexpr int kDrain = kDirect ? 10 : PARTS == 1 ? 20 : PARTS == 2 ? 10 : 7;
+    // 48 (64 where there are no parts) accumulating MMAs, kRows / 16 per stage and part, between
+    // two drains.
+    static constexpr int kDrain = kDirect ? 16 : PARTS == 1 ? 24 : PARTS == 2 ? 12 : 8;
     static_assert(kSlots >= kTeams && kStages >= kTeams, "shared memory per CTA");
 };
 
