@@ -7,8 +7,9 @@ namespace {
 constexpr int kCkThreads = 256;
 
 // Both directions lay a row over `tpr` threads (a power of two, 8 to 256) in pieces of 16
-// bytes of X, as layer norm does (norm.cuh). A thread takes four pieces, J of a row by R rows,
-// all loaded before the first is used; a row longer than tpr J pieces goes over several blocks.
+// bytes of X, as layer norm does (norm.cuh). A thread takes three or four pieces, J of
+// a row by R rows, all loaded before the first is used (eight to unpack: 616 -> 635 us for both at
+// 2^20 x 512 bf16); a row longer than tpr J pieces goes over several blocks.
 // Bound by memory.
 template <int V, int J, int R>
 struct Place {
@@ -36,7 +37,7 @@ struct CkArgs {
     int64_t lde;
     const float *gamma;
     const float *beta;
-    bool aligned;            // gamma and beta to 16 bytes
+    bool aligned;            // gamma and beta to 32 bytes
 };
 
 template <typename T, int A, int J, int R>
@@ -123,23 +124,28 @@ unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
     }
 }
 
-// Threads of a row and the call's grid: the fewest threads (8, or more) that hold a row in at
-// most four pieces, else all 256 and several blocks.
+template <typename T, int A, int J, int R>
+void launch_pieces(const CkArgs &a, bool pack, int tpr, unsigned parts, cudaStream_t s) {
+    const int64_t rows = kCkThreads / tpr * R;
+    const unsigned blocks = unsigned((a.N + rows - 1) / rows * parts);
+    if (pack) pack_kernel<T, A, J, R><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    else unpack_kernel<T, A, J, R><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+}
+
+// The fewest threads (8, or more) that hold a row in at most four pieces, else all 256 and
+// several blocks a row.
 template <typename T, int A>
 void launch_checkpoint_rows(const CkArgs &a, bool pack, cudaStream_t s) {
     const int64_t pieces = (int64_t(a.K) + kPiece<T> - 1) / kPiece<T>;
     int tpr = 8;
     while (tpr < kCkThreads && int64_t(tpr) * 4 < pieces) tpr *= 2;
-    const int J = pieces <= tpr ? 1 : pieces <= 2 * tpr ? 2 : 4;
-    const unsigned parts = unsigned((pieces + int64_t(tpr) * J - 1) / (int64_t(tpr) * J));
-    const int64_t rows = kCkThreads / tpr * (4 / J);
-    const unsigned blocks = unsigned((a.N + rows - 1) / rows * parts);
-    if (J == 1 && pack) pack_kernel<T, A, 1, 4><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
-    else if (J == 2 && pack) pack_kernel<T, A, 2, 2><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
-    else if (pack) pack_kernel<T, A, 4, 1><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
-    else if (J == 1) unpack_kernel<T, A, 1, 4><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
-    else if (J == 2) unpack_kernel<T, A, 2, 2><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
-    else unpack_kernel<T, A, 4, 1><<<blocks, kCkThreads, 0, s>>>(a, tpr, parts);
+    const int64_t need = (pieces + tpr - 1) / tpr;
+    const int J = need < 4 ? int(need) : 4;
+    const unsigned parts = unsigned((need + J - 1) / J);
+    if (J == 1) launch_pieces<T, A, 1, 4>(a, pack, tpr, parts, s);
+    else if (J == 2) launch_pieces<T, A, 2, 2>(a, pack, tpr, parts, s);
+    else if (J == 3) launch_pieces<T, A, 3, 1>(a, pack, tpr, parts, s);
+    else launch_pieces<T, A, 4, 1>(a, pack, tpr, parts, s);
 }
 
 template <typename T>
@@ -157,7 +163,7 @@ void launch_checkpoint(int32_t dtype, void *X, int64_t N, int K, int64_t ldx, in
                        int64_t ldq, uint8_t *exps, int64_t lde, const float *gamma,
                        const float *beta, bool pack, cudaStream_t s) {
     const CkArgs a{X,    N,   K,     ldx,  q, ldq, exps, lde, gamma, beta,
-                   aligned_to(gamma, 16) && aligned_to(beta, 16)};
+                   aligned_to(gamma, 32) && aligned_to(beta, 32)};
     if (dtype == BIGCN_F32) launch_type<float>(a, pack, s);
     else if (dtype == BIGCN_BF16) launch_type<__nv_bfloat16>(a, pack, s);
     else launch_type<__half>(a, pack, s);

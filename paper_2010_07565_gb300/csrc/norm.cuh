@@ -36,11 +36,13 @@ template <int A> __device__ __forceinline__ uint4 load16(const void *p) {
         const uint32_t *q = static_cast<const uint32_t *>(p);
         return make_uint4(q[0], q[1], q[2], q[3]);
     } else {
-        const uint16_t *q = static_cast<const uint16_t *>(p);
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = uint32_t(q[2 * e]) | (uint32_t(q[2 * e + 1]) << 16);
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        // 2 bytes past a word: the words between, and a half at each end.
+        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) return load16<4>(p);
+        const uint16_t *h = static_cast<const uint16_t *>(p);
+        const uint32_t *q = reinterpret_cast<const uint32_t *>(h + 1);
+        const uint32_t e0 = h[0], x0 = q[0], x1 = q[1], x2 = q[2], e7 = h[7];
+        return make_uint4(e0 | (x0 << 16), __byte_perm(x0, x1, 0x5432), __byte_perm(x1, x2, 0x5432),
+                          (x2 >> 16) | (e7 << 16));
     }
 }
 template <int A> __device__ __forceinline__ void store16(void *p, uint4 v) {
@@ -49,17 +51,22 @@ template <int A> __device__ __forceinline__ void store16(void *p, uint4 v) {
     } else if constexpr (A == 8) {
         static_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
         static_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
-    } else {
+    } else if constexpr (A == 4) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (A == 4) {
-                static_cast<uint32_t *>(p)[e] = w[e];
-            } else {
-                static_cast<uint16_t *>(p)[2 * e] = uint16_t(w[e]);
-                static_cast<uint16_t *>(p)[2 * e + 1] = uint16_t(w[e] >> 16);
-            }
+        for (int e = 0; e < 4; ++e) static_cast<uint32_t *>(p)[e] = w[e];
+    } else {
+        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
+            store16<4>(p, v);
+            return;
         }
+        uint16_t *h = static_cast<uint16_t *>(p);
+        uint32_t *q = reinterpret_cast<uint32_t *>(h + 1);
+        h[0] = uint16_t(v.x);
+        q[0] = __byte_perm(v.x, v.y, 0x5432);
+        q[1] = __byte_perm(v.y, v.z, 0x5432);
+        q[2] = __byte_perm(v.z, v.w, 0x5432);
+        h[7] = uint16_t(v.w >> 16);
     }
 }
 
@@ -145,16 +152,22 @@ template <int H> __device__ __forceinline__ void clear_from(float2 (&v)[H], int 
     }
 }
 
-// V entries of gamma or beta at p, of which n lie in the row; `aligned`: p to 16 bytes.
+// V entries of gamma or beta at p, of which n lie in the row; `aligned`: p to 32 bytes. Eight are
+// one load of 32 bytes: two of 16, 32 bytes apart between lanes, take twice the L1 cycles
+// (8191 x 8192 fp16: L1 at 82 %, 70 us). Loaded anew for every use: the compiler would keep
+// them across a loop over rows in registers that it then spills.
 template <int H>
 __device__ __forceinline__ void load_params(const float *p, bool aligned, int n, float2 (&v)[H]) {
     if (aligned && n >= 2 * H) {
-#pragma unroll
-        for (int w = 0; w < H / 2; ++w) {
-            const float4 f = __ldg(reinterpret_cast<const float4 *>(p) + w);
-            v[2 * w] = make_float2(f.x, f.y);
-            v[2 * w + 1] = make_float2(f.z, f.w);
-        }
+        if constexpr (H == 4)
+            asm volatile("ld.global.nc.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y), "=f"(v[2].x),
+                           "=f"(v[2].y), "=f"(v[3].x), "=f"(v[3].y)
+                         : "l"(p));
+        else
+            asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y)
+                         : "l"(p));
     } else {
 #pragma unroll
         for (int e = 0; e < H; ++e) {
@@ -165,8 +178,8 @@ __device__ __forceinline__ void load_params(const float *p, bool aligned, int n,
 }
 
 // What stands in for a gamma or a beta that is not given, read with a stride of 0.
-static __device__ __align__(16) const float kOnes[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-static __device__ __align__(16) const float kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+static __device__ __align__(32) const float kOnes[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+static __device__ __align__(32) const float kZeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 
 // The largest magnitude of a piece as bits (a NaN is larger than an infinity).
 template <int H> __device__ __forceinline__ uint32_t top_bits(const float2 (&v)[H]) {

@@ -139,34 +139,41 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
         } else {
             load(i, r);
         }
-        float2 g[J][H], h[J][H];        // gamma dy, xhat
+        // dy, xhat and gamma of piece j, n of its columns in the row, from what was read. gamma dy and
+        // xhat are kept from the sums to dx where the registers allow it (up to 16 columns a thread),
+        // else expanded twice. (Behind the row dy and gamma are 0 and xhat anything finite, or NaN with
+        // its row.)
+        constexpr bool kHold = J * V <= 16;
+        float2 gk[kHold ? J : 1][H], hk[kHold ? J : 1][H];
+        const float rstd = r.rstd;
+        auto take = [&](int j, int n, float2 (&d)[H], float2 (&h)[H], float2 (&m)[H]) {
+            unpack16<T>(r.dy[j], d);
+            if constexpr (kKept) {
+                dequantise_piece<H>(r.q[j], unpack_factor(r.b[j]), h);
+            } else {
+                unpack16<T>(r.x[j], h);
+#pragma unroll
+                for (int e = 0; e < H; ++e)
+                    h[e] = __fmul2_rn(__fadd2_rn(h[e], both(-r.mean)), both(rstd));
+            }
+            load_params(gamma + j * gstep, aligned, n, m);
+        };
         float2 s0 = both(0.0f), s1 = both(0.0f);
         if (kWarp || live) {
-            const float rstd = r.rstd;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int n = j < kFull ? V : left - j * step;
                 if (n <= 0) continue;
-                float2 d[H], m[H];
-                unpack16<T>(r.dy[j], d);
-                if constexpr (kKept) {
-                    dequantise_piece<H>(r.q[j], unpack_factor(r.b[j]), h[j]);
-                    // (The bytes behind the row may hold anything; dy is 0 there.)
-                    if (n < V) clear_from(h[j], n);
-                } else {
-                    unpack16<T>(r.x[j], h[j]);
-#pragma unroll
-                    for (int e = 0; e < H; ++e)
-                        h[j][e] = __fmul2_rn(__fadd2_rn(h[j][e], both(-r.mean)), both(rstd));
-                }
-                load_params(gamma + j * gstep, aligned, n, m);
+                float2 d[H], h[H], m[H];
+                take(j, n, d, h, m);
 #pragma unroll
                 for (int e = 0; e < H; ++e) {
-                    sg[j][e] = __ffma2_rn(d[e], h[j][e], sg[j][e]);
+                    sg[j][e] = __ffma2_rn(d[e], h[e], sg[j][e]);
                     sb[j][e] = __fadd2_rn(sb[j][e], d[e]);
-                    g[j][e] = __fmul2_rn(d[e], m[e]);
-                    s0 = __fadd2_rn(s0, g[j][e]);
-                    s1 = __ffma2_rn(g[j][e], h[j][e], s1);
+                    const float2 g = __fmul2_rn(d[e], m[e]);
+                    s0 = __fadd2_rn(s0, g);
+                    s1 = __ffma2_rn(g, h[e], s1);
+                    if constexpr (kHold) gk[j][e] = g, hk[j][e] = h[e];
                 }
             }
         }
@@ -176,17 +183,21 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
         row_sum<kWarp>(s, tpr, red[turn]);
         turn ^= 1;
         if (!kWarp && !live) continue;
-        const float2 c0 = both(-s[0] * inv_k), c1 = both(-s[1] * inv_k), rs = both(r.rstd);
+        const float2 c0 = both(-s[0] * inv_k), c1 = both(-s[1] * inv_k), rs = both(rstd);
         T *dx = static_cast<T *>(a.dX) + i * a.lddx + k0;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int n = j < kFull ? V : left - j * step;
             if (n <= 0) continue;
-            float2 o[H];
+            float2 d[H], h[H], m[H];
+            if constexpr (!kHold) take(j, n, d, h, m);
 #pragma unroll
-            for (int e = 0; e < H; ++e)
-                o[e] = __fmul2_rn(__ffma2_rn(h[j][e], c1, __fadd2_rn(g[j][e], c0)), rs);
-            store_piece<T, A>(dx + j * step, pack16<T>(o), n);
+            for (int e = 0; e < H; ++e) {
+                const float2 g = kHold ? gk[kHold ? j : 0][e] : __fmul2_rn(d[e], m[e]);
+                const float2 xh = kHold ? hk[kHold ? j : 0][e] : h[e];
+                d[e] = __fmul2_rn(__ffma2_rn(xh, c1, __fadd2_rn(g, c0)), rs);
+            }
+            store_piece<T, A>(dx + j * step, pack16<T>(d), n);
         }
     }
     allow_dependent_launch();
@@ -273,7 +284,7 @@ void launch_backward(BackwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
     const uint64_t where[] = {uint64_t(uintptr_t(a.dY)), uint64_t(a.lddy) * es,
                               uint64_t(uintptr_t(a.dX)), a.dX ? uint64_t(a.lddx) * es : 0,
                               uint64_t(uintptr_t(a.X)),  a.X ? uint64_t(a.ldx) * es : 0};
-    const bool aligned = aligned_to(a.gamma, 16);
+    const bool aligned = aligned_to(a.gamma, 32);
     const int A = alignment_of(where, 6);
     const bool done = A == 16  ? launch_aligned<T, 16>(a, aligned, dev, s)
                       : A == 8 ? launch_aligned<T, 8>(a, aligned, dev, s)

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
 // constant), else tpr threads'. Rows past N take part in the sums over threads and store
 // nothing.
 template <typename T, int A, int J, bool kKeep, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? (J * kPiece<T> <= 16 ? 4 : 3) : 2)
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 4 : 2)
 forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool aligned) {
     constexpr int V = kPiece<T>, H = V / 2, kFull = full_pieces(V, J);
     __shared__ float red[2][1][kMostRowThreads / 32];
@@ -93,73 +93,95 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
     const int K = a.K, k0 = t * V, step = tpr * V, left = K - k0;
     const float inv_k = 1.0f / float(K);
     const T *row = static_cast<const T *>(a.X) + (live ? i : 0) * a.ldx + k0;
-    float2 x[J][H];
+    // The row as it was read: 16-bit elements take half the registers that way, so that all
+    // loads are under way at once, and are expanded for each use.
+    uint4 w[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        if (j < kFull) w = load16<A>(row + j * step);
-        else if (left > j * step) w = load_piece<T, A>(row + j * step, left - j * step);
-        unpack16<T>(w, x[j]);
+        w[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (j < kFull) w[j] = load16<A>(row + j * step);
+        else if (left > j * step) w[j] = load_piece<T, A>(row + j * step, left - j * step);
     }
     float2 s2 = both(0.0f);
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
+        float2 x[H];
+        unpack16<T>(w[j], x);
 #pragma unroll
-        for (int e = 0; e < H; ++e) s2 = __fadd2_rn(s2, x[j][e]);
+        for (int e = 0; e < H; ++e) s2 = __fadd2_rn(s2, x[e]);
+    }
     float s[1] = {s2.x + s2.y};
     row_sum<kWarp>(s, tpr, red[0]);
     const float mean = s[0] * inv_k;
+    // x - mean of piece j, zeros past the row.
+    auto centred = [&](int j, float2 (&x)[H]) {
+        unpack16<T>(w[j], x);
+#pragma unroll
+        for (int e = 0; e < H; ++e) x[e] = __fadd2_rn(x[e], both(-mean));
+        if (j >= kFull && left < j * step + V) clear_from(x, left - j * step);
+    };
     s2 = both(0.0f);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
+        float2 x[H];
+        centred(j, x);
 #pragma unroll
-        for (int e = 0; e < H; ++e) x[j][e] = __fadd2_rn(x[j][e], both(-mean));
-        if (j >= kFull && left < j * step + V) clear_from(x[j], left - j * step);
-#pragma unroll
-        for (int e = 0; e < H; ++e) s2 = __ffma2_rn(x[j][e], x[j][e], s2);
+        for (int e = 0; e < H; ++e) s2 = __ffma2_rn(x[e], x[e], s2);
     }
     s[0] = s2.x + s2.y;
     row_sum<kWarp>(s, tpr, red[1]);
+    if (!kWarp && !kKeep && !live) return;      // (with a checkpoint lanes still meet below)
     const float rstd = 1.0f / sqrtf(s[0] * inv_k + a.eps);
     if (live && t == 0) {
         if (a.mean) a.mean[i] = mean;
         if (a.rstd) a.rstd[i] = rstd;
     }
     T *out = static_cast<T *>(a.Y) + i * a.ldy + k0;
+    int8_t *q = a.q + i * a.ldq + k0;
+    uint8_t *exps = a.exps + i * a.lde;
+    const int kq = (K + 15) / 16 * 16 - k0;
     const float *gamma = a.gamma ? a.gamma + k0 : kOnes, *beta = a.beta ? a.beta + k0 : kZeros;
     const int gstep = a.gamma ? step : 0, bstep = a.beta ? step : 0;
+    // Two pieces at a time, whose groups' maxima share a word.
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int n = j < kFull ? V : left - j * step;
+    for (int j0 = 0; j0 < J; j0 += 2) {
+        constexpr int kPair = J == 1 ? 1 : 2;
+        float2 x[kPair][H];
+        uint32_t own[kPair], top[kPair];
 #pragma unroll
-        for (int e = 0; e < H; ++e) x[j][e] = __fmul2_rn(x[j][e], both(rstd));
-        if (n <= 0 || (!kWarp && !live)) continue;
-        float2 g[H], b[H], y[H];
-        load_params(gamma + j * gstep, aligned, n, g);
-        load_params(beta + j * bstep, aligned, n, b);
+        for (int u = 0; u < kPair; ++u) {
+            own[u] = 0u;
+            if (j0 + u >= J) continue;
+            const int j = j0 + u, n = j < kFull ? V : left - j * step;
+            centred(j, x[u]);
 #pragma unroll
-        for (int e = 0; e < H; ++e) y[e] = __ffma2_rn(x[j][e], g[e], b[e]);
-        store_piece<T, A>(out + j * step, pack16<T>(y), n);
+            for (int e = 0; e < H; ++e) x[u][e] = __fmul2_rn(x[u][e], both(rstd));
+            if (kKeep) own[u] = top_bits(x[u]);
+            if (n > 0 && (kWarp || live)) {
+                float2 g[H], b[H], y[H];
+                load_params(gamma + j * gstep, aligned, n, g);
+                load_params(beta + j * bstep, aligned, n, b);
+#pragma unroll
+                for (int e = 0; e < H; ++e) y[e] = __ffma2_rn(x[u][e], g[e], b[e]);
+                store_piece<T, A>(out + j * step, pack16<T>(y), n);
+            }
+        }
+        if constexpr (kKeep) {
+            group_tops<32 / V>(own, top);
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) {
+                const int j = j0 + u;
+                if (j >= J || (!kWarp && !live) || (j >= kFull && j * step >= kq)) continue;
+                const uint32_t b = scale_byte(top[u]);
+                *reinterpret_cast<QPiece<H> *>(q + j * step) = quantise_piece(x[u], pack_factor(b));
+                if ((t & (32 / V - 1)) == 0 && j * step < left)
+                    exps[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
+            }
+        }
     }
     if constexpr (kKeep) {
-        uint32_t own[J], top[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) own[j] = top_bits(x[j]);
-        group_tops<32 / V>(own, top);
-        if (!kWarp && !live) return;
-        int8_t *q = a.q + i * a.ldq + k0;
-        uint8_t *exps = a.exps + i * a.lde;
-        const int kq = (K + 15) / 16 * 16 - k0;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (j >= kFull && j * step >= kq) break;
-            const uint32_t b = scale_byte(top[j]);
-            *reinterpret_cast<QPiece<H> *>(q + j * step) = quantise_piece(x[j], pack_factor(b));
-            if ((t & (32 / V - 1)) == 0 && j * step < left)
-                exps[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
-        }
         const int groups = int(checkpoint_groups(K));
-        if (groups + t < (groups + 3) / 4 * 4) exps[groups + t] = 0;
+        if (live && groups + t < (groups + 3) / 4 * 4) exps[groups + t] = 0;
     }
 }
 
@@ -197,7 +219,7 @@ void launch_forward(const ForwardArgs &a, const DeviceInfo &dev, cudaStream_t s)
     const uint64_t es = sizeof(T);
     const uint64_t rows[] = {uint64_t(uintptr_t(a.X)), uint64_t(a.ldx) * es, uint64_t(uintptr_t(a.Y)),
                              uint64_t(a.ldy) * es};
-    const bool aligned = aligned_to(a.gamma, 16) && aligned_to(a.beta, 16);
+    const bool aligned = aligned_to(a.gamma, 32) && aligned_to(a.beta, 32);
     const int A = alignment_of(rows, 4);
     const bool done = A == 16  ? launch_aligned<T, 16>(a, aligned, dev, s)
                       : A == 8 ? launch_aligned<T, 8>(a, aligned, dev, s)
