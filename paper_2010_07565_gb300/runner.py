@@ -11,6 +11,10 @@ aggregation fused with layer 2's pack and GEMM; layer-2 aggregation).
 (pack_rows, pack_weights, xnor_gemm_degscaled, spmm_prescaled per layer),
 keeping every intermediate in its own buffer, for step-by-step checks.
 The output is the logits (no softmax: Eq. 2 belongs to training).
+
+:class:`NormedLayer` is one layer in training whose features stay real (only the weights
+binarized) and whose input rows are normalised: layer norm, product, aggregation and their
+gradients, with the normalised rows kept in 8 bits in between.
 """
 from __future__ import annotations
 
@@ -125,3 +129,72 @@ class GCN2Forward:
         B.bigcn_xnor_gemm_degscaled(self.bits2, self.alpha2, self.wbits2, self.beta2,
                                     self.hidden, self.rowptr, self.Z2)
         B.bigcn_spmm_prescaled(self.rowptr, self.colidx, self.Z2, self.logits_steps)
+
+
+class NormedLayer:
+    """One layer in training, H = A~ (Y W~ + b) with Y = gamma xhat + beta the layer norm of X
+    and W~ = diag(beta_j) sign(W) (the ablation that binarizes the weights only, Sec. 6.3).
+
+    Between ``forward()`` and ``backward()`` it keeps xhat's 8-bit checkpoint and each row's
+    rstd: N (K + K/32 + 4) bytes in place of the 4 N K of Y, which the next layer may overwrite.
+    The one checkpoint serves both gradients that need the features:
+
+        G   = A~ dH                                       (the CSR is symmetric)
+        dWb = dL/dW~ = Y^T G,   db = sum_i G_i            (Algorithm 1's dL/dW~ with real features)
+        dY  = G W~^T
+        dX, dgamma, dbeta                                 the norm's gradients from dY
+
+    ``weight_gradient()`` takes dWb through the sign (Eq. bp-W)."""
+
+    def __init__(self, N: int, K: int, F: int, device, eps: float = 1e-5):
+        self.N, self.K, self.F, self.eps = N, K, F, eps
+        self.device = torch.device(device)
+        f32, i64 = torch.float32, torch.int64
+        e = lambda *shape, dtype=f32: torch.empty(shape, dtype=dtype, device=self.device)
+        # parameters
+        self.W, self.b = e(K, F), torch.zeros(F, device=self.device)
+        self.gamma, self.beta = torch.ones(K, device=self.device), torch.zeros(K, device=self.device)
+        # kept from forward to backward
+        self.q, self.exps = B.checkpoint_buffers(N, K, self.device)
+        self.rstd = e(N)
+        self.w_bits, self.w_scale = e(F, B.words_for(K), dtype=i64), e(F)
+        # scratch: free for others between calls
+        self.Y, self.Z, self.H = e(N, K), e(N, F), e(N, F)
+        # gradients
+        self.G, self.dY, self.dX = self.Z, self.Y, e(N, K)
+        self.dWb, self.db = e(K, F), e(F)
+        self.dgamma, self.dbeta = e(K), e(K)
+        self.w_rows, self.w_rows_scale = e(K, B.words_for(F), dtype=i64), e(K)
+        self.one, self.zero = torch.ones(K, device=self.device), torch.zeros(F, device=self.device)
+        need = max(B.bigcn_layer_norm_backward_workspace_bytes(N, K),
+                   B.bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F))
+        self.workspace = e(max(need, 1), dtype=torch.uint8)
+
+    def forward(self, X, rowptr, colidx):
+        """H from X (N x K fp32); enqueued on the current stream."""
+        B.bigcn_layer_norm_forward(X, self.gamma, self.beta, self.eps, self.Y, rstd=self.rstd,
+                                   q=self.q, exps=self.exps)
+        B.bigcn_pack_weights(self.W, self.w_bits, self.w_scale)
+        B.bigcn_real_binary_gemm(self.Y, None, None, self.w_bits, self.w_scale, self.Z)
+        self.Z += self.b
+        B.bigcn_spmm_norm(rowptr, colidx, self.Z, self.H)
+        return self.H
+
+    def backward(self, dH, rowptr, colidx):
+        """The gradients (dWb, db, dgamma, dbeta, dX) from dH = dL/dH (N x F)."""
+        B.bigcn_spmm_norm(rowptr, colidx, dH, self.G)
+        B.bigcn_checkpoint_weight_grad(self.q, self.exps, self.G, self.workspace, self.dWb,
+                                       gamma=self.gamma, beta=self.beta, db=self.db)
+        # dY = (G diag(beta_j)) sign(W)^T: W packed row by row over its F columns.
+        B.bigcn_pack_rows(self.W, None, None, self.w_rows, self.w_rows_scale)
+        B.bigcn_real_binary_gemm(self.G, self.w_scale, self.zero, self.w_rows, self.one, self.dY)
+        B.bigcn_layer_norm_backward(self.dY, self.gamma, self.rstd, self.workspace, q=self.q,
+                                    exps=self.exps, dX=self.dX, dgamma=self.dgamma,
+                                    dbeta=self.dbeta)
+        return self.dWb, self.db, self.dgamma, self.dbeta, self.dX
+
+    def weight_gradient(self):
+        """Eq. bp-W of dWb: sign(W) times the column means of dWb sign(W), and beta_j dWb where
+        |W| < 1 (the straight-through estimator of sign)."""
+        sign = torch.where(self.W >= 0, 1.0, -1.0)
+        return sign * (self.dWb * sign).mean(0) + self.w_scale * self.dWb * (self.W.abs() < 1)
