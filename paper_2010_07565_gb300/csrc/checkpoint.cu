@@ -48,15 +48,16 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
     const int K = a.K, left = K - at.k0;
     uint4 w[R][J];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        const T *row = static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0;
+        const int place = place_of(row, tpr < 32);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             w[r][j] = make_uint4(0u, 0u, 0u, 0u);
             if (at.i[r] < a.N && left > j * at.step)
-                w[r][j] = load_piece<T, A>(static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0 +
-                                               j * at.step,
-                                           left - j * at.step);
+                w[r][j] = load_piece<T, A>(row + j * at.step, left - j * at.step, place);
         }
+    }
     // Past K a piece is zeros and so is its q.
     const int kq = (K + 15) / 16 * 16 - at.k0;
 #pragma unroll
@@ -119,7 +120,8 @@ unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
 #pragma unroll
                 for (int e = 0; e < H; ++e)
                     v[e] = __ffma2_rn(v[e], a.gamma ? g[e] : both(1.0f), a.beta ? c[e] : both(0.0f));
-            store_piece<T, A>(static_cast<T *>(a.X) + at.i[r] * a.ldx + k, pack16<T>(v), n);
+            T *out = static_cast<T *>(a.X) + at.i[r] * a.ldx + k;
+            store_piece<T, A>(out, pack16<T>(v), n, place_of(out, tpr < 32));
         }
     }
 }

@@ -25,19 +25,34 @@ constexpr int kMostRowThreads = 512;
 template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 
 // ---- 16 bytes of a row --------------------------------------------------------------------
-template <int A> __device__ __forceinline__ uint4 load16(const void *p) {
+// A row that is aligned to A bytes lies at one of 16 / A places of 16 bytes, the same for all its
+// pieces: each place has its own accesses, the widest that it allows, by a branch that the row's
+// threads take together. Where a warp holds several rows these may lie at different places:
+// kMixed, by accesses that suit all. (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 ->
+// 315 us, backward 305 -> 253; rows of 55 columns, four a warp, 37 us, by places 51.)
+constexpr int kMixed = 1;
+__device__ __forceinline__ int place_of(const void *row, bool mixed) {
+    const int at = int(reinterpret_cast<uintptr_t>(row) & 15);
+    return mixed ? kMixed : (at & 2) ? 2 : (at & 4) ? 4 : at;
+}
+template <int A> __device__ __forceinline__ uint4 load16(const void *p, int place) {
     if constexpr (A == 16) {
         return *static_cast<const uint4 *>(p);
     } else if constexpr (A == 8) {
+        if (place == 0) return load16<16>(p, 0);
         const uint2 *q = static_cast<const uint2 *>(p);
         const uint2 a = q[0], b = q[1];
         return make_uint4(a.x, a.y, b.x, b.y);
     } else if constexpr (A == 4) {
+        if (place == 0 || place == 8) return load16<8>(p, place);
         const uint32_t *q = static_cast<const uint32_t *>(p);
-        return make_uint4(q[0], q[1], q[2], q[3]);
+        if (place == kMixed) return make_uint4(q[0], q[1], q[2], q[3]);
+        const uint2 m = *reinterpret_cast<const uint2 *>(q + 1);
+        return make_uint4(q[0], m.x, m.y, q[3]);
     } else {
         // 2 bytes past a word: the words between, and a half at each end.
-        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) return load16<4>(p);
+        if (place == kMixed ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : place != 2)
+            return load16<4>(p, place);
         const uint16_t *h = static_cast<const uint16_t *>(p);
         const uint32_t *q = reinterpret_cast<const uint32_t *>(h + 1);
         const uint32_t e0 = h[0], x0 = q[0], x1 = q[1], x2 = q[2], e7 = h[7];
@@ -45,19 +60,33 @@ template <int A> __device__ __forceinline__ uint4 load16(const void *p) {
                           (x2 >> 16) | (e7 << 16));
     }
 }
-template <int A> __device__ __forceinline__ void store16(void *p, uint4 v) {
+template <int A> __device__ __forceinline__ void store16(void *p, uint4 v, int place) {
     if constexpr (A == 16) {
         *static_cast<uint4 *>(p) = v;
     } else if constexpr (A == 8) {
-        static_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
-        static_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
+        if (place == 0) {
+            store16<16>(p, v, 0);
+        } else {
+            static_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
+            static_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
+        }
     } else if constexpr (A == 4) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) static_cast<uint32_t *>(p)[e] = w[e];
+        uint32_t *q = static_cast<uint32_t *>(p);
+        if (place == 0 || place == 8) {
+            store16<8>(p, v, place);
+        } else if (place == kMixed) {
+            q[0] = v.x;
+            q[1] = v.y;
+            q[2] = v.z;
+            q[3] = v.w;
+        } else {
+            q[0] = v.x;
+            *reinterpret_cast<uint2 *>(q + 1) = make_uint2(v.y, v.z);
+            q[3] = v.w;
+        }
     } else {
-        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
-            store16<4>(p, v);
+        if (place == kMixed ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : place != 2) {
+            store16<4>(p, v, place);
             return;
         }
         uint16_t *h = static_cast<uint16_t *>(p);
@@ -91,11 +120,13 @@ template <typename T> __device__ __forceinline__ void store_some(T *p, uint4 v, 
             else reinterpret_cast<uint16_t *>(p)[e] = uint16_t(w[e / 2] >> (16 * (e % 2)));
         }
 }
-template <typename T, int A> __device__ __forceinline__ uint4 load_piece(const T *p, int n) {
-    return n >= kPiece<T> ? load16<A>(p) : load_some(p, n);
+template <typename T, int A>
+__device__ __forceinline__ uint4 load_piece(const T *p, int n, int place) {
+    return n >= kPiece<T> ? load16<A>(p, place) : load_some(p, n);
 }
-template <typename T, int A> __device__ __forceinline__ void store_piece(T *p, uint4 v, int n) {
-    if (n >= kPiece<T>) store16<A>(p, v);
+template <typename T, int A>
+__device__ __forceinline__ void store_piece(T *p, uint4 v, int n, int place) {
+    if (n >= kPiece<T>) store16<A>(p, v, place);
     else store_some(p, v, n);
 }
 
