@@ -603,7 +603,7 @@ typedef enum bigcn_dtype {
 int32_t bigcn_checkpoint_groups(int32_t K);
 
 /* X (N x K, row stride ldx >= K, `dtype` a bigcn_dtype) to its checkpoint.
- * 0 <= N < 2^31, 1 <= K; q and exps must not overlap each other or X. */
+ * 0 <= N < 2^31, 1 <= K <= 2^30; q and exps must not overlap each other or X. */
 bigcn_status bigcn_checkpoint_pack(int32_t dtype, const void *X, int64_t N, int32_t K, int64_t ldx,
                                    int8_t *q, int64_t ldq, uint8_t *exps, int64_t lde,
                                    void *stream);
@@ -627,7 +627,7 @@ bigcn_status bigcn_checkpoint_unpack(int32_t dtype, const int8_t *q, int64_t ldq
  *        row divides by zero: that row is NaN).
  * mean, rstd   N fp32 each, each nullable: the backward's inputs.
  * q, exps (nullable, both or neither)   receive the checkpoint of xhat.
- * 0 <= N < 2^31, 1 <= K. No output may overlap another or an input.
+ * 0 <= N < 2^31, 1 <= K <= 2^30. No output may overlap another or an input.
  */
 bigcn_status bigcn_layer_norm_forward(int32_t dtype, const void *X, int64_t N, int32_t K,
                                       int64_t ldx, const float *gamma, const float *beta,
@@ -683,7 +683,7 @@ size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_
  * are fp32, over runs of rows added in a fixed order: deterministic on one device.
  * The tensor-core product waits on shared-memory barriers a bounded number of times:
  * where a wait runs out its part of dW is not written (bigcn_device_timeouts).
- * 0 <= N < 2^31, 1 <= K, 1 <= F. No output may overlap another or an input.
+ * 0 <= N < 2^31, 1 <= K, F <= 2^30. No output may overlap another or an input.
  */
 bigcn_status bigcn_checkpoint_weight_grad(int32_t dtype, const int8_t *q, int64_t ldq,
                                           const uint8_t *exps, int64_t lde, int64_t N, int32_t K,

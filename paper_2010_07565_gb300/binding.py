@@ -116,6 +116,8 @@ def library_path() -> str:
 def lib() -> ctypes.CDLL:
     """The loaded libbigcn.so. Raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = _build.LIB
@@ -139,7 +141,7 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         # torch.cuda.current_stream().cuda_stream without the Stream object (1 us against 4)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))

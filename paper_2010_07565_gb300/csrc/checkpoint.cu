@@ -184,7 +184,8 @@ extern "C" bigcn_status bigcn_checkpoint_pack(int32_t dtype, const void *X, int6
                                               int64_t ldx, int8_t *q, int64_t ldq, uint8_t *exps,
                                               int64_t lde, void *stream) {
     const size_t es = dtype_bytes(dtype);
-    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || ldx < K ||
+    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols ||
+        ldx < K ||
         !checkpoint_strides_ok(N, K, ldq, lde))
         return BIGCN_ERR_INVALID_ARG;
     if (N > 0 && N > kMaxElems / ldx) return BIGCN_ERR_INVALID_ARG;
@@ -208,7 +209,8 @@ extern "C" bigcn_status bigcn_checkpoint_unpack(int32_t dtype, const int8_t *q, 
                                                 int32_t K, const float *gamma, const float *beta,
                                                 void *X, int64_t ldx, void *stream) {
     const size_t es = dtype_bytes(dtype);
-    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || ldx < K ||
+    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols ||
+        ldx < K ||
         !checkpoint_strides_ok(N, K, ldq, lde))
         return BIGCN_ERR_INVALID_ARG;
     if (N > 0 && N > kMaxElems / ldx) return BIGCN_ERR_INVALID_ARG;

@@ -20,6 +20,7 @@ namespace bigcn {
 
 constexpr int kGroup = 32;              // columns per scale
 constexpr uint32_t kNanByte = 255;
+constexpr int kMaxCols = 1 << 30;       // of a row: 32-bit column indices step past its end
 
 __host__ __device__ constexpr int64_t checkpoint_groups(int64_t K) {
     return (K + kGroup - 1) / kGroup;

@@ -700,7 +700,8 @@ uint32_t take_grad_timeouts() {
 using namespace bigcn;
 
 extern "C" size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_t F) {
-    if (N < 0 || N > int64_t(INT32_MAX) || K < 1 || F < 1 || int64_t(K) > kMaxElems / (1 << 20) / F)
+    if (N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols || F < 1 || F > kMaxCols ||
+        int64_t(K) > kMaxElems / (1 << 20) / F)
         return 0;
     const size_t a = plan_bytes(grad_plan(N, K, F, kMostTma));
     const size_t b = plan_bytes(grad_plan(N, K, F, kMostLoaded));

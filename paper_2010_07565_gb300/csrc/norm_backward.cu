@@ -47,8 +47,10 @@ constexpr size_t kAlign = 256;
 using namespace bigcn;
 
 extern "C" size_t bigcn_layer_norm_backward_workspace_bytes(int64_t N, int32_t K) {
-    if (N < 0 || N > int64_t(INT32_MAX) || K < 1) return 0;
-    return (size_t(kMaxChunks) * 2 * size_t(K) * 4 + kAlign - 1) / kAlign * kAlign;
+    if (N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols) return 0;
+    // A chunk is a row or more.
+    const size_t chunks = N < kMaxChunks ? size_t(N > 0 ? N : 1) : size_t(kMaxChunks);
+    return (chunks * 2 * size_t(K) * 4 + kAlign - 1) / kAlign * kAlign;
 }
 
 extern "C" bigcn_status bigcn_layer_norm_backward(
@@ -57,7 +59,8 @@ extern "C" bigcn_status bigcn_layer_norm_backward(
     const uint8_t *exps, int64_t lde, const float *rstd, void *dX, int64_t lddx, float *dgamma,
     float *dbeta, void *workspace, size_t ws_bytes, void *stream) {
     const size_t es = dtype_bytes(dtype);
-    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || lddy < K || (dX && lddx < K))
+    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols ||
+        lddy < K || (dX && lddx < K))
         return BIGCN_ERR_INVALID_ARG;
     if (!dX && !dgamma && !dbeta) return BIGCN_ERR_INVALID_ARG;
     const bool params = dgamma || dbeta;
@@ -108,9 +111,8 @@ extern "C" bigcn_status bigcn_layer_norm_backward(
             }
         return BIGCN_OK;
     }
-    BackwardArgs a{dY,   N,    K,  lddy, gamma, X,
-                         ldx,  mean, q,  ldq,  exps,  lde,
-                         rstd, dX,   lddx, params ? static_cast<float *>(workspace) : nullptr, 0};
+    BackwardArgs a{dY,   N,  K,    lddy, gamma, X,    ldx, mean, q,
+                   ldq,  exps, lde, rstd, dX,  lddx, params ? static_cast<float *>(workspace) : nullptr, 0};
     if (dtype == BIGCN_F32) launch_backward<float>(a, dev, s);
     else if (dtype == BIGCN_BF16) launch_backward<__nv_bfloat16>(a, dev, s);
     else launch_backward<__half>(a, dev, s);

@@ -245,8 +245,8 @@ extern "C" bigcn_status bigcn_layer_norm_forward(int32_t dtype, const void *X, i
                                                  int64_t ldq, uint8_t *exps, int64_t lde,
                                                  void *stream) {
     const size_t es = dtype_bytes(dtype);
-    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || ldx < K || ldy < K ||
-        !(eps >= 0.0f) || !std::isfinite(eps) || (q == nullptr) != (exps == nullptr))
+    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxCols || ldx < K ||
+        ldy < K || !(eps >= 0.0f) || !std::isfinite(eps) || (q == nullptr) != (exps == nullptr))
         return BIGCN_ERR_INVALID_ARG;
     if (q && !checkpoint_strides_ok(N, K, ldq, lde)) return BIGCN_ERR_INVALID_ARG;
     if (N > 0 && (N > kMaxElems / ldx || N > kMaxElems / ldy)) return BIGCN_ERR_INVALID_ARG;

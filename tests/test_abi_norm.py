@@ -146,3 +146,28 @@ def test_weight_grad_refusals(lib):
                dict(dZ=ptr(4) + 2), dict(dW=ptr(5) + 2), dict(db=ptr(6) + 2),
                dict(ws=ptr(7) + 64), dict(dtype=BF16, dZ=ptr(4) + 1)):
         assert f(**kw) == MISALIGNED, kw
+
+
+def test_rows_past_the_widest_are_refused(lib):
+    """K and F up to 2^30: the kernels' column indices have 32 bits and step past a row's end."""
+    K = (1 << 30) + 16
+    wide = dict(K=K, ldx=K, ldq=K, lde=(1 << 25) + 4)
+    assert lib.bigcn_checkpoint_pack(*pack_args(X=1 << 40, q=1 << 50, exps=1 << 51, **wide)) == INVALID
+    assert lib.bigcn_checkpoint_unpack(*unpack_args(
+        X=1 << 40, q=1 << 50, exps=1 << 51, gamma=None, beta=None, **wide)) == INVALID
+    assert lib.bigcn_layer_norm_forward(*forward_args(
+        X=1 << 40, Y=1 << 45, ldy=K, q=1 << 50, exps=1 << 51, gamma=None, beta=None, **wide)) == INVALID
+    assert lib.bigcn_layer_norm_backward_workspace_bytes(10, K) == 0
+    assert lib.bigcn_layer_norm_backward(*backward_args(
+        lib, K=K, lddy=K, lddx=K, ldq=K, lde=(1 << 25) + 4, dY=1 << 40, dX=1 << 45, q=1 << 50,
+        exps=1 << 51, gamma=None, dgamma=None, dbeta=None, ws=None, wsb=0)) == INVALID
+    assert lib.bigcn_checkpoint_weight_grad_workspace_bytes(100, K, 9) == 0
+    assert lib.bigcn_checkpoint_weight_grad_workspace_bytes(100, 9, K) == 0
+
+
+def test_backward_workspace_follows_the_rows(lib):
+    """A row's sums each, at most 1024 of them: a single wide row needs no more than its own."""
+    w = lib.bigcn_layer_norm_backward_workspace_bytes
+    assert w(1, 70001) == (2 * 70001 * 4 + 255) // 256 * 256
+    assert w(1024, 64) == w(1 << 30, 64) == 1024 * 2 * 64 * 4
+    assert 0 < w(0, 64) <= w(1, 64) < w(2, 64)
