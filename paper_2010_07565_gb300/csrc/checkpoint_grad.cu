@@ -251,35 +251,41 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
         if (lane == 0) {
             const uint32_t idesc = atom_idesc(round_up_to(cols, 16));
             bool any = false;
+            int s = 0, o = 0, at = 0;           // slot, stage, place in the block of kDrain
+            uint32_t op_parity = 0u, drain_parity = 1u;
             for (int st = 0; st < n; ++st) {
-                const int s = st % kSlots, o = st % kStages;
-                const int block = st / kDrain, at = st % kDrain;
-                bool go = wait_unless(smem_addr(&filled[o]), uint32_t(st / kStages) & 1u, stopv);
-                if (S::kDirect)
-                    go = go && wait_unless(smem_addr(&loaded[s]), uint32_t(st / kSlots) & 1u, stopv);
-                if (at == 0 && block > 0)
-                    go = go && wait_unless(smem_addr(&drained), uint32_t(block - 1) & 1u, stopv);
+                // (What the workers have filled they have seen loaded.)
+                bool go = wait_unless(smem_addr(&filled[o]), op_parity, stopv);
+                if (at == 0 && st > 0)
+                    go = go && wait_unless(smem_addr(&drained), drain_parity, stopv);
                 if (!go) {
                     *stopv = 1u;
                     break;
                 }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t a0 = base + uint32_t(o * S::kOp);
-                const uint32_t b0 = S::kDirect ? base + uint32_t(kSlot0 + s * S::kSlot)
-                                               : a0 + uint32_t(S::kOpA);
+                const uint64_t a0 = atom_desc<kRows>(base + uint32_t(o * S::kOp));
+                const uint64_t b0 = atom_desc<kRows>(
+                    base + uint32_t(S::kDirect ? kSlot0 + s * S::kSlot : o * S::kOp + S::kOpA));
+#pragma unroll 1
+                for (int t = 0; t < mt; ++t)
 #pragma unroll
-                for (int k = 0; k < kRows / 16; ++k)
-                    for (int t = 0; t < mt; ++t)
+                    for (int k = 0; k < kRows / 16; ++k)
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part)
                             mma_rows(tmem + uint32_t(t * NT),
-                                     atom_desc<kRows>(a0 + uint32_t(t * 2 * kAtom + k * 2048)),
-                                     atom_desc<kRows>(b0 + uint32_t(part * S::kPart + k * 2048)), idesc,
+                                     a0 + uint32_t((t * 2 * kAtom + k * 2048) >> 4),
+                                     b0 + uint32_t((part * S::kPart + k * 2048) >> 4), idesc,
                                      at > 0 || k > 0 || part > 0);
                 any = true;
                 mma_commit(smem_addr(&used[o]));
                 if (S::kDirect) mma_commit(smem_addr(&freed[s]));
-                if (at == kDrain - 1 || st == n - 1) mma_commit(smem_addr(&summed));
+                if (++at == kDrain || st == n - 1) {
+                    mma_commit(smem_addr(&summed));
+                    at = 0;
+                    drain_parity ^= 1u;
+                }
+                if (++s == kSlots) s = 0;
+                if (++o == kStages) o = 0, op_parity ^= 1u;
             }
             if (any) mma_commit(smem_addr(&done));
             else mbar_arrive(smem_addr(&done));
