@@ -50,8 +50,8 @@ constexpr int kWorkers = 512;
 constexpr int kWorkerWarps = kWorkers / 32;
 constexpr int kTeams = 2;               // of workers, which take stages in turn
 constexpr int kTeamWarps = kWorkerWarps / kTeams;
-constexpr int kCopyWarp = kWorkerWarps, kMmaWarp = kWorkerWarps + 1;
-constexpr int kGradThreads = kWorkers + 64;
+constexpr int kCopyWarp = kWorkerWarps, kMmaWarp = kWorkerWarps + 1, kScaleWarp = kWorkerWarps + 2;
+constexpr int kGradThreads = kWorkers + 96;
 constexpr int kAccCols = 256;           // accumulator columns; as many of running sums
 constexpr size_t kAlign = 256;
 constexpr int kSmemMost = 227 * 1024 - 1024 - 5120;   // less alignment and static memory
@@ -185,7 +185,7 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     }
     if (tid == 0) {
         for (int s = 0; s < kSlots; ++s) {
-            mbar_init(smem_addr(&loaded[s]), 33);       // the copy warp's lanes, and its bytes
+            mbar_init(smem_addr(&loaded[s]), 33);       // the scale warp's lanes; boxes' bytes
             mbar_init(smem_addr(&freed[s]), S::kDirect ? 1 : kTeamWarps);
         }
         for (int s = 0; s < kStages; ++s) {
@@ -206,42 +206,43 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
 
     float colsum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 
-    if (warp == kCopyWarp) {
+    if (warp == kCopyWarp || warp == kScaleWarp) {
         const uint32_t bytes = uint32_t(mt * kRows * 128 + (kTma ? atoms * kRows * 64 * S::kElem : 0));
-        int issued = 0;
-        for (int st = 0; st < n; ++st) {
-            const int s = st % kSlots;
-            const bool go = st < kSlots || wait_unless(smem_addr(&freed[s]),
-                                                       uint32_t(st / kSlots - 1) & 1u, stopv);
+        int issued = 0, s = 0;
+        uint32_t slot = base + uint32_t(kSlot0), parity = 1u;
+        int64_t row = st0 * kRows;
+        for (int st = 0; st < n; ++st, row += kRows) {
+            const bool go = st < kSlots || wait_unless(smem_addr(&freed[s]), parity, stopv);
             if (!__all_sync(kFullMask, go)) {
                 *stopv = 1u;
                 break;
             }
-            const uint32_t slot = base + uint32_t(kSlot0 + s * S::kSlot);
             const uint32_t bar = smem_addr(&loaded[s]);
-            const int64_t row0 = (st0 + st) * kRows;
-            // Scale bytes: lane = row, four groups (128 features) a copy.
+            if (warp == kScaleWarp) {
+                // Scale bytes: lane = row, four groups (128 features) a copy.
 #pragma unroll
-            for (int h = 0; h < kRows / 32; ++h) {
-                const int row = 32 * h + lane;
-                const bool in = row0 + row < p.N;
-                const uint8_t *e = p.exps + (in ? (row0 + row) * p.lde + tile0 * 4 : 0);
-                for (int t = 0; t < mt; ++t)
-                    copy4(slot + uint32_t(S::kSlotZ + S::kSlotQ + (t * kRows + row) * 4),
-                          in ? e + t * 4 : e, in ? 4u : 0u);
-            }
-            if (lane == 0) {
+                for (int h = 0; h < kRows / 32; ++h) {
+                    const int64_t i = row + 32 * h + lane;
+                    const bool in = i < p.N;
+                    const uint8_t *e = p.exps + (in ? i * p.lde + tile0 * 4 : 0);
+                    for (int t = 0; t < mt; ++t)
+                        copy4(slot + uint32_t(S::kSlotZ + S::kSlotQ + (t * kRows + 32 * h + lane) * 4),
+                              in ? e + t * 4 : e, in ? 4u : 0u);
+                }
+                copies_arrive(bar);
+            } else if (lane == 0) {
                 mbar_expect(bar, bytes);
                 if constexpr (kTma)
                     for (int a = 0; a < atoms; ++a)
                         tma_load(slot + uint32_t(a * kRows * 64 * S::kElem), &p.z_map, n0 + 64 * a,
-                                 int(row0), bar);
+                                 int(row), bar);
                 for (int t = 0; t < mt; ++t)
                     tma_load(slot + uint32_t(S::kSlotZ + t * kRows * 128), &p.q_map,
-                             int(tile0 + t) * 128, int(row0), bar);
+                             int(tile0 + t) * 128, int(row), bar);
             }
-            copies_arrive(bar);
             issued = st + 1;
+            slot += S::kSlot;
+            if (++s == kSlots) s = 0, slot = base + uint32_t(kSlot0), parity ^= 1u;
             __syncwarp();
         }
         // What is still in flight lands before the shared memory is given up.
