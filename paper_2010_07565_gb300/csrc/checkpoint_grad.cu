@@ -87,7 +87,8 @@ struct GradShape {
 
 struct GradParams {
     CUtensorMap q_map;       // K rounded up to 16 bytes x N
-    CUtensorMap z_map;       // F x N of dZ (kTma)
+    CUtensorMap z_map;       // F x N of dZ (kTma), or
+    bool z_atoms;            // 64 x N x F / 64: all atoms of a stage are one box
     const uint8_t *exps;
     int64_t lde;
     int64_t N;
@@ -207,7 +208,8 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     float colsum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 
     if (warp == kCopyWarp || warp == kScaleWarp) {
-        const uint32_t bytes = uint32_t(mt * kRows * 128 + (kTma ? atoms * kRows * 64 * S::kElem : 0));
+        const int boxes = p.z_atoms ? NT / 64 : atoms;
+        const uint32_t bytes = uint32_t(mt * kRows * 128 + (kTma ? boxes * kRows * 64 * S::kElem : 0));
         int issued = 0, s = 0;
         uint32_t slot = base + uint32_t(kSlot0), parity = 1u;
         int64_t row = st0 * kRows;
@@ -232,10 +234,12 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                 copies_arrive(bar);
             } else if (lane == 0) {
                 mbar_expect(bar, bytes);
-                if constexpr (kTma)
-                    for (int a = 0; a < atoms; ++a)
+                if constexpr (kTma) {
+                    if (p.z_atoms) tma_load_3d(slot, &p.z_map, 0, int(row), n0 / 64, bar);
+                    else for (int a = 0; a < atoms; ++a)
                         tma_load(slot + uint32_t(a * kRows * 64 * S::kElem), &p.z_map, n0 + 64 * a,
                                  int(row), bar);
+                }
                 for (int t = 0; t < mt; ++t)
                     tma_load(slot + uint32_t(S::kSlotZ + t * kRows * 128), &p.q_map,
                              int(tile0 + t) * 128, int(row), bar);
@@ -657,16 +661,18 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// A map of `rows` rows of `width` elements, boxes of box x box_rows.
+// A map of `rows` rows of `width` elements, boxes of box x box_rows; of `atoms` > 1: its rows
+// are cut into parts of `width` elements, `atoms` of which are a box.
 bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
-            int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle) {
+            int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle, int64_t parts = 1,
+            int64_t part_bytes = 0, int box_parts = 1) {
     const EncodeTiled fn = encoder();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {cuuint64_t(width), cuuint64_t(rows)};
-    const cuuint64_t strides[1] = {cuuint64_t(row_bytes)};
-    const cuuint32_t boxes[2] = {cuuint32_t(box), cuuint32_t(box_rows)};
-    const cuuint32_t steps[2] = {1, 1};
-    return fn(map, type, 2, const_cast<void *>(base), dims, strides, boxes, steps,
+    const cuuint64_t dims[3] = {cuuint64_t(width), cuuint64_t(rows), cuuint64_t(parts)};
+    const cuuint64_t strides[2] = {cuuint64_t(row_bytes), cuuint64_t(part_bytes)};
+    const cuuint32_t boxes[3] = {cuuint32_t(box), cuuint32_t(box_rows), cuuint32_t(box_parts)};
+    const cuuint32_t steps[3] = {1, 1, 1};
+    return fn(map, type, part_bytes ? 3 : 2, const_cast<void *>(base), dims, strides, boxes, steps,
               CU_TENSOR_MAP_INTERLEAVE_NONE,
               swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -760,11 +766,17 @@ extern "C" bigcn_status bigcn_checkpoint_weight_grad(
                                      : dtype == BIGCN_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     // Tensor copies want rows that start on 16-byte boundaries. A bf16 dZ is copied as an operand,
-    // in stages of 64 rows (GradShape).
+    // in stages of 64 rows (GradShape); all atoms of a stage at once where F is a multiple of 64
+    // (behind a last partial atom the box would read past the rows' end).
     const int64_t zrow = lddz * int64_t(es);
     const bool direct = dtype == BIGCN_BF16;
-    const bool tma = aligned_to(dZ, 16) && zrow % 16 == 0 &&
-                     encode(&p.z_map, type, dZ, F, N, zrow, 64, direct ? 64 : 32, direct);
+    const int most = aligned_to(dZ, 16) && zrow % 16 == 0 ? kMostTma : kMostLoaded;
+    p.z_atoms = F % 64 == 0;
+    const bool tma =
+        most == kMostTma &&
+        (p.z_atoms ? encode(&p.z_map, type, dZ, 64, N, zrow, 64, direct ? 64 : 32, direct, F / 64,
+                            64 * int64_t(es), grad_plan(N, K, F, most).NT / 64)
+                   : encode(&p.z_map, type, dZ, F, N, zrow, 64, direct ? 64 : 32, direct));
     const int rows = tma && direct ? 64 : 32;
     const int64_t width = (int64_t(K) + 15) / 16 * 16;
     if (!encode(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, rows,
