@@ -20,6 +20,7 @@
 // They meet on mbarriers only:
 //   loaded[slot]   a slot's copies have landed         freed[slot]   it may be refilled
 //   filled[stage]  a team has written a stage          used[stage]   its MMAs are done
+//                                    (with a dZ that is copied as an operand: freed[slot] says it)
 //   summed         a block's MMAs are done             drained       its sums were taken
 //
 // Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
@@ -82,7 +83,7 @@ struct GradShape {
     // 48 (64 where there are no parts) accumulating MMAs, kRows / 16 per stage and part, between
     // two drains.
     static constexpr int kDrain = kDirect ? 16 : PARTS == 1 ? 24 : PARTS == 2 ? 12 : 8;
-    static_assert(kSlots >= kTeams && kStages >= kTeams, "shared memory per CTA");
+    static_assert(kSlots >= kTeams && kStages >= kTeams && kSlots >= kStages, "shared memory per CTA");
 };
 
 struct GradParams {
@@ -253,24 +254,25 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
         for (int st = max(0, issued - kSlots); st < issued; ++st)
             mbar_wait(smem_addr(&loaded[st % kSlots]), uint32_t(st / kSlots) & 1u);
     } else if (warp == kMmaWarp) {
-        if (lane == 0) {
-            const uint32_t idesc = atom_idesc(round_up_to(cols, 16));
-            bool any = false;
-            int s = 0, o = 0, at = 0;           // slot, stage, place in the block of kDrain
-            uint32_t op_parity = 0u, drain_parity = 1u;
-            for (int st = 0; st < n; ++st) {
-                // (What the workers have filled they have seen loaded.)
-                bool go = wait_unless(smem_addr(&filled[o]), op_parity, stopv);
-                if (at == 0 && st > 0)
-                    go = go && wait_unless(smem_addr(&drained), drain_parity, stopv);
-                if (!go) {
-                    *stopv = 1u;
-                    break;
-                }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t a0 = atom_desc<kRows>(base + uint32_t(o * S::kOp));
-                const uint64_t b0 = atom_desc<kRows>(
-                    base + uint32_t(S::kDirect ? kSlot0 + s * S::kSlot : o * S::kOp + S::kOpA));
+        // The warp stays together (its addresses are uniform then), one lane issues.
+        const uint32_t idesc = atom_idesc(round_up_to(cols, 16));
+        bool any = false;
+        int s = 0, o = 0, at = 0;           // slot, stage, place in the block of kDrain
+        uint32_t op_parity = 0u, drain_parity = 1u;
+        for (int st = 0; st < n; ++st) {
+            // (What the workers have filled they have seen loaded.)
+            bool go = wait_unless(smem_addr(&filled[o]), op_parity, stopv);
+            if (at == 0 && st > 0) go = go && wait_unless(smem_addr(&drained), drain_parity, stopv);
+            if (!__all_sync(kFullMask, go)) {
+                *stopv = 1u;
+                break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t a0 = atom_desc<kRows>(base + uint32_t(o * S::kOp));
+            const uint64_t b0 = atom_desc<kRows>(
+                base + uint32_t(S::kDirect ? kSlot0 + s * S::kSlot : o * S::kOp + S::kOpA));
+            const bool last = at + 1 == kDrain || st == n - 1;
+            if (elect_one()) {
 #pragma unroll 1
                 for (int t = 0; t < mt; ++t)
 #pragma unroll
@@ -281,17 +283,15 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                                      a0 + uint32_t((t * 2 * kAtom + k * 2048) >> 4),
                                      b0 + uint32_t((part * S::kPart + k * 2048) >> 4), idesc,
                                      at > 0 || k > 0 || part > 0);
-                any = true;
-                mma_commit(smem_addr(&used[o]));
-                if (S::kDirect) mma_commit(smem_addr(&freed[s]));
-                if (++at == kDrain || st == n - 1) {
-                    mma_commit(smem_addr(&summed));
-                    at = 0;
-                    drain_parity ^= 1u;
-                }
-                if (++s == kSlots) s = 0;
-                if (++o == kStages) o = 0, op_parity ^= 1u;
+                mma_commit(S::kDirect ? smem_addr(&freed[s]) : smem_addr(&used[o]));
+                if (last) mma_commit(smem_addr(&summed));
             }
+            any = true;
+            if (++at == kDrain) at = 0, drain_parity ^= 1u;
+            if (++s == kSlots) s = 0;
+            if (++o == kStages) o = 0, op_parity ^= 1u;
+        }
+        if (elect_one()) {
             if (any) mma_commit(smem_addr(&done));
             else mbar_arrive(smem_addr(&done));
         }
@@ -361,7 +361,16 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             }
             // (A stage's first use waits for the phase before the first, which is complete.)
             bool go = wait_unless(smem_addr(&loaded[s]), sp, stopv);
-            go = go && wait_unless(smem_addr(&used[o]), op_parity ^ 1u, stopv);
+            if constexpr (S::kDirect) {
+                // The slot of the stage's last use: freed by the same MMAs. (Its next phase is
+                // st's own or later: kSlots >= kStages.)
+                const int last = st - kStages;
+                if (last >= 0)
+                    go = go && wait_unless(smem_addr(&freed[last % kSlots]),
+                                           uint32_t(last / kSlots) & 1u, stopv);
+            } else {
+                go = go && wait_unless(smem_addr(&used[o]), op_parity ^ 1u, stopv);
+            }
             ok = __all_sync(kFullMask, go);
             if (!ok) break;
             const unsigned char *slot = mem + kSlot0 + s * S::kSlot;

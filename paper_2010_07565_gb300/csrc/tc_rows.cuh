@@ -48,6 +48,17 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint64_t a, uint64_t b
         "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u));
 }
 
+// True for one lane of a warp that is together, always the same one.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t on;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(on));
+    return on != 0;
+}
+
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile(
         "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
