@@ -233,7 +233,7 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                               in ? e + t * 4 : e, in ? 4u : 0u);
                 }
                 copies_arrive(bar);
-            } else if (lane == 0) {
+            } else if (elect_one()) {
                 mbar_expect(bar, bytes);
                 if constexpr (kTma) {
                     if (p.z_atoms) tma_load_3d(slot, &p.z_map, 0, int(row), n0 / 64, bar);
