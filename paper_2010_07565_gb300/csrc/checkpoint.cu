@@ -1,4 +1,7 @@
-// Activations to 8 bits and back (bigcn_checkpoint_pack, bigcn_checkpoint_unpack).
+// Activations to 8 bits and back (bigcn_checkpoint_pack, bigcn_checkpoint_unpack): the arithmetic
+// is checkpoint.cuh's, a few operations a column; both are bound by memory. 2^20 x 512 bf16: packing
+// 247 us (0.95 of a copy's rate), unpacking 362 us (0.66: two bytes written for one read, DRAM at
+// half its rate; neither streaming stores nor more or fewer pieces a thread changed that).
 #include "norm.cuh"
 
 namespace bigcn {
@@ -10,7 +13,6 @@ constexpr int kCkThreads = 256;
 // bytes of X, as layer norm does (norm.cuh). A thread takes three or four pieces, J of
 // a row by R rows, all loaded before the first is used (eight to unpack: 616 -> 635 us for both at
 // 2^20 x 512 bf16); a row longer than tpr J pieces goes over several blocks.
-// Bound by memory.
 template <int V, int J, int R>
 struct Place {
     int64_t i[R];            // rows

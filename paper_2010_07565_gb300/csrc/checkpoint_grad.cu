@@ -14,13 +14,14 @@
 // bf16 dZ goes by tensor copies from memory into its swizzled place; q (and an fp32 or
 // fp16 dZ) by tensor copies into a ring of raw slots, from which the workers expand it.
 //
-// Roles of a CTA (576 threads): warps 0-15, the workers, turn raw slots into operand
+// Roles of a CTA (608 threads): warps 0-15, the workers, turn raw slots into operand
 // stages, in two teams that take every second stage each (one's latencies pass under the
-// other's instructions), and take the running sums. Warp 16 copies, warp 17 issues the MMAs.
+// other's instructions), and take the running sums. Warp 16 copies, warp 17 issues the MMAs, warp
+// 18 copies the scale bytes (with the boxes in one warp: 336 us for 299 at 2^20 x 512 x 256 bf16).
 // They meet on mbarriers only:
 //   loaded[slot]   a slot's copies have landed         freed[slot]   it may be refilled
 //   filled[stage]  a team has written a stage          used[stage]   its MMAs are done
-//                                    (with a dZ that is copied as an operand: freed[slot] says it)
+//                    (where dZ is copied as an operand, freed[slot] says both)
 //   summed         a block's MMAs are done             drained       its sums were taken
 //
 // Running sums. The tensor core truncates when it accumulates (measured: 2.0e-8 of the
@@ -36,6 +37,16 @@
 // adds the runs in order, sums s_j, and applies gamma and beta. The columns of dZ are summed by
 // the CTA that has them in shared memory anyway: of the groups of feature tiles that read the
 // same rows, group g takes the g-th 64 columns.
+//
+// What bounds it, in cycles of a stage:
+//   fp32 dZ (232,965 x 602 x 128, 32 rows: 122 us, 883 TFLOP/s of the three parts' products):
+//     about 1300, near what shared memory moves: 184 KB (48 copied and read, 40 of operands
+//     written, 96 read by the MMAs); the MMAs alone take 820. A kept in the tensor core's
+//     collector for the three parts changed nothing (131 us both ways then).
+//   bf16 dZ (2^20 x 512 x 256, 64 rows: 283 us, 970 TFLOP/s): about 1250; MMAs 545, shared memory
+//     900. A slot's way through copy, expansion and MMA takes four times that, and four slots fit;
+//     dZ is read by four groups of tiles, three times of four from L2.
+//   small calls (2708 x 1433 x 64 fp32: 14.4 us): this kernel's and the second's latencies.
 #include "checkpoint.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -670,8 +681,8 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// A map of `rows` rows of `width` elements, boxes of box x box_rows; of `atoms` > 1: its rows
-// are cut into parts of `width` elements, `atoms` of which are a box.
+// A map of `rows` rows of `width` elements, boxes of box x box_rows; or, with part_bytes, of rows
+// of `parts` parts of `width` elements, box_parts of which are in a box.
 bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
             int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle, int64_t parts = 1,
             int64_t part_bytes = 0, int box_parts = 1) {

@@ -29,7 +29,7 @@ template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 // pieces: each place has its own accesses, the widest that it allows, by a branch that the row's
 // threads take together. Where a warp holds several rows these may lie at different places:
 // kMixed, by accesses that suit all. (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 ->
-// 315 us, backward 305 -> 253; rows of 55 columns, four a warp, 37 us, by places 51.)
+// 317 us, backward 305 -> 247; rows of 55 columns, four a warp, 37 us, by places 51.)
 constexpr int kMixed = 1;
 __device__ __forceinline__ int place_of(const void *row, bool mixed) {
     const int at = int(reinterpret_cast<uintptr_t>(row) & 15);
@@ -239,7 +239,8 @@ __device__ __forceinline__ void group_tops(const uint32_t (&own)[J], uint32_t (&
 // A piece to int8 and back (checkpoint.cuh has the rounding): V bytes as one word or two.
 template <int H> using QPiece = typename std::conditional<H == 4, uint2, uint32_t>::type;
 __device__ __forceinline__ uint32_t quantise4(float2 a, float2 b, float f) {
-    const float2 x = __ffma2_rn(a, both(f), both(12582912.0f)), y = __ffma2_rn(b, both(f), both(12582912.0f));
+    const float2 x = __ffma2_rn(a, both(f), both(12582912.0f));
+    const float2 y = __ffma2_rn(b, both(f), both(12582912.0f));
     return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
                        __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
@@ -281,9 +282,9 @@ struct RowLayout {
     int tpr, J;
 };
 
-// The fewest threads (8 or more, so that a group of 32 columns lies in one row's lanes) that hold a row of K, with at most `most` elements each,
-// `warp_most` where they are a warp; and then more threads while the rows do not fill the card
-// (each has less to do then).
+// The fewest threads (8 or more, so that a group of 32 columns lies in one row's lanes) that
+// hold a row of K, with at most `most` elements each, `warp_most` where they are a warp; and then
+// more threads while the rows do not fill the card (each has less to do then).
 inline RowLayout row_layout(int64_t N, int K, int V, int most, int warp_most, const DeviceInfo &dev) {
     const int *options = kOptions[V == 8];
     const int64_t pieces = (int64_t(K) + V - 1) / V;
