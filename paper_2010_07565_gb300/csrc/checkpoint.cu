@@ -52,12 +52,12 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const T *row = static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0;
-        const int place = place_of(row, tpr < 32);
+        const bool whole = whole_pieces<A>(row, tpr >= 32);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             w[r][j] = make_uint4(0u, 0u, 0u, 0u);
             if (at.i[r] < a.N && left > j * at.step)
-                w[r][j] = load_piece<T, A>(row + j * at.step, left - j * at.step, place);
+                w[r][j] = load_piece<T, A>(row + j * at.step, left - j * at.step, whole);
         }
     }
     // Past K a piece is zeros and so is its q.
@@ -123,7 +123,7 @@ unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
                 for (int e = 0; e < H; ++e)
                     v[e] = __ffma2_rn(v[e], a.gamma ? g[e] : both(1.0f), a.beta ? c[e] : both(0.0f));
             T *out = static_cast<T *>(a.X) + at.i[r] * a.ldx + k;
-            store_piece<T, A>(out, pack16<T>(v), n, place_of(out, tpr < 32));
+            store_piece<T, A>(out, pack16<T>(v), n, whole_pieces<A>(out, tpr >= 32));
         }
     }
 }

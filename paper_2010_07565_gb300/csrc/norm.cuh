@@ -25,34 +25,29 @@ constexpr int kMostRowThreads = 512;
 template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 
 // ---- 16 bytes of a row --------------------------------------------------------------------
-// A row that is aligned to A bytes lies at one of 16 / A places of 16 bytes, the same for all its
-// pieces: each place has its own accesses, the widest that it allows, by a branch that the row's
-// threads take together. Where a warp holds several rows these may lie at different places:
-// kMixed, by accesses that suit all. (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 ->
-// 317 us, backward 305 -> 247; rows of 55 columns, four a warp, 37 us, by places 51.)
-constexpr int kMixed = 1;
-__device__ __forceinline__ int place_of(const void *row, bool mixed) {
-    const int at = int(reinterpret_cast<uintptr_t>(row) & 15);
-    return mixed ? kMixed : (at & 2) ? 2 : (at & 4) ? 4 : at;
+// Rows aligned to 8 bytes lie at 0 or 8 of 16, each row at the same for all its pieces: `whole`,
+// by which its pieces are one access or two, is a branch that the row's threads take together
+// (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 -> 317 us, backward 305 -> 247). Not
+// so where a warp holds several rows, which would part (90,863 x 55 columns: 37 -> 51 us), and not
+// by the four places of rows aligned to 4 bytes, whose code is too long (100,000 x 601 fp32:
+// backward 132 -> 310 us).
+template <int A> __device__ __forceinline__ bool whole_pieces(const void *row, bool together) {
+    return A == 8 && together && (reinterpret_cast<uintptr_t>(row) & 15) == 0;
 }
-template <int A> __device__ __forceinline__ uint4 load16(const void *p, int place) {
+template <int A> __device__ __forceinline__ uint4 load16(const void *p, bool whole) {
     if constexpr (A == 16) {
         return *static_cast<const uint4 *>(p);
     } else if constexpr (A == 8) {
-        if (place == 0) return load16<16>(p, 0);
+        if (whole) return load16<16>(p, true);
         const uint2 *q = static_cast<const uint2 *>(p);
         const uint2 a = q[0], b = q[1];
         return make_uint4(a.x, a.y, b.x, b.y);
     } else if constexpr (A == 4) {
-        if (place == 0 || place == 8) return load16<8>(p, place);
         const uint32_t *q = static_cast<const uint32_t *>(p);
-        if (place == kMixed) return make_uint4(q[0], q[1], q[2], q[3]);
-        const uint2 m = *reinterpret_cast<const uint2 *>(q + 1);
-        return make_uint4(q[0], m.x, m.y, q[3]);
+        return make_uint4(q[0], q[1], q[2], q[3]);
     } else {
         // 2 bytes past a word: the words between, and a half at each end.
-        if (place == kMixed ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : place != 2)
-            return load16<4>(p, place);
+        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) return load16<4>(p, false);
         const uint16_t *h = static_cast<const uint16_t *>(p);
         const uint32_t *q = reinterpret_cast<const uint32_t *>(h + 1);
         const uint32_t e0 = h[0], x0 = q[0], x1 = q[1], x2 = q[2], e7 = h[7];
@@ -60,33 +55,25 @@ template <int A> __device__ __forceinline__ uint4 load16(const void *p, int plac
                           (x2 >> 16) | (e7 << 16));
     }
 }
-template <int A> __device__ __forceinline__ void store16(void *p, uint4 v, int place) {
+template <int A> __device__ __forceinline__ void store16(void *p, uint4 v, bool whole) {
     if constexpr (A == 16) {
         *static_cast<uint4 *>(p) = v;
     } else if constexpr (A == 8) {
-        if (place == 0) {
-            store16<16>(p, v, 0);
+        if (whole) {
+            store16<16>(p, v, true);
         } else {
             static_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
             static_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
         }
     } else if constexpr (A == 4) {
         uint32_t *q = static_cast<uint32_t *>(p);
-        if (place == 0 || place == 8) {
-            store16<8>(p, v, place);
-        } else if (place == kMixed) {
-            q[0] = v.x;
-            q[1] = v.y;
-            q[2] = v.z;
-            q[3] = v.w;
-        } else {
-            q[0] = v.x;
-            *reinterpret_cast<uint2 *>(q + 1) = make_uint2(v.y, v.z);
-            q[3] = v.w;
-        }
+        q[0] = v.x;
+        q[1] = v.y;
+        q[2] = v.z;
+        q[3] = v.w;
     } else {
-        if (place == kMixed ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : place != 2) {
-            store16<4>(p, v, place);
+        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
+            store16<4>(p, v, false);
             return;
         }
         uint16_t *h = static_cast<uint16_t *>(p);
@@ -121,12 +108,12 @@ template <typename T> __device__ __forceinline__ void store_some(T *p, uint4 v, 
         }
 }
 template <typename T, int A>
-__device__ __forceinline__ uint4 load_piece(const T *p, int n, int place) {
-    return n >= kPiece<T> ? load16<A>(p, place) : load_some(p, n);
+__device__ __forceinline__ uint4 load_piece(const T *p, int n, bool whole) {
+    return n >= kPiece<T> ? load16<A>(p, whole) : load_some(p, n);
 }
 template <typename T, int A>
-__device__ __forceinline__ void store_piece(T *p, uint4 v, int n, int place) {
-    if (n >= kPiece<T>) store16<A>(p, v, place);
+__device__ __forceinline__ void store_piece(T *p, uint4 v, int n, bool whole) {
+    if (n >= kPiece<T>) store16<A>(p, v, whole);
     else store_some(p, v, n);
 }
 

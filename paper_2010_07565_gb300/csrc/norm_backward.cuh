@@ -95,16 +95,16 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
     const float *gamma = a.gamma ? a.gamma + k0 : kOnes;
     const int gstep = a.gamma ? step : 0;
 
-    const bool mixed = !kWarp && tpr < 32;
+    const bool together = kWarp || tpr >= 32;
     auto load = [&](int64_t i, RawRow<J, H, kKept> &r) {
         if (i >= a.N) return;
         const T *dy = static_cast<const T *>(a.dY) + i * a.lddy + k0;
-        const int dy_place = place_of(dy, mixed);
+        const bool dy_whole = whole_pieces<A>(dy, together);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (j < kFull) r.dy[j] = load16<A>(dy + j * step, dy_place);
+            if (j < kFull) r.dy[j] = load16<A>(dy + j * step, dy_whole);
             else if (left > j * step)
-                r.dy[j] = load_piece<T, A>(dy + j * step, left - j * step, dy_place);
+                r.dy[j] = load_piece<T, A>(dy + j * step, left - j * step, dy_whole);
         }
         if constexpr (kKept) {
             const int8_t *q = a.q + i * a.ldq + k0;
@@ -117,12 +117,12 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
                 }
         } else {
             const T *x = static_cast<const T *>(a.X) + i * a.ldx + k0;
-            const int x_place = place_of(x, mixed);
+            const bool x_whole = whole_pieces<A>(x, together);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                if (j < kFull) r.x[j] = load16<A>(x + j * step, x_place);
+                if (j < kFull) r.x[j] = load16<A>(x + j * step, x_whole);
                 else if (left > j * step)
-                    r.x[j] = load_piece<T, A>(x + j * step, left - j * step, x_place);
+                    r.x[j] = load_piece<T, A>(x + j * step, left - j * step, x_whole);
             }
             r.mean = a.mean[i];
         }
@@ -190,7 +190,7 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
         if (!kWarp && !live) continue;
         const float2 c0 = both(-s[0] * inv_k), c1 = both(-s[1] * inv_k), rs = both(rstd);
         T *dx = static_cast<T *>(a.dX) + i * a.lddx + k0;
-        const int dx_place = place_of(dx, mixed);
+        const bool dx_whole = whole_pieces<A>(dx, together);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int n = j < kFull ? V : left - j * step;
@@ -203,7 +203,7 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
                 const float2 xh = kHold ? hk[kHold ? j : 0][e] : h[e];
                 d[e] = __fmul2_rn(__ffma2_rn(xh, c1, __fadd2_rn(g, c0)), rs);
             }
-            store_piece<T, A>(dx + j * step, pack16<T>(d), n, dx_place);
+            store_piece<T, A>(dx + j * step, pack16<T>(d), n, dx_whole);
         }
     }
     allow_dependent_launch();

@@ -98,13 +98,13 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
     // The row as it was read: 16-bit elements take half the registers that way, so that all
     // loads are under way at once, and are expanded for each use.
     uint4 w[J];
-    const bool mixed = !kWarp && tpr < 32;
-    const int x_place = place_of(row, mixed);
+    const bool together = kWarp || tpr >= 32;
+    const bool x_whole = whole_pieces<A>(row, together);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         w[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (j < kFull) w[j] = load16<A>(row + j * step, x_place);
-        else if (left > j * step) w[j] = load_piece<T, A>(row + j * step, left - j * step, x_place);
+        if (j < kFull) w[j] = load16<A>(row + j * step, x_whole);
+        else if (left > j * step) w[j] = load_piece<T, A>(row + j * step, left - j * step, x_whole);
     }
     float2 s2 = both(0.0f);
 #pragma unroll
@@ -141,7 +141,7 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
         if (a.rstd) a.rstd[i] = rstd;
     }
     T *out = static_cast<T *>(a.Y) + i * a.ldy + k0;
-    const int y_place = place_of(out, mixed);
+    const bool y_whole = whole_pieces<A>(out, together);
     int8_t *q = a.q + i * a.ldq + k0;
     uint8_t *exps = a.exps + i * a.lde;
     const int kq = (K + 15) / 16 * 16 - k0;
@@ -168,7 +168,7 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
                 load_params(beta + j * bstep, aligned, n, b);
 #pragma unroll
                 for (int e = 0; e < H; ++e) y[e] = __ffma2_rn(x[u][e], g[e], b[e]);
-                store_piece<T, A>(out + j * step, pack16<T>(y), n, y_place);
+                store_piece<T, A>(out + j * step, pack16<T>(y), n, y_whole);
             }
         }
         if constexpr (kKeep) {

@@ -149,3 +149,17 @@ def test_weight_grad_matches_differences(cuda_device):
         assert abs(d - (f64(dW) * dw).sum()) <= 1e-5 * np.abs(f64(dW) * dw).sum()
         d = (loss(W, b + 1e-3 * dbv) - loss(W, b - 1e-3 * dbv)) / 2e-3
         assert abs(d - (f64(db) * dbv).sum()) <= 1e-5 * np.abs(f64(db) * dbv).sum()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("N,K,F", [(700, 260, 192), (333, 640, 192), (1000, 520, 320), (65, 40, 448),
+                                   (1, 600, 192), (130, 1100, 704)])
+def test_weight_grad_boxes_past_the_last_column(cuda_device, N, K, F, dtype):
+    """F a multiple of 64, the width of a copied part of dZ's rows, but not of the column tile: the
+    last box reaches past F. Rows with a stride above F, whose padding is NaN, and without one."""
+    q, exps, v, dz = case(N, K, F, dtype, N + F, cuda_device)
+    for pad in (0, 16):
+        dZ, _ = strided(dz, pad, 0, cuda_device)
+        dW, db = B.checkpoint_weight_grad(q, exps, dZ)
+        check(dW, db, v, np.ones(K), np.zeros(K), f64(dz), f"{N}x{K}x{F}+{pad}")
+    assert B.device_timeouts() == 0
