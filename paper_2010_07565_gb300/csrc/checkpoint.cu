@@ -48,16 +48,18 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
     constexpr int V = kPiece<T>, H = V / 2;
     const Place<V, J, R> at(tpr, parts);
     const int K = a.K, left = K - at.k0;
-    uint4 w[R][J];
+    Raw<A> w[R][J];
+    bool odd[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const T *row = static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0;
         const bool whole = whole_pieces<A>(row, tpr >= 32);
+        odd[r] = odd_pieces<A>(row);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            w[r][j] = make_uint4(0u, 0u, 0u, 0u);
+            w[r][j] = raw_zero<A>();
             if (at.i[r] < a.N && left > j * at.step)
-                w[r][j] = load_piece<T, A>(row + j * at.step, left - j * at.step, whole);
+                w[r][j] = load_piece<T, A>(row + j * at.step, left - j * at.step, whole, odd[r]);
         }
     }
     // Past K a piece is zeros and so is its q.
@@ -68,7 +70,7 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
         uint32_t own[J], top[J];
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            unpack16<T>(w[r][j], x[j]);
+            unpack16<T>(settled<A>(w[r][j], odd[r]), x[j]);
             own[j] = top_bits(x[j]);
         }
         group_tops<32 / V>(own, top);

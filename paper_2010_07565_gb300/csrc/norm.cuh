@@ -27,18 +27,35 @@ template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 // ---- 16 bytes of a row --------------------------------------------------------------------
 // Rows aligned to 8 bytes lie at 0 or 8 of 16, each row at the same for all its pieces: `whole`,
 // by which its pieces are one access or two, is a branch that the row's threads take together
-// (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 -> 317 us, backward 305 -> 247). Not
+// (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 -> 309 us, backward 305 -> 247). Not
 // so where a warp holds several rows, which would part (90,863 x 55 columns: 37 -> 51 us), and not
 // by the four places of rows aligned to 4 bytes, whose code is too long (100,000 x 601 fp32:
 // backward 132 -> 310 us).
 template <int A> __device__ __forceinline__ bool whole_pieces(const void *row, bool together) {
     return A == 8 && together && (reinterpret_cast<uintptr_t>(row) & 15) == 0;
 }
-template <int A> __device__ __forceinline__ uint4 load16(const void *p, bool whole) {
+
+// 16 bytes as they were read. A piece of a row that is aligned to 2 bytes may start 2 bytes past a
+// word (`odd`): it is read as the three words between and a half at each end, and joined by
+// settled(), later: a use behind each load would wait for it (100,000 x 601 bf16: backward from
+// the checkpoint 238 -> 203 us, from its input 323 -> 245).
+struct OddPiece {
+    uint4 w;                 // odd: three words and the half before them
+    uint32_t end;            // odd: the half behind them
+};
+template <int A> using Raw = typename std::conditional<A == 2, OddPiece, uint4>::type;
+template <int A> __device__ __forceinline__ Raw<A> raw_zero() {
+    if constexpr (A == 2) return {make_uint4(0u, 0u, 0u, 0u), 0u};
+    else return make_uint4(0u, 0u, 0u, 0u);
+}
+template <int A> __device__ __forceinline__ bool odd_pieces(const void *row) {
+    return A == 2 && (reinterpret_cast<uintptr_t>(row) & 2) != 0;
+}
+template <int A> __device__ __forceinline__ Raw<A> load16(const void *p, bool whole, bool odd) {
     if constexpr (A == 16) {
         return *static_cast<const uint4 *>(p);
     } else if constexpr (A == 8) {
-        if (whole) return load16<16>(p, true);
+        if (whole) return *static_cast<const uint4 *>(p);
         const uint2 *q = static_cast<const uint2 *>(p);
         const uint2 a = q[0], b = q[1];
         return make_uint4(a.x, a.y, b.x, b.y);
@@ -46,13 +63,19 @@ template <int A> __device__ __forceinline__ uint4 load16(const void *p, bool who
         const uint32_t *q = static_cast<const uint32_t *>(p);
         return make_uint4(q[0], q[1], q[2], q[3]);
     } else {
-        // 2 bytes past a word: the words between, and a half at each end.
-        if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) return load16<4>(p, false);
+        if (!odd) return {load16<4>(p, false, false), 0u};
         const uint16_t *h = static_cast<const uint16_t *>(p);
         const uint32_t *q = reinterpret_cast<const uint32_t *>(h + 1);
-        const uint32_t e0 = h[0], x0 = q[0], x1 = q[1], x2 = q[2], e7 = h[7];
-        return make_uint4(e0 | (x0 << 16), __byte_perm(x0, x1, 0x5432), __byte_perm(x1, x2, 0x5432),
-                          (x2 >> 16) | (e7 << 16));
+        return {make_uint4(q[0], q[1], q[2], h[0]), h[7]};
+    }
+}
+template <int A> __device__ __forceinline__ uint4 settled(const Raw<A> &r, bool odd) {
+    if constexpr (A == 2) {
+        if (!odd) return r.w;
+        return make_uint4(__byte_perm(r.w.w, r.w.x, 0x5410), __byte_perm(r.w.x, r.w.y, 0x5432),
+                          __byte_perm(r.w.y, r.w.z, 0x5432), __byte_perm(r.w.z, r.end, 0x5432));
+    } else {
+        return r;
     }
 }
 template <int A> __device__ __forceinline__ void store16(void *p, uint4 v, bool whole) {
@@ -108,8 +131,17 @@ template <typename T> __device__ __forceinline__ void store_some(T *p, uint4 v, 
         }
 }
 template <typename T, int A>
-__device__ __forceinline__ uint4 load_piece(const T *p, int n, bool whole) {
-    return n >= kPiece<T> ? load16<A>(p, whole) : load_some(p, n);
+__device__ __forceinline__ Raw<A> load_piece(const T *p, int n, bool whole, bool odd) {
+    if (n >= kPiece<T>) return load16<A>(p, whole, odd);
+    const uint4 v = load_some(p, n);
+    if constexpr (A == 2) {
+        if (!odd) return {v, 0u};
+        return {make_uint4(__byte_perm(v.x, v.y, 0x5432), __byte_perm(v.y, v.z, 0x5432),
+                           __byte_perm(v.z, v.w, 0x5432), v.x & 0xFFFFu),
+                v.w >> 16};
+    } else {
+        return v;
+    }
 }
 template <typename T, int A>
 __device__ __forceinline__ void store_piece(T *p, uint4 v, int n, bool whole) {

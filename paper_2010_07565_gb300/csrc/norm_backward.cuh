@@ -65,12 +65,13 @@ __global__ void __launch_bounds__(kRowThreads) param_any_kernel(const BackwardAr
 }
 
 // What a row's pieces are read as: dy, and x or the checkpoint's bytes.
-template <int J, int H, bool kKept> struct RawRow {
-    uint4 dy[J];
-    uint4 x[kKept ? 1 : J];
+template <int A, int J, int H, bool kKept> struct RawRow {
+    Raw<A> dy[J];
+    Raw<A> x[kKept ? 1 : J];
     QPiece<H> q[kKept ? J : 1];
     uint8_t b[kKept ? J : 1];
     float rstd, mean;
+    bool dy_odd, x_odd;
 };
 
 // Rows in registers (norm.cuh); a.chunks blocks, block b takes the sets of rows b, b + chunks,
@@ -96,15 +97,16 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
     const int gstep = a.gamma ? step : 0;
 
     const bool together = kWarp || tpr >= 32;
-    auto load = [&](int64_t i, RawRow<J, H, kKept> &r) {
+    auto load = [&](int64_t i, RawRow<A, J, H, kKept> &r) {
         if (i >= a.N) return;
         const T *dy = static_cast<const T *>(a.dY) + i * a.lddy + k0;
         const bool dy_whole = whole_pieces<A>(dy, together);
+        r.dy_odd = odd_pieces<A>(dy);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (j < kFull) r.dy[j] = load16<A>(dy + j * step, dy_whole);
+            if (j < kFull) r.dy[j] = load16<A>(dy + j * step, dy_whole, r.dy_odd);
             else if (left > j * step)
-                r.dy[j] = load_piece<T, A>(dy + j * step, left - j * step, dy_whole);
+                r.dy[j] = load_piece<T, A>(dy + j * step, left - j * step, dy_whole, r.dy_odd);
         }
         if constexpr (kKept) {
             const int8_t *q = a.q + i * a.ldq + k0;
@@ -118,11 +120,12 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
         } else {
             const T *x = static_cast<const T *>(a.X) + i * a.ldx + k0;
             const bool x_whole = whole_pieces<A>(x, together);
+            r.x_odd = odd_pieces<A>(x);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                if (j < kFull) r.x[j] = load16<A>(x + j * step, x_whole);
+                if (j < kFull) r.x[j] = load16<A>(x + j * step, x_whole, r.x_odd);
                 else if (left > j * step)
-                    r.x[j] = load_piece<T, A>(x + j * step, left - j * step, x_whole);
+                    r.x[j] = load_piece<T, A>(x + j * step, left - j * step, x_whole, r.x_odd);
             }
             r.mean = a.mean[i];
         }
@@ -131,13 +134,13 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
 
     const int64_t stride = int64_t(a.chunks) * rows;
     int turn = 0;
-    RawRow<J, H, kKept> next;
+    RawRow<A, J, H, kKept> next;
     if (kAhead) load(int64_t(blockIdx.x) * rows + slot, next);
     for (int64_t i0 = int64_t(blockIdx.x) * rows; i0 < a.N; i0 += stride) {
         const int64_t i = i0 + slot;
         const bool live = i < a.N;
         if (kWarp && !live) break;
-        RawRow<J, H, kKept> r;
+        RawRow<A, J, H, kKept> r;
         if (kAhead) {
             r = next;
             load(i + stride, next);
@@ -152,11 +155,11 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
         float2 gk[kHold ? J : 1][H], hk[kHold ? J : 1][H];
         const float rstd = r.rstd;
         auto take = [&](int j, int n, float2 (&d)[H], float2 (&h)[H], float2 (&m)[H]) {
-            unpack16<T>(r.dy[j], d);
+            unpack16<T>(settled<A>(r.dy[j], r.dy_odd), d);
             if constexpr (kKept) {
                 dequantise_piece<H>(r.q[j], unpack_factor(r.b[j]), h);
             } else {
-                unpack16<T>(r.x[j], h);
+                unpack16<T>(settled<A>(r.x[j], r.x_odd), h);
 #pragma unroll
                 for (int e = 0; e < H; ++e)
                     h[e] = __fmul2_rn(__fadd2_rn(h[e], both(-r.mean)), both(rstd));

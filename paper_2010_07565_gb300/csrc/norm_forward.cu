@@ -4,7 +4,7 @@
 //   xhat = (x - mean) rstd,  y = gamma xhat + beta
 //
 // Bound by memory: a row is read once into registers and written once, the checkpoint with
-// it. 232,965 x 602 fp32 with the checkpoint: 317 us, 5.3 TB/s (0.79 of a copy's rate; the
+// it. 232,965 x 602 fp32 with the checkpoint: 309 us, 5.5 TB/s (0.81 of a copy's rate; the
 // issue slots are next, and rows of 2408 bytes share sectors of 32); 8191 x 8192 fp16: 59 us, 4.5 TB/s (L1 at 71 %, which reads gamma and beta for every row).
 // The variance is the mean square of x - mean over the row in registers (never
 // E[x^2] - mean^2, which cancels where a row's level is above its spread).
@@ -98,14 +98,18 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
     // The row as it was read: 16-bit elements take half the registers that way, so that all
     // loads are under way at once, and are expanded for each use.
     uint4 w[J];
+    Raw<A> raw[J];
     const bool together = kWarp || tpr >= 32;
-    const bool x_whole = whole_pieces<A>(row, together);
+    const bool x_whole = whole_pieces<A>(row, together), x_odd = odd_pieces<A>(row);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        w[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (j < kFull) w[j] = load16<A>(row + j * step, x_whole);
-        else if (left > j * step) w[j] = load_piece<T, A>(row + j * step, left - j * step, x_whole);
+        raw[j] = raw_zero<A>();
+        if (j < kFull) raw[j] = load16<A>(row + j * step, x_whole, x_odd);
+        else if (left > j * step)
+            raw[j] = load_piece<T, A>(row + j * step, left - j * step, x_whole, x_odd);
     }
+#pragma unroll
+    for (int j = 0; j < J; ++j) w[j] = settled<A>(raw[j], x_odd);
     float2 s2 = both(0.0f);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
