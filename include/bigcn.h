@@ -623,9 +623,10 @@ bigcn_status bigcn_checkpoint_unpack(int32_t dtype, const int8_t *q, int64_t ldq
  *   xhat_ik = (x_ik - mean_i) rstd_i,   Y_ik = gamma_k xhat_ik + beta_k
  *
  * X, Y   N x K of `dtype`, row strides ldx, ldy >= K; Y rounded once.
- * gamma, beta   K fp32, each nullable (1 and 0).   eps finite, >= 0 (0 with a constant
- *        row divides by zero: that row is NaN).
- * mean, rstd   N fp32 each, each nullable: the backward's inputs.
+ * gamma, beta   K fp32, each nullable (1 and 0).   eps finite, >= 0 (0 with a row that is
+ *        constant, as far as fp32 sums tell, divides by zero: that row is NaN).
+ * mean, rstd   N fp32 each, each nullable: the backward's inputs. mean is the row's to
+ *        fp32's rounding, so that a constant row's is its value and its xhat 0.
  * q, exps (nullable, both or neither)   receive the checkpoint of xhat.
  * 0 <= N < 2^31, 1 <= K <= 2^30. No output may overlap another or an input.
  */

@@ -347,12 +347,12 @@ __device__ __forceinline__ void row_sum(float (&v)[kN], int tpr, float (*red)[kM
 #pragma unroll
         for (int n = 0; n < kN; ++n) red[n][warp] = v[n];
     __syncthreads();
+    // Every warp adds the row's warps alike, a power of two of them, in a few instructions a value.
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
-        float s = 0.0f;
-        for (int w = 0; w < warps; ++w) s += red[n][first + w];
-        v[n] = s;
-    }
+    for (int n = 0; n < kN; ++n) v[n] = red[n][first + (threadIdx.x & (warps - 1))];
+    for (int o = warps >> 1; o > 0; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) v[n] += __shfl_xor_sync(kFullMask, v[n], o);
 }
 
 // Sums of a block of kRowThreads, the same for every thread; warps added in order.

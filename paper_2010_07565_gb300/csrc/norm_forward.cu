@@ -6,8 +6,11 @@
 // Bound by memory: a row is read once into registers and written once, the checkpoint with
 // it. 232,965 x 602 fp32 with the checkpoint: 309 us, 5.5 TB/s (0.81 of a copy's rate; the
 // issue slots are next, and rows of 2408 bytes share sectors of 32); 8191 x 8192 fp16: 59 us, 4.5 TB/s (L1 at 71 %, which reads gamma and beta for every row).
-// The variance is the mean square of x - mean over the row in registers (never
-// E[x^2] - mean^2, which cancels where a row's level is above its spread).
+// The mean and the variance are those of d = x - m0 over the row in registers, m0 = sum x / K
+// (never E[x^2] - mean^2, which cancels where a row's level is above its spread). m0 itself is off by
+// some ulps, of the sum and of 1 / K, and an ulp of 1000 is 0.02 of xhat in a constant row (eps =
+// 1e-5): with the mean of d added, the mean is off by its rounding to fp32 alone, and that of a
+// constant row is its value.
 #include <cmath>
 
 #include "norm.cuh"
@@ -33,6 +36,18 @@ struct ForwardArgs {
     int64_t lde;
 };
 
+// The row's mean and variance from m0, S1 = sum d and S2 = sum d^2: m0 + S1 / K and S2 / K - (S1 / K)^2.
+// The difference cancels only where the spread is below m0's own error, some ulps of the row's
+// level. In a constant row it is what the rounding of the sums leaves, at most 3 (K / 32 + 40) u of
+// S2 (u = 2^-24; rows of 16384 columns: 2^-13.2; the threads of longer ones add K / 256): taken for 0.
+// (A NaN stays one.)
+__device__ __forceinline__ void finish_moments(float (&s)[2], int K, float inv_k, float &mean,
+                                               float &variance) {
+    const float c = s[0] * inv_k, left = fmaf(-s[0], c, s[1]);
+    mean += c;
+    variance = left < s[1] * fmaf(float(K), 0x1p-29f, 0x1p-13f) ? 0.0f : left * inv_k;
+}
+
 // Rows that do not fit registers (more than 8192 fp32 or 16384 16-bit columns): a block per
 // row, which walks it three times; the later walks find it in L1 or L2.
 template <typename T>
@@ -44,17 +59,18 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
     for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
         const T *x = static_cast<const T *>(a.X) + i * a.ldx;
         T *y = static_cast<T *>(a.Y) + i * a.ldy;
-        float s[1] = {0.0f};
-        for (int k = threadIdx.x; k < K; k += kRowThreads) s[0] += to_f32(x[k]);
-        block_sum(s);
-        const float mean = s[0] * inv_k;
-        s[0] = 0.0f;
+        float s0[1] = {0.0f}, s[2] = {0.0f, 0.0f}, variance;
+        for (int k = threadIdx.x; k < K; k += kRowThreads) s0[0] += to_f32(x[k]);
+        block_sum(s0);
+        float mean = s0[0] * inv_k;
         for (int k = threadIdx.x; k < K; k += kRowThreads) {
             const float d = to_f32(x[k]) - mean;
-            s[0] = fmaf(d, d, s[0]);
+            s[0] += d;
+            s[1] = fmaf(d, d, s[1]);
         }
         block_sum(s);
-        const float rstd = 1.0f / sqrtf(s[0] * inv_k + a.eps);
+        finish_moments(s, K, inv_k, mean, variance);
+        const float rstd = 1.0f / sqrtf(variance + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[i] = mean;
             if (a.rstd) a.rstd[i] = rstd;
@@ -84,7 +100,7 @@ template <typename T, int A, int J, bool kKeep, bool kWarp>
 __global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 4 : 2)
 forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool aligned) {
     constexpr int V = kPiece<T>, H = V / 2, kFull = full_pieces(V, J);
-    __shared__ float red[2][1][kMostRowThreads / 32];
+    __shared__ float red0[1][kMostRowThreads / 32], red[2][kMostRowThreads / 32];
     const int tpr = kWarp ? 32 : row_threads;
     const int t = threadIdx.x & (tpr - 1);
     const int64_t i = int64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
@@ -118,9 +134,9 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
 #pragma unroll
         for (int e = 0; e < H; ++e) s2 = __fadd2_rn(s2, x[e]);
     }
-    float s[1] = {s2.x + s2.y};
-    row_sum<kWarp>(s, tpr, red[0]);
-    const float mean = s[0] * inv_k;
+    float s0[1] = {s2.x + s2.y}, variance;
+    row_sum<kWarp>(s0, tpr, red0);
+    float mean = s0[0] * inv_k;
     // x - mean of piece j, zeros past the row.
     auto centred = [&](int j, float2 (&x)[H]) {
         unpack16<T>(w[j], x);
@@ -128,18 +144,23 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
         for (int e = 0; e < H; ++e) x[e] = __fadd2_rn(x[e], both(-mean));
         if (j >= kFull && left < j * step + V) clear_from(x, left - j * step);
     };
+    float2 s1 = both(0.0f);
     s2 = both(0.0f);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         float2 x[H];
         centred(j, x);
 #pragma unroll
-        for (int e = 0; e < H; ++e) s2 = __ffma2_rn(x[e], x[e], s2);
+        for (int e = 0; e < H; ++e) {
+            s1 = __fadd2_rn(s1, x[e]);
+            s2 = __ffma2_rn(x[e], x[e], s2);
+        }
     }
-    s[0] = s2.x + s2.y;
-    row_sum<kWarp>(s, tpr, red[1]);
+    float s[2] = {s1.x + s1.y, s2.x + s2.y};
+    row_sum<kWarp>(s, tpr, red);
+    finish_moments(s, K, inv_k, mean, variance);
     if (!kWarp && !kKeep && !live) return;      // (with a checkpoint lanes still meet below)
-    const float rstd = 1.0f / sqrtf(s[0] * inv_k + a.eps);
+    const float rstd = 1.0f / sqrtf(variance + a.eps);
     if (live && t == 0) {
         if (a.mean) a.mean[i] = mean;
         if (a.rstd) a.rstd[i] = rstd;
