@@ -588,8 +588,8 @@ typedef enum bigcn_dtype {
  *   v[i,k] = q[i,k] * 2^(exps[i, k/32] - 127),   q in [-127, 127],
  *
  * exps the least byte >= 1 by which the group's largest magnitude rounds (to nearest
- * even) to at most 127; a group that holds a NaN or an infinity has byte 255 and NaN
- * values. |v - x| is at most half a step: 1/127.5 of the group's largest magnitude, or
+ * even) to at most 127; a group that holds a NaN or an infinity has byte 255, q 0 and
+ * NaN values (readers go by the byte). |v - x| is at most half a step: 1/127.5 of the group's largest magnitude, or
  * 2^-127 in groups below 2^-120. Values have 7 significant bits, exact in bf16.
  *
  * q      N rows of ldq bytes, 16-byte aligned, ldq >= K a multiple of 16.

@@ -81,7 +81,7 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
         for (int j = 0; j < J; ++j) {
             if (j * at.step >= kq) break;
             const uint32_t b = scale_byte(top[j]);
-            *reinterpret_cast<QPiece<H> *>(q + j * at.step) = quantise_piece(x[j], pack_factor(b));
+            *reinterpret_cast<QPiece<H> *>(q + j * at.step) = quantise_piece(x[j], b);
             if ((threadIdx.x & (32 / V - 1)) == 0 && j * at.step < left)
                 exps[unsigned(at.k0 + j * at.step) / kGroup] = uint8_t(b);
         }

@@ -6,7 +6,7 @@
 // amax / 127 costs at most one of the 8 bits and buys three things: a byte per
 // scale, a division-free packing whose result does not depend on rounding, and
 // values of 7 significant bits, exact in bf16 and so exact as an operand of the
-// tensor cores. A group with a NaN or an infinity has b = 255; its values are NaN.
+// tensor cores. A group with a NaN or an infinity has b = 255 and q = 0; its values are NaN.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
 }
 
 // 2^(127 - b), which scales a group's values to [-127.5, 127.5). (An infinity for a NaN
-// group, whose q do not matter.)
+// group, whose q are written 0 without it.)
 __device__ __forceinline__ float pack_factor(uint32_t b) {
     return __uint_as_float(0x7F000000u - (b << 23));
 }

@@ -263,9 +263,12 @@ __device__ __forceinline__ uint32_t quantise4(float2 a, float2 b, float f) {
     return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040),
                        __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
-template <int H> __device__ __forceinline__ QPiece<H> quantise_piece(const float2 (&v)[H], float f) {
-    if constexpr (H == 2) return quantise4(v[0], v[1], f);
-    else return make_uint2(quantise4(v[0], v[1], f), quantise4(v[2], v[3], f));
+// By the group's scale byte; zeros in a NaN group, whose last columns may lie behind the row.
+template <int H> __device__ __forceinline__ QPiece<H> quantise_piece(const float2 (&v)[H], uint32_t b) {
+    const float f = pack_factor(b);
+    const uint32_t keep = b == kNanByte ? 0u : ~0u;
+    if constexpr (H == 2) return quantise4(v[0], v[1], f) & keep;
+    else return make_uint2(quantise4(v[0], v[1], f) & keep, quantise4(v[2], v[3], f) & keep);
 }
 __device__ __forceinline__ void dequantise4(uint32_t w, float f, float2 &a, float2 &b) {
     const uint32_t u = w ^ 0x80808080u;

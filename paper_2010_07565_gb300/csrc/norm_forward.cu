@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
             }
             if (a.q) {
                 const uint32_t b = scale_byte(__reduce_max_sync(kFullMask, abs_bits(v)));
-                if (k < kq) a.q[i * a.ldq + k] = int8_t(q_low(v, pack_factor(b)));
+                if (k < kq) a.q[i * a.ldq + k] = int8_t(b == kNanByte ? 0u : q_low(v, pack_factor(b)));
                 if (lane == 0) a.exps[i * a.lde + g] = uint8_t(b);
                 if (g == groups - 1 && g + 1 + lane < padded) a.exps[i * a.lde + g + 1 + lane] = 0;
             }
@@ -203,7 +203,7 @@ forward_rows_kernel(const ForwardArgs a, const int row_threads, const bool align
                 const int j = j0 + u;
                 if (j >= J || (!kWarp && !live) || (j >= kFull && j * step >= kq)) continue;
                 const uint32_t b = scale_byte(top[u]);
-                *reinterpret_cast<QPiece<H> *>(q + j * step) = quantise_piece(x[u], pack_factor(b));
+                *reinterpret_cast<QPiece<H> *>(q + j * step) = quantise_piece(x[u], b);
                 if ((t & (32 / V - 1)) == 0 && j * step < left)
                     exps[unsigned(k0 + j * step) / kGroup] = uint8_t(b);
             }
