@@ -140,8 +140,11 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        # torch.cuda.current_stream().cuda_stream without the Stream object (1 us against 4)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        # The private calls give the same handle without the Stream object (1 us against 4). Where
+        # CUDA is not up, or not in this torch, its public call brings it up or says why not.
+        if torch.cuda.is_initialized():
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
