@@ -683,7 +683,8 @@ size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_
  * Both factors enter the sums exactly (fp32 gradients to within 2^-23) and the sums
  * are fp32, over runs of rows added in a fixed order: deterministic on one device.
  * The tensor-core product waits on shared-memory barriers a bounded number of times:
- * where a wait runs out its part of dW is not written (bigcn_device_timeouts).
+ * where a wait runs out, the entries of dW and db whose sums lack its rows are NaN
+ * (0 waits in correct operation; bigcn_device_timeouts counts them).
  * 0 <= N < 2^31, 1 <= K, F <= 2^30. No output may overlap another or an input.
  */
 bigcn_status bigcn_checkpoint_weight_grad(int32_t dtype, const int8_t *q, int64_t ldq,

@@ -48,6 +48,7 @@
 //     dZ is read by four groups of tiles, three times of four from L2.
 //   small calls (2708 x 1433 x 64 fp32: 14.4 us): this kernel's and the second's latencies.
 #include "checkpoint.cuh"
+#include "checkpoint_runs.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
 
@@ -489,11 +490,16 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
         if (!ok) *stopv = 1u;
     }
 
-    // Every MMA has ended once `done` completes. A CTA whose waits ran out writes nothing.
+    // Every MMA has ended once `done` completes. A CTA whose waits ran out leaves NaN for its sums.
     const bool ended = mbar_wait(smem_addr(&done), 0u);
     const bool ok = __syncthreads_and(ended && *stopv == 0u) != 0;
-    if (!ok && tid == 0) atomicAdd(&g_grad_timeouts, 1u);
+    float *const own_colsum = p.colsum + int64_t(run) * p.nt * NT + n0 + 64 * own;
+    const int own_cols = sums_cols ? min(64, cols - 64 * own) : 0;
     allow_dependent_launch();
+    if (!ok) {
+        if (tid == 0) atomicAdd(&g_grad_timeouts, 1u);
+        abandon_run(p.partial, p.tiles, p.parts_full, NT, ny, tile0, mt, run, own_colsum, own_cols);
+    }
     if (ok && warp < kWorkerWarps) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int quad = warp & 3, quarter = warp >> 2, f = 32 * quad + lane;
@@ -503,8 +509,7 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
             if (t >= mt) break;
             uint32_t sum[32];
             tmem_ld32(tmem + (uint32_t(32 * quad) << 16) + uint32_t(kAccCols + at), sum);
-            float *dst = p.partial +
-                         (((int64_t(ny) * p.tiles + tile0 + t) * p.parts_full + run) * NT + col) * 128 + f;
+            float *dst = run_sums(p.partial, p.tiles, p.parts_full, NT, ny, tile0 + t, run) + col * 128 + f;
 #pragma unroll
             for (int j = 0; j < 32; ++j)
                 if (col + j < cols) dst[j * 128] = __uint_as_float(sum[j]);
@@ -522,10 +527,10 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
                 colpart[warp][32 + lane] = colsum[1];
             }
             asm volatile("bar.sync 1, 512;" ::: "memory");
-            if (tid < 64 && 64 * own + tid < cols) {
+            if (tid < own_cols) {
                 float t = 0.0f;
                 for (int w = 0; w < kWorkerWarps; ++w) t += colpart[w][tid];
-                p.colsum[int64_t(run) * p.nt * NT + n0 + 64 * own + tid] = t;
+                own_colsum[tid] = t;
             }
         }
     }
@@ -534,82 +539,6 @@ grad_rows_kernel(const __grid_constant__ GradParams p) {
     if (warp == kMmaWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                      "r"(2 * kAccCols));
-}
-
-// The runs' sums added in order, and gamma, beta: a block takes four columns of a tile of 128
-// features. A warp adds every eighth run (four features a lane), the eight sums are added in
-// order.
-constexpr int kSumThreads = 256;
-struct GradSumParams {
-    const float *partial;
-    const float *colsum;
-    int64_t tiles;
-    int64_t groups;
-    int parts_full, parts_last;
-    int mt;
-    int NT;
-    int padded;              // nt * NT
-    int K;
-    int F;
-    const float *gamma;
-    const float *beta;
-    float *dW;
-    int64_t lddw;
-    float *db;
-};
-
-__global__ void __launch_bounds__(kSumThreads) grad_sum_kernel(const GradSumParams p) {
-    __shared__ __align__(16) float part[8][4][128];
-    __shared__ float cpart[64][4];
-    __shared__ float csum[4];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int64_t tile = blockIdx.x % p.tiles;
-    const int j0 = int(blockIdx.x / p.tiles) * 4, ny = j0 / p.NT, col0 = j0 % p.NT;
-    const int runs = tile / p.mt == p.groups - 1 ? p.parts_last : p.parts_full;
-    // The group that summed these columns.
-    const int cruns = col0 / 64 == p.groups - 1 ? p.parts_last : p.parts_full;
-    grid_dependency_wait();
-    {
-        const int c = tid & 3;
-        float t = 0.0f;
-        if (j0 + c < p.F)
-            for (int s = tid >> 2; s < cruns; s += 64) t += p.colsum[int64_t(s) * p.padded + j0 + c];
-        cpart[tid >> 2][c] = t;
-    }
-    float4 acc[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const float4 *src = reinterpret_cast<const float4 *>(
-                            p.partial + ((int64_t(ny) * p.tiles + tile) * p.parts_full * p.NT + col0) * 128) +
-                        lane;
-    for (int s = warp; s < runs; s += 8)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (j0 + c < p.F) {
-                const float4 v = src[(int64_t(s) * p.NT + c) * 32];
-                acc[c].x += v.x, acc[c].y += v.y, acc[c].z += v.z, acc[c].w += v.w;
-            }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) *reinterpret_cast<float4 *>(&part[warp][c][4 * lane]) = acc[c];
-    __syncthreads();
-    if (tid < 4) {
-        float t = 0.0f;
-        const int used = min(cruns, 64);
-        for (int s = 0; s < used; ++s) t += cpart[s][tid];
-        csum[tid] = t;
-        if (tile == 0 && p.db && j0 + tid < p.F) p.db[j0 + tid] = t;
-    }
-    __syncthreads();
-    for (int q = tid; q < 512; q += kSumThreads) {
-        const int f = q >> 2, c = q & 3;
-        const int64_t k = tile * 128 + f;
-        if (k >= p.K || j0 + c >= p.F) continue;
-        float t = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) t += part[w][c][f];
-        const float g = p.gamma ? __ldg(p.gamma + k) : 1.0f;
-        p.dW[k * p.lddw + j0 + c] = p.beta ? fmaf(g, t, __ldg(p.beta + k) * csum[c]) : g * t;
-    }
 }
 
 // How a call is cut into CTAs.
