@@ -573,8 +573,8 @@ bigcn_status bigcn_spmm_prescaled_rows(const int64_t *rowptr, const int32_t *col
  * Tensors of these calls are of one of three element types; parameters (gamma,
  * beta), statistics and the parameters' gradients are fp32 throughout, as are all
  * sums. Pointers are aligned to their element. NaN and infinities are data here: a
- * row that holds one gives NaN in that row's outputs (and in the gradients that sum
- * over rows) and touches no other row.
+ * row that holds one gives NaN in that row's outputs (an infinite gradient NaN or
+ * infinities, there and in the gradients that sum over rows) and touches no other row.
  */
 typedef enum bigcn_dtype {
     BIGCN_F32 = 0,
@@ -680,8 +680,10 @@ size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_
  * dW     K x F fp32, row stride lddw >= F.   db  F fp32, nullable.
  * workspace  >= bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F) bytes, 256-byte
  *            aligned, overlapping nothing else.
- * Both factors enter the sums exactly (fp32 gradients to within 2^-23) and the sums
- * are fp32, over runs of rows added in a fixed order: deterministic on one device.
+ * Both factors enter the sums exactly, but for fp32 gradients below 2^-110: those to within
+ * 2^-134. The sums are fp32, at most 64 additions in a row the tensor core's, which truncate
+ * (about 1e-6 of the result together), over runs of rows added in a fixed order: deterministic
+ * on one device.
  * The tensor-core product waits on shared-memory barriers a bounded number of times:
  * where a wait runs out, the entries of dW and db whose sums lack its rows are NaN
  * (0 waits in correct operation; bigcn_device_timeouts counts them).

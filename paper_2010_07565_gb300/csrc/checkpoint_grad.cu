@@ -5,8 +5,8 @@
 //
 // The sum over the rows i runs on the tensor cores (tcgen05, bf16 operands, fp32
 // accumulators), and nothing is rounded on the way in: v = q 2^e has 7 significant bits
-// and is a bf16; dZ is one bf16 part (bf16), two (fp16: 8 + 3 bits, exact) or three (fp32,
-// within 2^-23 of it).
+// and is a bf16; dZ is one bf16 part (bf16), two (fp16: 8 + 3 bits) or three (fp32: 8 + 8 + 8
+// bits, exact above 2^-110, within 2^-134 below).
 //
 // Operands. M = 128 features a tile, N = the columns, the contraction over 32 or 64 rows a
 // stage. Both matrices are row-major, i.e. their features and columns lie along memory

@@ -98,7 +98,8 @@ __device__ __forceinline__ void tmem_wait_st() {
 }
 
 // Two values as three bf16 parts each, in pairs: the upper halves of v, of what is left
-// (exact), and the rounding of what is left then; together within 2^-23 of v. A NaN or an
+// (exact), and what is left then, 8 bits of the 24 each: together v, but where the last part's
+// bits pass below bf16's least subnormal, 2^-133 (|v| < 2^-110), within 2^-134. A NaN or an
 // infinity leaves a NaN in the middle part.
 __device__ __forceinline__ void bf16_parts(float v0, float v1, uint32_t &hi, uint32_t &mid,
                                            uint32_t &lo) {
