@@ -131,13 +131,30 @@ class GCN2Forward:
         B.bigcn_spmm_prescaled(self.rowptr, self.colidx, self.Z2, self.logits_steps)
 
 
+class NormedScratch:
+    """What layers of a stack need only within a call: the largest layer's Y (and dY), Z (and
+    G), dX and workspace, for ``sizes``, the layers' (N, K, F). Layers that are given one share
+    it, on one stream; dX holds a layer's gradient until the layer below has run its backward."""
+
+    def __init__(self, sizes, device):
+        sizes = list(sizes)
+        e = lambda n, dtype=torch.float32: torch.empty(n, dtype=dtype, device=torch.device(device))
+        most = lambda f: max(f(*size) for size in sizes)
+        self.Y, self.dX = (e(most(lambda N, K, F: N * K)) for _ in range(2))
+        self.Z = e(most(lambda N, K, F: N * F))
+        self.workspace = e(most(lambda N, K, F: max(
+            B.bigcn_layer_norm_backward_workspace_bytes(N, K),
+            B.bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F), 1)), dtype=torch.uint8)
+
+
 class NormedLayer:
     """One layer in training, H = A~ (Y W~ + b) with Y = gamma xhat + beta the layer norm of X
     and W~ = diag(beta_j) sign(W) (the ablation that binarizes the weights only, Sec. 6.3).
 
     Between ``forward()`` and ``backward()`` it keeps xhat's 8-bit checkpoint and each row's
-    rstd: N (K + K/32 + 4) bytes in place of the 4 N K of Y, which the next layer may overwrite.
-    The one checkpoint serves both gradients that need the features:
+    rstd: N (K + K/32 + 4) bytes in place of the 4 N K of Y. Y, Z and dX are scratch, of the
+    layer's own or, for the layers of a stack, of one ``scratch`` (a :class:`NormedScratch`)
+    that they share. The one checkpoint serves both gradients that need the features:
 
         G   = A~ dH                                       (the CSR is symmetric)
         dWb = dL/dW~ = Y^T G,   db = sum_i G_i            (Algorithm 1's dL/dW~ with real features)
@@ -146,7 +163,7 @@ class NormedLayer:
 
     ``weight_gradient()`` takes dWb through the sign (Eq. bp-W)."""
 
-    def __init__(self, N: int, K: int, F: int, device, eps: float = 1e-5):
+    def __init__(self, N: int, K: int, F: int, device, eps: float = 1e-5, scratch=None):
         self.N, self.K, self.F, self.eps = N, K, F, eps
         self.device = torch.device(device)
         f32, i64 = torch.float32, torch.int64
@@ -158,17 +175,18 @@ class NormedLayer:
         self.q, self.exps = B.checkpoint_buffers(N, K, self.device)
         self.rstd = e(N)
         self.w_bits, self.w_scale = e(F, B.words_for(K), dtype=i64), e(F)
-        # scratch: free for others between calls
-        self.Y, self.Z, self.H = e(N, K), e(N, F), e(N, F)
+        self.H = e(N, F)
+        # scratch: free for other layers between calls (dX until the layer below has read it)
+        scratch = scratch or NormedScratch([(N, K, F)], self.device)
+        take = lambda t, cols: t[:N * cols].view(N, cols)
+        self.Y, self.Z, self.dX = take(scratch.Y, K), take(scratch.Z, F), take(scratch.dX, K)
+        self.workspace = scratch.workspace
         # gradients
-        self.G, self.dY, self.dX = self.Z, self.Y, e(N, K)
+        self.G, self.dY = self.Z, self.Y
         self.dWb, self.db = e(K, F), e(F)
         self.dgamma, self.dbeta = e(K), e(K)
         self.w_rows, self.w_rows_scale = e(K, B.words_for(F), dtype=i64), e(K)
         self.one, self.zero = torch.ones(K, device=self.device), torch.zeros(F, device=self.device)
-        need = max(B.bigcn_layer_norm_backward_workspace_bytes(N, K),
-                   B.bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F))
-        self.workspace = e(max(need, 1), dtype=torch.uint8)
 
     def forward(self, X, rowptr, colidx):
         """H from X (N x K fp32); enqueued on the current stream."""
