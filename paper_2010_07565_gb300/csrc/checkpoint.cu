@@ -1,7 +1,8 @@
 // Activations to 8 bits and back (bigcn_checkpoint_pack, bigcn_checkpoint_unpack): the arithmetic
 // is checkpoint.cuh's, a few operations a column; both are bound by memory. 2^20 x 512 bf16: packing
 // 247 us (0.95 of a copy's rate), unpacking 362 us (0.66: two bytes written for one read, DRAM at
-// half its rate; neither streaming stores nor more or fewer pieces a thread changed that).
+// half its rate; neither streaming stores nor more or fewer pieces a thread changed that), 395 with
+// gamma and beta.
 #include "norm.cuh"
 
 namespace bigcn {

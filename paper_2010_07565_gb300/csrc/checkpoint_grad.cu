@@ -38,15 +38,21 @@
 // the CTA that has them in shared memory anyway: of the groups of feature tiles that read the
 // same rows, group g takes the g-th 64 columns.
 //
-// What bounds it, in cycles of a stage:
-//   fp32 dZ (232,965 x 602 x 128, 32 rows: 122 us, 883 TFLOP/s of the three parts' products):
-//     about 1300, near what shared memory moves: 184 KB (48 copied and read, 40 of operands
-//     written, 96 read by the MMAs); the MMAs alone take 820. A kept in the tensor core's
-//     collector for the three parts changed nothing (131 us both ways then).
-//   bf16 dZ (2^20 x 512 x 256, 64 rows: 283 us, 970 TFLOP/s): about 1250; MMAs 545, shared memory
-//     900. A slot's way through copy, expansion and MMA takes four times that, and four slots fit;
-//     dZ is read by four groups of tiles, three times of four from L2.
-//   small calls (2708 x 1433 x 64 fp32: 14.4 us): this kernel's and the second's latencies.
+// What bounds it (cycles and times of one kernel by ncu, at 1.92 to 1.94 GHz; the call's by events):
+//   fp32 dZ (232,965 x 602 x 128, 32 rows a stage: 122 us, 883 TFLOP/s of the three parts' products):
+//     this kernel 118 us, 229,000 cycles for a CTA's 135 stages, its start and its end: 1700 a
+//     stage, in which shared memory moves 184 KB (48 copied and read, 40 of operands written, 96 read
+//     by the MMAs), 108 bytes a cycle of the 128 it has; the tensor pipe is active in 41 %. A
+//     kept in the tensor core's collector for the three parts changed nothing (131 us both ways
+//     then). The second kernel reads 17 MB of sums: 11 us alone, partly under the first's end.
+//   bf16 dZ (2^20 x 512 x 256, 64 rows a stage: 276 us, 995 TFLOP/s): this kernel 263 us, 504,000
+//     cycles for 432 stages: 1170 a stage, tensor pipe 44 %, shared memory 120 KB (940 cycles). A
+//     slot's way through copy, expansion and MMA takes four times that, and four slots fit; dZ is read
+//     by four groups of tiles, three times of four from L2. The second kernel: 11 us alone.
+//   small calls (2708 x 1433 x 64 fp32: 14.3 us): this kernel's and the second's latencies (10.7 and
+//     8.0 us alone).
+//   rows of dZ that are no multiple of 16 bytes (the workers load it, an element a lane): 232,965 x
+//     602 x 41 111 us in fp32 and 182 in bf16, 2708 x 1433 x 7 as long as x 64.
 #include "checkpoint.cuh"
 #include "checkpoint_runs.cuh"
 #include "launch.cuh"
@@ -58,7 +64,7 @@ __device__ unsigned int g_grad_timeouts;
 
 namespace {
 
-constexpr int kGradCtas = 152;          // SMs of the card
+constexpr int kGradCtas = 152;          // SMs of a GB300; the workspace query asks no device
 constexpr int kWorkers = 512;
 constexpr int kWorkerWarps = kWorkers / 32;
 constexpr int kTeams = 2;               // of workers, which take stages in turn

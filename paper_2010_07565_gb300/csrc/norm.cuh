@@ -27,7 +27,8 @@ template <typename T> constexpr int kPiece = 16 / int(sizeof(T));      // V
 // ---- 16 bytes of a row --------------------------------------------------------------------
 // Rows aligned to 8 bytes lie at 0 or 8 of 16, each row at the same for all its pieces: `whole`,
 // by which its pieces are one access or two, is a branch that the row's threads take together
-// (232,965 x 602 fp32, rows at 0 and 8 in turn: forward 355 -> 309 us, backward 305 -> 247). Not
+// (232,965 x 602 fp32, rows at 0 and 8 in turn: forward and its checkpoint read back 355 -> 309 us,
+// backward 305 -> 247). Not
 // so where a warp holds several rows, which would part (90,863 x 55 columns: 37 -> 51 us), and not
 // by the four places of rows aligned to 4 bytes, whose code is too long (100,000 x 601 fp32:
 // backward 132 -> 310 us).

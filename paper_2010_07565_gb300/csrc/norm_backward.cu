@@ -7,9 +7,12 @@
 // the source are read once and dx written once, by blocks that stay and take rows in turn;
 // each keeps its rows' sums of dy xhat and dy in the registers that hold the columns, adds
 // its threads' sums in shared memory at the end, and a second kernel adds the blocks' in
-// order. 232,965 x 602 fp32 from the checkpoint: 247 us, 5.1 TB/s (0.76 of a copy's rate); 2^20 x
-// 256 bf16: 284 us, 4.8 TB/s (0.70): 16 warps an SM, whose registers hold the columns' sums, issue
-// at half the rate and wait on memory for the rest.
+// order. 232,965 x 602 fp32 from the checkpoint: 250 us, 5.1 TB/s (0.75 of a copy's rate); 2^20 x
+// 256 bf16: 285 us, 4.7 TB/s (0.70): a row takes 16 threads with two pieces each, 118 registers a
+// thread (the columns' sums are 32 of them, the present row and the next most of the rest), so 16
+// warps an SM, which issue at half the rate and wait on memory for the rest. From the input
+// 232,965 x 602 fp32 takes 265 us (0.94). Six pieces a thread (fp32 rows of 641 to 768 columns) spill 60 to 136 bytes:
+// 200,000 x 700 at 0.74 from the input and 0.58 from the checkpoint, x 640 at 0.84.
 #include "norm_args.cuh"
 
 namespace bigcn {

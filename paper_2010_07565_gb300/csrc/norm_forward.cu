@@ -4,8 +4,9 @@
 //   xhat = (x - mean) rstd,  y = gamma xhat + beta
 //
 // Bound by memory: a row is read once into registers and written once, the checkpoint with
-// it. 232,965 x 602 fp32 with the checkpoint: 309 us, 5.5 TB/s (0.81 of a copy's rate; the
-// issue slots are next, and rows of 2408 bytes share sectors of 32); 8191 x 8192 fp16: 59 us, 4.5 TB/s (L1 at 71 %, which reads gamma and beta for every row).
+// it. 232,965 x 602 fp32 with the checkpoint: 203 us, 6.2 TB/s (0.92 of a copy's rate); 2^20 x 256
+// bf16 with it: 232 us (0.86); 8191 x 8192 fp16: 61 us, 4.4 TB/s (L1 at 73 % while a block is on an
+// SM, which reads gamma and beta for every row).
 // The mean and the variance are those of d = x - m0 over the row in registers, m0 = sum x / K
 // (never E[x^2] - mean^2, which cancels where a row's level is above its spread). m0 itself is off by
 // some ulps, of the sum and of 1 / K, and an ulp of 1000 is 0.02 of xhat in a constant row (eps =

@@ -140,7 +140,8 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 }
 
 // Four bytes from memory to shared memory, zeros where `bytes` is 0; and this thread's
-// arrival on bar once all its earlier such copies have landed.
+// arrival on bar once all its earlier such copies have landed (at once where it made none), one of
+// those that the barrier was initialised for.
 __device__ __forceinline__ void copy4(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes)
                  : "memory");
