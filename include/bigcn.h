@@ -665,6 +665,59 @@ bigcn_status bigcn_layer_norm_backward(int32_t dtype, const void *dY, int64_t N,
                                        float *dbeta, void *workspace, size_t ws_bytes,
                                        void *stream);
 
+/*
+ * The residual's addition and the root-mean-square norm of the sum:
+ *
+ *   s_ik = x_ik + r_ik (rounded once to `dtype`),   rstd_i = 1 / sqrt((1/K) sum_k s_ik^2 + eps),
+ *   shat_ik = s_ik rstd_i,   Y_ik = gamma_k shat_ik
+ *
+ * What is normalised is the rounded sum, which the stream carries on and the backward reads.
+ *
+ * X, R, S, Y   N x K of `dtype`, row strides ldx, ldr, lds, ldy >= K. R nullable (s = x; S is then
+ *        NULL too). S, Y nullable. S may take the place of R or of X: the same pointer and row stride.
+ * gamma  K fp32, nullable (1).   eps finite, >= 0 (0 with a row of zeros divides by zero: that
+ *        row is NaN).
+ * rstd   N fp32, nullable: the backward's input. Right for every finite row: where single squares
+ *        would leave fp32's range the sum is taken of scaled values (above 2^126 in magnitude rstd is
+ *        subnormal and has fewer bits).
+ * q, exps (nullable, both or neither)   receive the checkpoint of shat.
+ * A row with a NaN or an infinity (of the sum, which may pass fp16's range) has rstd NaN, and so its
+ * shat and Y. At least one output is given. 0 <= N < 2^31, 1 <= K <= 2^30. No output may overlap another
+ * or, S's place apart, an input.
+ */
+bigcn_status bigcn_rms_norm_forward(int32_t dtype, const void *X, int64_t N, int32_t K, int64_t ldx,
+                                    const void *R, int64_t ldr, const float *gamma, float eps,
+                                    void *S, int64_t lds, void *Y, int64_t ldy, float *rstd,
+                                    int8_t *q, int64_t ldq, uint8_t *exps, int64_t lde,
+                                    void *stream);
+
+/* Bytes of device workspace bigcn_rms_norm_backward needs when it returns dgamma; 0 on
+ * invalid sizes. */
+size_t bigcn_rms_norm_backward_workspace_bytes(int64_t N, int32_t K);
+
+/*
+ * Its gradients, from dY = dL/dY (N x K of `dtype`, row stride lddy), with g = gamma dY, and
+ * dS (nullable; N x K of `dtype`, row stride ldds), the sum's gradient by way of what follows it
+ * in the stream:
+ *
+ *   dX_ik = rstd_i (g_ik - shat_ik (1/K) sum_k g_ik shat_ik) + dS_ik,   dgamma_k = sum_i dY_ik shat_ik
+ *
+ * dX is the gradient of x and of r alike. shat comes from one of two places, the other NULL: from S
+ * (the forward's sum, or its X where there was no R), or from the checkpoint q, exps. rstd (N) is
+ * required. gamma nullable (1). dX (N x K of `dtype`, row stride lddx) and dgamma (K fp32) are each
+ * nullable, but not both; dS asks for dX. dX may take the place of dS: the same pointer and row stride.
+ * workspace  >= bigcn_rms_norm_backward_workspace_bytes(N, K) bytes, 256-byte aligned,
+ *            overlapping nothing else; not needed (may be NULL) when dgamma is NULL. Sums over
+ *            rows are added in a fixed order: results are deterministic on one device.
+ * No output may overlap another or, dS's place apart, an input.
+ */
+bigcn_status bigcn_rms_norm_backward(int32_t dtype, const void *dY, int64_t N, int32_t K,
+                                     int64_t lddy, const float *gamma, const void *S, int64_t lds,
+                                     const int8_t *q, int64_t ldq, const uint8_t *exps,
+                                     int64_t lde, const float *rstd, const void *dS, int64_t ldds,
+                                     void *dX, int64_t lddx, float *dgamma, void *workspace,
+                                     size_t ws_bytes, void *stream);
+
 /* Bytes of device workspace bigcn_checkpoint_weight_grad needs; 0 on invalid sizes. */
 size_t bigcn_checkpoint_weight_grad_workspace_bytes(int64_t N, int32_t K, int32_t F);
 
@@ -695,6 +748,97 @@ bigcn_status bigcn_checkpoint_weight_grad(int32_t dtype, const int8_t *q, int64_
                                           int32_t F, int64_t lddz, float *dW, int64_t lddw,
                                           float *db, void *workspace, size_t ws_bytes,
                                           void *stream);
+
+/*
+ * Rows in microscaled 4-bit floating point: each row in groups of 32 consecutive columns,
+ *
+ *   v[i,k] = m[i,k] * 2^(exps[i, k/32] - 127),   m one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign,
+ *
+ * exps the least byte >= 1 by which the group's largest magnitude rounds to at most 6, and m the
+ * nearest such number, of two as near the one of even code. A code has the sign in bit 3 and
+ * the magnitude's place in that list in bits 0-2; byte k/2 of a row holds column k's code in its
+ * low half (k even) or its high half (k odd). A group that holds a NaN or an infinity has byte 255,
+ * codes 0 and NaN values (readers go by the byte). |v - x| is at most 1/5 of |x|, or a quarter of
+ * 2^(exps - 127) where |x| is below that power.
+ *
+ * q      N rows of ldq bytes, 16-byte aligned, ldq >= 16 ceil(K/32) a multiple of 16.
+ * exps   N rows of lde bytes, 4-byte aligned, lde >= ceil(K/32) a multiple of 4.
+ * Calls write whole groups and ceil(K/32) rounded up to 4 bytes of exps; the codes past K are written
+ * 0, and have to be 0 where the product reads them; the bytes past the last group are written 0 and
+ * ignored when read. Packed here, exps are 1 to 253 or 255; readers take 0 (2^-127) and 254 too.
+ */
+
+/* X (N x K, row stride ldx >= K, `dtype` a bigcn_dtype) to 4 bits.
+ * 0 <= N < 2^31, 1 <= K <= 2^30; q and exps must not overlap each other or X. */
+bigcn_status bigcn_fp4_pack(int32_t dtype, const void *X, int64_t N, int32_t K, int64_t ldx,
+                            uint8_t *q, int64_t ldq, uint8_t *exps, int64_t lde, void *stream);
+
+/* The columns of W (K x F, row stride ldw >= F) to 4-bit rows: row j of q and exps (F of them)
+ * is column j of W. 1 <= K, F <= 2^30. */
+bigcn_status bigcn_fp4_pack_columns(int32_t dtype, const void *W, int32_t K, int32_t F, int64_t ldw,
+                                    uint8_t *q, int64_t ldq, uint8_t *exps, int64_t lde,
+                                    void *stream);
+
+/* X = v, rounded once to `dtype` (exact in fp32 and bf16; an infinity past the type's range, which in
+ * those two a group of magnitudes from 7 2^125 on may pass). X must not overlap the inputs. */
+bigcn_status bigcn_fp4_unpack(int32_t dtype, const uint8_t *q, int64_t ldq, const uint8_t *exps,
+                              int64_t lde, int64_t N, int32_t K, void *X, int64_t ldx,
+                              void *stream);
+
+/*
+ * The product of two matrices of 4-bit rows, A (N x K) and B (F x K):
+ *
+ *   Z_ij = sum_k a_ik b_jk + bias_j
+ *
+ * A layer's forward product takes the rows of its input and the columns of its weights
+ * (bigcn_fp4_pack_columns); its input's gradient the rows of dZ and the weights' rows.
+ *
+ * Z     N x F of `dtype`, row stride ldz >= F, rounded once.   bias  F fp32, nullable (0).
+ * The operands enter exactly; the sums are fp32, those of 64 columns at a time taken and added by
+ * the tensor core, which truncates. A group of NaN makes every sum that it is part of NaN.
+ * The kernel waits on shared-memory barriers a bounded number of times: where a wait runs out, the
+ * tile's part of Z is NaN (0 waits in correct operation; bigcn_device_timeouts counts them).
+ * 0 <= N < 2^31, 1 <= K <= 32768, 1 <= F <= 2^30. Z may not overlap an input.
+ */
+bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t ldaq, const uint8_t *a_exps,
+                            int64_t ldae, int64_t N, const uint8_t *bq, int64_t ldbq,
+                            const uint8_t *b_exps, int64_t ldbe, int32_t F, int32_t K,
+                            const float *bias, void *Z, int64_t ldz, void *stream);
+
+/* Bytes of device workspace that the two calls below need for n tensors; 0 on an invalid n. */
+size_t bigcn_grad_norm_workspace_bytes(int32_t n);
+
+/*
+ * The norm of n tensors together, norm[0] = sqrt(sum over tensors and elements of g^2).
+ *
+ * dtypes, tensors, counts   HOST arrays of n: each tensor's bigcn_dtype, the device pointer of its
+ *        elements, which lie one behind the other, and how many they are (0: the pointer is not
+ *        looked at). They are read before the call returns; a captured call keeps what they said.
+ * norm   one fp32, rounded once of 64-bit sums of fp32 sums of at most 32 squares each (relative error
+ *        below 2^-20), whatever the elements' range; NaN or an infinity where the tensors hold one.
+ * workspace  >= bigcn_grad_norm_workspace_bytes(n) bytes, 256-byte aligned. Sums are added in a
+ *        fixed order: deterministic for tensors of the same alignment to 16 bytes.
+ * 0 <= n <= 65536. norm and workspace may not overlap a tensor or each other. Tensors may overlap (an
+ * element counts as often as it is listed).
+ */
+bigcn_status bigcn_grad_norm(int32_t n, const int32_t *dtypes, const void *const *tensors,
+                             const int64_t *counts, float *norm, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+/*
+ * The same norm, and the tensors scaled down to it: out_t = tensor_t min(1, max_norm / norm),
+ * rounded once (the factor itself is an fp32). Where the norm is at most max_norm, or not finite (NaN,
+ * infinite or past fp32's range), the factor is 1 and out the tensors' bits: a caller that skips
+ * such a step looks at norm.
+ *
+ * out    HOST array of n device pointers, of the tensors' types and counts; out[t] may be tensors[t]
+ *        (in place). max_norm  >= 0, not NaN.
+ * Nothing written (out, norm, workspace) may overlap anything else, out[t] = tensors[t] apart; a tensor
+ * that is scaled in place is listed once.
+ */
+bigcn_status bigcn_clip_grad_norm(int32_t n, const int32_t *dtypes, const void *const *tensors,
+                                  void *const *out, const int64_t *counts, float max_norm,
+                                  float *norm, void *workspace, size_t ws_bytes, void *stream);
 
 /* Bytes of the device scratch array behind bigcn_layer_forward_static. */
 #define BIGCN_STATIC_SCRATCH_BYTES (((size_t)32 << 20) + 256) /* the last 256: control words */

@@ -94,6 +94,19 @@ SIGNATURES = {
     "bigcn_checkpoint_weight_grad_workspace_bytes": ([_i64, _i32, _i32], _sz),
     "bigcn_checkpoint_weight_grad": ([_i32, _p, _i64, _p, _i64, _i64, _i32, _p, _p, _p, _i32,
                                       _i64, _p, _i64, _p, _p, _sz, _p], ctypes.c_int),
+    "bigcn_rms_norm_forward": ([_i32, _p, _i64, _i32, _i64, _p, _i64, _p, ctypes.c_float, _p, _i64,
+                                _p, _i64, _p, _p, _i64, _p, _i64, _p], ctypes.c_int),
+    "bigcn_rms_norm_backward_workspace_bytes": ([_i64, _i32], _sz),
+    "bigcn_rms_norm_backward": ([_i32, _p, _i64, _i32, _i64, _p, _p, _i64, _p, _i64, _p, _i64, _p,
+                                 _p, _i64, _p, _i64, _p, _p, _sz, _p], ctypes.c_int),
+    "bigcn_fp4_pack": ([_i32, _p, _i64, _i32, _i64, _p, _i64, _p, _i64, _p], ctypes.c_int),
+    "bigcn_fp4_pack_columns": ([_i32, _p, _i32, _i32, _i64, _p, _i64, _p, _i64, _p], ctypes.c_int),
+    "bigcn_fp4_unpack": ([_i32, _p, _i64, _p, _i64, _i64, _i32, _p, _i64, _p], ctypes.c_int),
+    "bigcn_fp4_gemm": ([_i32, _p, _i64, _p, _i64, _i64, _p, _i64, _p, _i64, _i32, _i32, _p, _p,
+                        _i64, _p], ctypes.c_int),
+    "bigcn_grad_norm_workspace_bytes": ([_i32], _sz),
+    "bigcn_grad_norm": ([_i32, _p, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
+    "bigcn_clip_grad_norm": ([_i32, _p, _p, _p, _p, ctypes.c_float, _p, _p, _sz, _p], ctypes.c_int),
     "bigcn_weighted_dinv": ([_p, _p, _i64, _i64, _p, _p], ctypes.c_int),
     "bigcn_spmm_norm_weighted": ([_p, _p, _p, _p, _i64, _i64, _p, _i64, _i32, _p, _i64, _p],
                                  ctypes.c_int),
@@ -596,6 +609,157 @@ def bigcn_checkpoint_weight_grad(q, exps, dZ, workspace, dW, gamma=None, beta=No
         _ptr(workspace), _bytes(workspace), _stream(stream)))
 
 
+def _on_device(*tensors):
+    """Refuses tensors that are not on the current CUDA device, whose stream the call takes."""
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("expected tensors on the current CUDA device")
+
+
+def bigcn_rms_norm_forward(X, gamma, eps, R=None, S=None, Y=None, rstd=None, q=None, exps=None,
+                           stream=None):
+    """S = X + R (X without R), Y = gamma shat with shat the rows of S over their root mean
+    square; rstd (N fp32) and the checkpoint of shat where given. S may be R or X. gamma: None
+    for 1."""
+    N, K = X.shape
+    r, ldr = _matrix(R, N, K, "R", X)
+    s, lds = _matrix(S, N, K, "S", X)
+    y, ldy = _matrix(Y, N, K, "Y", X)
+    g, out, kept = _vector(gamma, K, "gamma"), _vector(rstd, N, "rstd"), _kept(q, exps, N, K)
+    dtype, ldx = _dtype(X), _ld(X)
+    _on_device(X, gamma, R, S, Y, rstd, q, exps)
+    _check("bigcn_rms_norm_forward", lib().bigcn_rms_norm_forward(
+        dtype, _ptr(X), N, K, ldx, r, ldr, g, eps, s, lds, y, ldy, out, *kept, _stream(stream)))
+
+
+def bigcn_rms_norm_backward_workspace_bytes(N: int, K: int) -> int:
+    return int(lib().bigcn_rms_norm_backward_workspace_bytes(N, K))
+
+
+def bigcn_rms_norm_backward(dY, gamma, rstd, workspace, S=None, q=None, exps=None, dS=None, dX=None,
+                            dgamma=None, stream=None):
+    """dX (of the sum's addends alike) and dgamma (those given) from dY, with shat from the sum S or
+    from the checkpoint q, exps; dS, which dX may be, is added to dX. workspace: None where dgamma is
+    not given."""
+    N, K = dY.shape
+    s, lds = _matrix(S, N, K, "S", dY)
+    ds, ldds = _matrix(dS, N, K, "dS", dY)
+    dx, lddx = _matrix(dX, N, K, "dX", dY)
+    g, out, kept = _vector(gamma, K, "gamma"), _vector(dgamma, K, "dgamma"), _kept(q, exps, N, K)
+    dtype, lddy, r = _dtype(dY), _ld(dY), _vector(rstd, N, "rstd")
+    _on_device(dY, gamma, rstd, workspace, S, q, exps, dS, dX, dgamma)
+    _check("bigcn_rms_norm_backward", lib().bigcn_rms_norm_backward(
+        dtype, _ptr(dY), N, K, lddy, g, s, lds, *kept, r, ds, ldds, dx, lddx, out,
+        _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def _fp4(q, exps, N, K, what):
+    """(q, ldq, exps, lde) of N 4-bit rows of K columns."""
+    if q.dtype != torch.uint8 or exps.dtype != torch.uint8 or q.shape != (N, (K + 1) // 2) or \
+            exps.shape != (N, (K + 31) // 32):
+        raise ValueError(f"{what}: 4-bit rows are q (N x ceil(K / 2)) and exps (N x ceil(K / 32)), "
+                         "both uint8")
+    return _ptr(q), _ld(q), _ptr(exps), _ld(exps)
+
+
+def bigcn_fp4_pack(X, q, exps, stream=None):
+    """X (N x K, fp32, bf16 or fp16) to 4 bits: q (N x ceil(K/2) uint8) and exps (N x ceil(K/32)
+    uint8), views of rows of the strides that the header asks for (:func:`fp4_buffers`)."""
+    N, K = X.shape
+    dtype, ldx, rows = _dtype(X), _ld(X), _fp4(q, exps, N, K, "X")
+    _on_device(X, q, exps)
+    _check("bigcn_fp4_pack", lib().bigcn_fp4_pack(
+        dtype, _ptr(X), N, K, ldx, *rows, _stream(stream)))
+
+
+def bigcn_fp4_pack_columns(W, q, exps, stream=None):
+    """The columns of W (K x F) to F 4-bit rows of K."""
+    K, F = W.shape
+    dtype, ldw, rows = _dtype(W), _ld(W), _fp4(q, exps, F, K, "W")
+    _on_device(W, q, exps)
+    _check("bigcn_fp4_pack_columns", lib().bigcn_fp4_pack_columns(
+        dtype, _ptr(W), K, F, ldw, *rows, _stream(stream)))
+
+
+def bigcn_fp4_unpack(q, exps, X, stream=None):
+    """X (N x K) from its 4 bits."""
+    N, K = X.shape
+    dtype, ldx, rows = _dtype(X), _ld(X), _fp4(q, exps, N, K, "X")
+    _on_device(X, q, exps)
+    _check("bigcn_fp4_unpack", lib().bigcn_fp4_unpack(
+        dtype, *rows, N, K, _ptr(X), ldx, _stream(stream)))
+
+
+def bigcn_fp4_gemm(aq, a_exps, bq, b_exps, K, Z, bias=None, stream=None):
+    """Z = A B^T + bias (N x F) of the 4-bit rows A (N x K) and B (F x K)."""
+    N, F = Z.shape
+    dtype, ldz, b = _dtype(Z), _ld(Z), _vector(bias, F, "bias")
+    rows_a, rows_b = _fp4(aq, a_exps, N, K, "A"), _fp4(bq, b_exps, F, K, "B")
+    _on_device(aq, a_exps, bq, b_exps, Z, bias)
+    _check("bigcn_fp4_gemm", lib().bigcn_fp4_gemm(
+        dtype, *rows_a, N, *rows_b, F, K, b, _ptr(Z), ldz, _stream(stream)))
+
+
+class TensorList:
+    """Contiguous fp32, bf16 or fp16 tensors of any shapes as the calls over many tensors take
+    them: built once and kept by a program whose gradients stay where they are (it holds them)."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        for t in self.tensors:
+            if not t.is_contiguous():
+                raise ValueError("expected contiguous tensors")
+        self.dtypes = (_i32 * n)(*[_dtype(t) for t in self.tensors])
+        self.pointers = (_p * n)(*[t.data_ptr() for t in self.tensors])
+        self.counts = (_i64 * n)(*[t.numel() for t in self.tensors])
+        self.devices = {t.get_device() for t in self.tensors}
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _list(tensors):
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _lists_on_device(*lists):
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    for t in lists:
+        if t.devices - {device}:
+            raise ValueError("expected tensors on the current CUDA device")
+
+
+def bigcn_grad_norm_workspace_bytes(tensors) -> int:
+    """For a list of tensors (or their number)."""
+    n = tensors if isinstance(tensors, int) else len(tensors)
+    return int(lib().bigcn_grad_norm_workspace_bytes(n))
+
+
+def bigcn_grad_norm(tensors, norm, workspace, stream=None):
+    """norm (one fp32) = the norm of all tensors together (a :class:`TensorList` or tensors)."""
+    t, out = _list(tensors), _vector(norm, 1, "norm")
+    _lists_on_device(t)
+    _on_device(norm, workspace)
+    _check("bigcn_grad_norm", lib().bigcn_grad_norm(
+        len(t), t.dtypes, t.pointers, t.counts, out, _ptr(workspace), _bytes(workspace),
+        _stream(stream)))
+
+
+def bigcn_clip_grad_norm(tensors, max_norm, norm, workspace, out=None, stream=None):
+    """norm as above, and out (None: the tensors themselves) = tensors min(1, max_norm / norm)."""
+    t, n = _list(tensors), _vector(norm, 1, "norm")
+    o = t if out is None else _list(out)
+    if o is not t and (bytes(o.counts) != bytes(t.counts) or bytes(o.dtypes) != bytes(t.dtypes)):
+        raise ValueError("out must be tensors of the same types and lengths")
+    _lists_on_device(t, o)
+    _on_device(norm, workspace)
+    _check("bigcn_clip_grad_norm", lib().bigcn_clip_grad_norm(
+        len(t), t.dtypes, t.pointers, o.pointers, t.counts, max_norm, n, _ptr(workspace),
+        _bytes(workspace), _stream(stream)))
+
+
 # ------------------------------------------------- allocating conveniences ---
 def pack_rows(X, scale=None, shift=None, stream=None):
     N, K = X.shape
@@ -695,3 +859,78 @@ def checkpoint_weight_grad(q, exps, dZ, gamma=None, beta=None, stream=None):
     db = torch.empty(F, dtype=torch.float32, device=dZ.device)
     bigcn_checkpoint_weight_grad(q, exps, dZ, ws, dW, gamma, beta, db, stream)
     return dW, db
+
+
+def rms_norm_forward(X, gamma=None, eps=1e-5, R=None, checkpoint=True, stream=None):
+    """(Y, S, rstd, q, exps); S is X without R, q and exps None without ``checkpoint``."""
+    N, K = X.shape
+    Y = torch.empty((N, K), dtype=X.dtype, device=X.device)
+    S = torch.empty_like(Y) if R is not None else None
+    rstd = torch.empty(N, dtype=torch.float32, device=X.device)
+    q, exps = checkpoint_buffers(N, K, X.device) if checkpoint else (None, None)
+    bigcn_rms_norm_forward(X, gamma, eps, R, S, Y, rstd, q, exps, stream)
+    return Y, X if S is None else S, rstd, q, exps
+
+
+def rms_norm_backward(dY, gamma, rstd, S=None, q=None, exps=None, dS=None, stream=None):
+    """(dX, dgamma) with shat from S or from q and exps."""
+    N, K = dY.shape
+    ws = torch.empty(bigcn_rms_norm_backward_workspace_bytes(N, K), dtype=torch.uint8,
+                     device=dY.device)
+    dX = torch.empty((N, K), dtype=dY.dtype, device=dY.device)
+    dgamma = torch.empty(K, dtype=torch.float32, device=dY.device)
+    bigcn_rms_norm_backward(dY, gamma, rstd, ws, S, q, exps, dS, dX, dgamma, stream)
+    return dX, dgamma
+
+
+def fp4_buffers(N, K, device):
+    """(q, exps) for N 4-bit rows of K columns: views of rows padded as the header asks."""
+    groups = (K + 31) // 32
+    q = torch.empty((N, groups * 16), dtype=torch.uint8, device=device)
+    exps = torch.empty((N, (groups + 3) // 4 * 4), dtype=torch.uint8, device=device)
+    return q[:, :(K + 1) // 2], exps[:, :groups]
+
+
+def fp4_pack(X, stream=None):
+    q, exps = fp4_buffers(*X.shape, X.device)
+    bigcn_fp4_pack(X, q, exps, stream)
+    return q, exps
+
+
+def fp4_pack_columns(W, stream=None):
+    q, exps = fp4_buffers(W.shape[1], W.shape[0], W.device)
+    bigcn_fp4_pack_columns(W, q, exps, stream)
+    return q, exps
+
+
+def fp4_unpack(q, exps, K, dtype=torch.float32, stream=None):
+    X = torch.empty((q.shape[0], K), dtype=dtype, device=q.device)
+    bigcn_fp4_unpack(q, exps, X, stream)
+    return X
+
+
+def fp4_gemm(aq, a_exps, bq, b_exps, K, bias=None, dtype=torch.float32, stream=None):
+    Z = torch.empty((aq.shape[0], bq.shape[0]), dtype=dtype, device=aq.device)
+    bigcn_fp4_gemm(aq, a_exps, bq, b_exps, K, Z, bias, stream)
+    return Z
+
+
+def _norm_buffers(tensors):
+    tensors = _list(tensors)
+    device = tensors.tensors[0].device if len(tensors) else torch.device("cuda")
+    ws = torch.empty(bigcn_grad_norm_workspace_bytes(tensors), dtype=torch.uint8, device=device)
+    return tensors, torch.empty(1, dtype=torch.float32, device=device), ws
+
+
+def grad_norm(tensors, stream=None):
+    """The norm of all tensors together (a tensor of one fp32)."""
+    tensors, norm, ws = _norm_buffers(tensors)
+    bigcn_grad_norm(tensors, norm, ws, stream)
+    return norm
+
+
+def clip_grad_norm(tensors, max_norm, stream=None):
+    """Scales the tensors in place to at most ``max_norm`` together; their norm before."""
+    tensors, norm, ws = _norm_buffers(tensors)
+    bigcn_clip_grad_norm(tensors, max_norm, norm, ws, stream=stream)
+    return norm

@@ -57,6 +57,7 @@
 #include "checkpoint_runs.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
+#include "tensor_map.cuh"
 
 namespace bigcn {
 
@@ -595,44 +596,6 @@ size_t plan_bytes(const GradPlan &g) { return round_up(g.partial_bytes) + round_
 // columns of it.
 constexpr int kMostTma = 256, kMostLoaded = 128;
 
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's encoder of tensor maps (the library links no driver); nullptr without one.
-EncodeTiled encoder() {
-    static const EncodeTiled fn = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
-                                             &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return fn;
-}
-
-// A map of `rows` rows of `width` elements, boxes of box x box_rows; or, with part_bytes, of rows
-// of `parts` parts of `width` elements, box_parts of which are in a box.
-bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
-            int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle, int64_t parts = 1,
-            int64_t part_bytes = 0, int box_parts = 1) {
-    const EncodeTiled fn = encoder();
-    if (!fn) return false;
-    const cuuint64_t dims[3] = {cuuint64_t(width), cuuint64_t(rows), cuuint64_t(parts)};
-    const cuuint64_t strides[2] = {cuuint64_t(row_bytes), cuuint64_t(part_bytes)};
-    const cuuint32_t boxes[3] = {cuuint32_t(box), cuuint32_t(box_rows), cuuint32_t(box_parts)};
-    const cuuint32_t steps[3] = {1, 1, 1};
-    return fn(map, type, part_bytes ? 3 : 2, const_cast<void *>(base), dims, strides, boxes, steps,
-              CU_TENSOR_MAP_INTERLEAVE_NONE,
-              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <typename T, int NT, int PARTS, bool kTma>
 void launch_rows(const GradParams &p, unsigned grid, cudaStream_t s) {
     using S = GradShape<NT, PARTS, kTma>;
@@ -729,12 +692,12 @@ extern "C" bigcn_status bigcn_checkpoint_weight_grad(
     p.z_atoms = F % 64 == 0;
     const bool tma =
         most == kMostTma &&
-        (p.z_atoms ? encode(&p.z_map, type, dZ, 64, N, zrow, 64, direct ? 64 : 32, direct, F / 64,
+        (p.z_atoms ? encode_map(&p.z_map, type, dZ, 64, N, zrow, 64, direct ? 64 : 32, direct, F / 64,
                             64 * int64_t(es), grad_plan(N, K, F, most).NT / 64)
-                   : encode(&p.z_map, type, dZ, F, N, zrow, 64, direct ? 64 : 32, direct));
+                   : encode_map(&p.z_map, type, dZ, F, N, zrow, 64, direct ? 64 : 32, direct));
     const int rows = tma && direct ? 64 : 32;
     const int64_t width = (int64_t(K) + 15) / 16 * 16;
-    if (!encode(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, rows,
+    if (!encode_map(&p.q_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, width, N, N > 1 ? ldq : width, 128, rows,
                 false))
         return BIGCN_ERR_CUDA;
     p.stages = (N + rows - 1) / rows;

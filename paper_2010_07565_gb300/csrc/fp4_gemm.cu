@@ -1,0 +1,415 @@
+// The product of two matrices of microscaled 4-bit rows (bigcn_fp4_gemm), Z = A B^T + bias, on the
+// tensor cores: tcgen05 block-scaled e2m1 x e2m1 with a ue8m0 scale per 32 columns of either
+// operand, fp32 accumulators in tensor memory. Codes go by tensor copies from memory into their
+// swizzled places (128 bytes, 256 columns, of a row a stage); the scale bytes, four groups to a word,
+// by 4-byte copies to where the tensor core's copy into tensor memory wants them: of 128 rows, row r
+// at word (r mod 32) 4 + r / 32.
+//
+// Roles of a CTA (8 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
+// codes, warps 2 and 3 A's and B's scale bytes, warp 1 issues the MMAs, warps 4-7 take the sums out.
+// They meet on mbarriers only:
+//   full[stage]   its copies have landed        empty[stage]  its MMAs are done
+//   summed[acc]   a tile's MMAs are done        taken[acc]    its sums were taken
+#include "fp4.cuh"
+#include "launch.cuh"
+#include "tc_rows.cuh"
+#include "tensor_map.cuh"
+
+namespace bigcn {
+
+__device__ unsigned int g_fp4_timeouts;
+
+namespace {
+
+constexpr int kGemmThreads = 256;
+constexpr int kStageCols = 256;         // columns of a stage: 128 bytes of a row
+constexpr int kTmemCols = 512;
+constexpr int kScaleChunk = 512;        // bytes: a word of scales of 128 rows
+constexpr int kMaxGemmCols = 1 << 15;   // K: at most 512 accumulating MMAs (see the header)
+
+template <int NT>
+struct Fp4Shape {
+    static constexpr int kA = kUmmaM * 128, kB = NT * 128;
+    static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of B's scales
+    static constexpr int kScales = 2 * (1 + kChunks) * kScaleChunk;
+    static constexpr int kStage = kA + kB + kScales;
+    static constexpr int kStages = NT >= 256 ? 4 : NT >= 128 ? 6 : 8;
+    static constexpr int kStaging = 4 * 32 * 33 * 4;                // of the four epilogue warps
+    static constexpr int kSmem = 1024 + kStages * kStage + kStaging;
+    static constexpr int kAccs = NT > 128 ? 1 : 2;
+    static constexpr int kScaleCols = 8 * (1 + kChunks);            // of tensor memory, a stage
+    static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
+    static_assert(kSmem <= 227 * 1024 - 1024, "shared memory per CTA");
+    static_assert(kAccs * NT + kStages * kScaleCols <= kTmemCols, "tensor memory per CTA");
+};
+
+struct Fp4GemmArgs {
+    CUtensorMap a_map, b_map;
+    const uint8_t *a_exps, *b_exps;
+    int64_t lda_e, ldb_e;
+    int64_t N;
+    int F;
+    int groups;              // of 32 columns
+    int nt;                  // column tiles
+    int64_t tiles;
+    const float *bias;       // nullable
+    void *Z;
+    int64_t ldz;
+};
+
+// Instruction descriptor of the block-scaled product: e2m1 x e2m1, both K-major, ue8m0 scales, M =
+// 128, N = n; the scales of a 64-column step are bytes id and id + 1 of their words.
+__device__ __forceinline__ uint32_t fp4_idesc(int n, uint32_t id) {
+    return (id << 4) | (1u << 7) | (1u << 10) | (uint32_t(n >> 3) << 17) | (1u << 23) |
+           (uint32_t(kUmmaM >> 4) << 24) | (id << 29);
+}
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                        uint32_t a_scales, uint32_t b_scales, bool accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], "
+        "p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate ? 1u : 0u));
+}
+// 512 bytes, 32 rows of 16, to four columns of tensor memory, the same in each quarter of its lanes.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr) {
+    uint64_t d = uint64_t((saddr >> 4) & 0x3FFFu);
+    d |= uint64_t(128 >> 4) << 32;              // groups of 8 rows 128 bytes apart, no swizzle
+    d |= uint64_t(1) << 46;
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d));
+}
+
+// A warp's 32 rows by 32 columns of words (a word: one fp32 or two 16-bit columns) from shared
+// memory to Z, a row at a time.
+template <typename T>
+__device__ __forceinline__ void store_rows(const uint32_t *stage, T *z, int64_t ldz, int rows, int cols,
+                                           int lane, bool pairs) {
+    if constexpr (sizeof(T) == 4) {
+        if (lane < cols)
+            for (int r = 0; r < rows; ++r)
+                reinterpret_cast<uint32_t *>(z + r * ldz)[lane] = stage[r * 33 + lane];
+    } else {
+        const bool first = 2 * lane < cols, second = 2 * lane + 1 < cols;
+        for (int r = 0; r < rows; ++r) {
+            const uint32_t w = stage[r * 33 + lane];
+            uint16_t *to = reinterpret_cast<uint16_t *>(z + r * ldz) + 2 * lane;
+            if (pairs && second) {
+                *reinterpret_cast<uint32_t *>(to) = w;
+            } else {
+                if (first) to[0] = uint16_t(w);
+                if (second) to[1] = uint16_t(w >> 16);
+            }
+        }
+    }
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
+    using S = Fp4Shape<NT>;
+    constexpr int kStages = S::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], summed[S::kAccs], taken[S::kAccs],
+        done;
+    __shared__ uint32_t tmem_base, stop;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_addr(&tmem_base)),
+                     "r"(kTmemCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_addr(&full[s]), 65);         // both scale warps' lanes; the boxes' bytes
+            mbar_init(smem_addr(&empty[s]), 1);
+        }
+        for (int b = 0; b < S::kAccs; ++b) {
+            mbar_init(smem_addr(&summed[b]), 1);
+            mbar_init(smem_addr(&taken[b]), 4);
+        }
+        mbar_init(smem_addr(&done), 1);
+        stop = 0u;
+        mbar_fence_init();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    volatile uint32_t *const stopv = &stop;
+    const int stages = (p.groups + 7) / 8;              // of a tile
+
+    if (warp == 0 || warp == 2 || warp == 3) {
+        // Copies into the ring of stages.
+        int s = 0, issued = 0;
+        uint32_t parity = 1u;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+            const int64_t m0 = t / p.nt * kUmmaM;
+            const int n0 = int(t % p.nt) * NT;
+            for (int st = 0; st < stages; ++st) {
+                const bool go = wait_unless(smem_addr(&empty[s]), parity, stopv);
+                if (!__all_sync(kFullMask, go)) {
+                    *stopv = 1u;
+                    ok = false;
+                    break;
+                }
+                const uint32_t at = base + uint32_t(s * S::kStage), bar = smem_addr(&full[s]);
+                if (warp == 0) {
+                    if (elect_one()) {
+                        mbar_expect(bar, S::kA + S::kB);
+                        tma_load(at, &p.a_map, st * 128, int(m0), bar);
+                        tma_load(at + S::kA, &p.b_map, st * 128, n0, bar);
+                    }
+                } else {
+                    // Word h of the stage (four groups) of rows lane, lane + 32, ...
+                    const bool a = warp == 2;
+                    const int64_t row0 = a ? m0 : n0, rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
+                    const uint8_t *exps = a ? p.a_exps : p.b_exps;
+                    const uint32_t to = at + S::kA + S::kB + (a ? 0u : 2u * kScaleChunk);
+                    const int words = a ? 4 : (NT + 31) / 32;
+#pragma unroll
+                    for (int j = 0; j < (NT + 31) / 32 || j < 4; ++j) {
+                        if (j >= words) break;
+                        const int64_t i = row0 + 32 * j + lane;
+                        const uint8_t *e = exps + (i < rows ? i * ld : 0);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            // (Zeros behind the last group, whatever memory holds there.)
+                            const int left = i < rows ? min(4, p.groups - st * 8 - h * 4) : 0;
+                            copy4(to + uint32_t((h * (a ? 1 : S::kChunks) + j / 4) * kScaleChunk +
+                                                lane * 16 + j % 4 * 4),
+                                  left > 0 ? e + st * 8 + h * 4 : exps, uint32_t(max(left, 0)));
+                        }
+                    }
+                    copies_arrive(bar);
+                }
+                __syncwarp();
+                ++issued;
+                if (++s == kStages) s = 0, parity ^= 1u;
+            }
+        }
+        // What is still in flight lands before the shared memory is given up.
+        for (int it = issued > kStages ? issued - kStages : 0; it < issued; ++it)
+            mbar_wait(smem_addr(&full[it % kStages]), uint32_t(it / kStages) & 1u);
+    } else if (warp == 1) {
+        // The warp stays together, one lane issues.
+        int s = 0, b = 0;
+        uint32_t parity = 0u, acc_parity = 1u;
+        bool any = false, ok = true;
+        for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+            const int n0 = int(t % p.nt) * NT, cols = min(NT, p.F - n0);
+            const int n = (cols + 31) / 32 * 32;
+            const uint32_t acc = tmem + uint32_t(b * NT);
+            ok = __all_sync(kFullMask, wait_unless(smem_addr(&taken[b]), acc_parity, stopv));
+            for (int st = 0; ok && st < stages; ++st) {
+                ok = __all_sync(kFullMask, wait_unless(smem_addr(&full[s]), parity, stopv));
+                if (!ok) break;
+                // The scale bytes came by copies of the generic proxy.
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = base + uint32_t(s * S::kStage);
+                const uint32_t scales = at + S::kA + S::kB;
+                // A stage has columns of tensor memory of its own: its MMAs have ended when it is
+                // filled again.
+                const uint32_t sa = tmem + uint32_t(S::kAccs * NT + s * S::kScaleCols), sb = sa + 8;
+                const uint64_t da = sw128_desc(at), db = sw128_desc(at + S::kA);
+                const int steps = min(4, (p.groups - st * 8 + 1) / 2);
+                if (elect_one()) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        copy_scales(sa + uint32_t(4 * h), scales + uint32_t(h * kScaleChunk));
+#pragma unroll
+                        for (int c = 0; c < S::kChunks; ++c)
+                            copy_scales(sb + uint32_t(4 * (h * S::kChunks + c)),
+                                        scales + uint32_t((2 + h * S::kChunks + c) * kScaleChunk));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k >= steps) break;
+                        mma_fp4(acc, da + uint32_t(2 * k), db + uint32_t(2 * k),
+                                fp4_idesc(n, uint32_t(k % 2) * 2u), sa + uint32_t(4 * (k / 2)),
+                                sb + uint32_t(4 * S::kChunks * (k / 2)), st > 0 || k > 0);
+                    }
+                    mma_commit(smem_addr(&empty[s]));
+                    if (st == stages - 1) mma_commit(smem_addr(&summed[b]));
+                }
+                __syncwarp();
+                any = true;
+                if (++s == kStages) s = 0, parity ^= 1u;
+            }
+            if (++b == S::kAccs) b = 0, acc_parity ^= 1u;
+        }
+        if (!ok) *stopv = 1u;
+        if (elect_one()) {
+            if (any) mma_commit(smem_addr(&done));
+            else mbar_arrive(smem_addr(&done));
+        }
+        __syncwarp();
+    } else {
+        // Sums out, a warp the 32 lanes of tensor memory that it may read. Tiles whose waits ran out
+        // are NaN.
+        const int quad = warp & 3;
+        uint32_t *const stage = reinterpret_cast<uint32_t *>(
+            smem_raw + (base - raw) + kStages * S::kStage + quad * 32 * 33 * 4);
+        constexpr int kCols = sizeof(T) == 4 ? 32 : 64;         // of a pass
+        const bool pairs = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p.Z) & 3) == 0 &&
+                           p.ldz % 2 == 0;
+        int b = 0;
+        uint32_t parity = 0u;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+            const int64_t row0 = t / p.nt * kUmmaM + 32 * quad;
+            const int n0 = int(t % p.nt) * NT, cols = min(NT, p.F - n0);
+            const int rows = int(min(int64_t(32), max(int64_t(0), p.N - row0)));
+            if (ok) {
+                ok = __all_sync(kFullMask, wait_unless(smem_addr(&summed[b]), parity, stopv));
+                if (!ok) *stopv = 1u;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + (uint32_t(32 * quad) << 16) + uint32_t(b * NT);
+            T *z = static_cast<T *>(p.Z) + row0 * p.ldz + n0;
+#pragma unroll 1
+            for (int c = 0; c < cols; c += kCols) {
+#pragma unroll
+                for (int h = 0; h < kCols / 32; ++h) {
+                    if (c + 32 * h >= cols) break;
+                    uint32_t v[32];
+                    tmem_ld32(acc + uint32_t(c + 32 * h), v);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        if (!ok) v[e] = 0x7FC00000u;
+                        else if (p.bias && c + 32 * h + e < cols)
+                            v[e] = __float_as_uint(__uint_as_float(v[e]) +
+                                                   __ldg(p.bias + n0 + c + 32 * h + e));
+                    }
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) stage[lane * 33 + e] = v[e];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            uint32_t w;
+                            if constexpr (std::is_same<T, __half>::value) {
+                                const __half2 x = __floats2half2_rn(__uint_as_float(v[2 * e]),
+                                                                    __uint_as_float(v[2 * e + 1]));
+                                w = *reinterpret_cast<const uint32_t *>(&x);
+                            } else {
+                                const __nv_bfloat162 x = __floats2bfloat162_rn(
+                                    __uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                                w = *reinterpret_cast<const uint32_t *>(&x);
+                            }
+                            stage[lane * 33 + 16 * h + e] = w;
+                        }
+                    }
+                }
+                __syncwarp();
+                store_rows<T>(stage, z + c, p.ldz, rows, cols - c, lane, pairs);
+                __syncwarp();
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
+            if (++b == S::kAccs) b = 0, parity ^= 1u;
+        }
+    }
+
+    // Every MMA has ended once `done` completes.
+    const bool ended = mbar_wait(smem_addr(&done), 0u);
+    if (__syncthreads_or(!ended || *stopv != 0u) && tid == 0) atomicAdd(&g_fp4_timeouts, 1u);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+                     "r"(kTmemCols));
+}
+
+template <typename T, int NT>
+void launch_nt(const Fp4GemmArgs &p, unsigned grid, cudaStream_t s) {
+    using S = Fp4Shape<NT>;
+    cudaFuncSetAttribute(fp4_gemm_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    fp4_gemm_kernel<T, NT><<<grid, kGemmThreads, S::kSmem, s>>>(p);
+}
+
+template <typename T>
+void launch_gemm(const Fp4GemmArgs &p, int NT, unsigned grid, cudaStream_t s) {
+    if (NT == 256) launch_nt<T, 256>(p, grid, s);
+    else if (NT == 128) launch_nt<T, 128>(p, grid, s);
+    else if (NT == 64) launch_nt<T, 64>(p, grid, s);
+    else launch_nt<T, 32>(p, grid, s);
+}
+
+}  // namespace
+
+uint32_t take_fp4_timeouts() {
+    unsigned int n = 0;
+    const unsigned int zero = 0;
+    if (cudaMemcpyFromSymbol(&n, g_fp4_timeouts, sizeof(n)) != cudaSuccess ||
+        cudaMemcpyToSymbol(g_fp4_timeouts, &zero, sizeof(zero)) != cudaSuccess) {
+        cudaGetLastError();
+        return ~0u;
+    }
+    return n;
+}
+
+}  // namespace bigcn
+
+using namespace bigcn;
+
+extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t ldaq,
+                                       const uint8_t *a_exps, int64_t ldae, int64_t N,
+                                       const uint8_t *bq, int64_t ldbq, const uint8_t *b_exps,
+                                       int64_t ldbe, int32_t F, int32_t K, const float *bias, void *Z,
+                                       int64_t ldz, void *stream) {
+    const size_t es = dtype_bytes(dtype);
+    if (es == 0 || N < 0 || N > int64_t(INT32_MAX) || K < 1 || K > kMaxGemmCols || F < 1 ||
+        F > kMaxCols || ldz < F || !fp4_strides_ok(N, K, ldaq, ldae) ||
+        !fp4_strides_ok(F, K, ldbq, ldbe) || (N > 0 && N > kMaxElems / ldz))
+        return BIGCN_ERR_INVALID_ARG;
+    if (N == 0) return BIGCN_OK;
+    if (!aq || !a_exps || !bq || !b_exps || !Z) return BIGCN_ERR_INVALID_ARG;
+    if (!checkpoint_aligned(aq, a_exps) || !checkpoint_aligned(bq, b_exps) || !aligned_to(Z, es) ||
+        (bias && !aligned_to(bias, 4)))
+        return BIGCN_ERR_MISALIGNED;
+    const void *in[] = {aq, a_exps, bq, b_exps, bias};
+    const size_t inb[] = {fp4_q_span(N, K, ldaq), checkpoint_exps_span(N, K, ldae),
+                          fp4_q_span(F, K, ldbq), checkpoint_exps_span(F, K, ldbe), size_t(F) * 4};
+    for (int p = 0; p < 5; ++p)
+        if (overlaps(Z, span_bytes(N, F, ldz, es), in[p], inb[p])) return BIGCN_ERR_INVALID_ARG;
+    DeviceInfo dev;
+    const bigcn_status st = current_device(&dev);
+    if (st != BIGCN_OK) return st;
+
+    const int64_t mt = (N + kUmmaM - 1) / kUmmaM;
+    int NT = F > 128 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
+    while (NT > 32 && mt * ((F + NT - 1) / NT) * 2 <= dev.sm_count) NT /= 2;
+    Fp4GemmArgs p;
+    p.groups = int(checkpoint_groups(K));
+    const int64_t width = int64_t(p.groups) * 16;
+    if (!encode_map(&p.a_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, aq, width, N, N > 1 ? ldaq : width, 128,
+                    kUmmaM, true) ||
+        !encode_map(&p.b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, bq, width, F, F > 1 ? ldbq : width, 128,
+                    NT, true))
+        return BIGCN_ERR_CUDA;
+    p.a_exps = a_exps;
+    p.b_exps = b_exps;
+    p.lda_e = ldae;
+    p.ldb_e = ldbe;
+    p.N = N;
+    p.F = F;
+    p.nt = (F + NT - 1) / NT;
+    p.tiles = mt * p.nt;
+    p.bias = bias;
+    p.Z = Z;
+    p.ldz = ldz;
+    const unsigned grid = unsigned(p.tiles < dev.sm_count ? p.tiles : dev.sm_count);
+    const cudaStream_t s = as_stream(stream);
+    if (dtype == BIGCN_F32) launch_gemm<float>(p, NT, grid, s);
+    else if (dtype == BIGCN_BF16) launch_gemm<__nv_bfloat16>(p, NT, grid, s);
+    else launch_gemm<__half>(p, NT, grid, s);
+    return launch_status();
+}

@@ -437,4 +437,7 @@ uint32_t take_mix_timeouts();
 // Likewise for the checkpoints' weight gradient (checkpoint_grad.cu).
 uint32_t take_grad_timeouts();
 
+// And for the product of 4-bit rows (fp4_gemm.cu).
+uint32_t take_fp4_timeouts();
+
 }  // namespace bigcn

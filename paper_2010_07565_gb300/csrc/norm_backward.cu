@@ -18,31 +18,6 @@
 namespace bigcn {
 namespace {
 
-// dgamma, dbeta = the chunks' sums: a block takes 32 columns, warp w every 32nd chunk from w
-// on; the warps' sums are added in order.
-constexpr int kSumThreads = 1024;
-__global__ void __launch_bounds__(kSumThreads)
-param_sum_kernel(const float *__restrict__ partial, int chunks, int K, float *__restrict__ dgamma,
-                 float *__restrict__ dbeta) {
-    __shared__ float part[32][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t t = int64_t(blockIdx.x) * 32 + lane;
-    grid_dependency_wait();
-    float s = 0.0f;
-    if (t < 2 * int64_t(K))
-#pragma unroll 4
-        for (int c = warp; c < chunks; c += 32) s += partial[int64_t(c) * 2 * K + t];
-    part[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && t < 2 * int64_t(K)) {
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 32; ++w) v += part[w][lane];
-        float *out = t < K ? dgamma : dbeta;
-        if (out) out[t < K ? t : t - K] = v;
-    }
-}
-
 constexpr size_t kAlign = 256;
 
 }  // namespace
@@ -117,13 +92,14 @@ extern "C" bigcn_status bigcn_layer_norm_backward(
         return BIGCN_OK;
     }
     float *partial = params ? static_cast<float *>(workspace) : nullptr;
-    BackwardArgs a{dY, N, K, lddy, gamma, X, ldx, mean, q, ldq, exps, lde, rstd, dX, lddx, partial, 0};
-    if (dtype == BIGCN_F32) launch_backward<float>(a, dev, s);
-    else if (dtype == BIGCN_BF16) launch_backward<__nv_bfloat16>(a, dev, s);
-    else launch_backward<__half>(a, dev, s);
+    BackwardArgs a{dY, N, K, lddy, gamma, X, ldx, mean, q, ldq, exps, lde, rstd, dX, lddx, partial, 0,
+                   nullptr, 0};
+    if (dtype == BIGCN_F32) launch_backward<float, false>(a, dev, s);
+    else if (dtype == BIGCN_BF16) launch_backward<__nv_bfloat16, false>(a, dev, s);
+    else launch_backward<__half, false>(a, dev, s);
     if (params)
         launch_kernel(param_sum_kernel, dim3(unsigned((2 * int64_t(K) + 31) / 32)),
-                      dim3(kSumThreads), 0, s, true, dim3(1, 1, 1), a.partial, a.chunks, K, dgamma,
-                      dbeta);
+                      dim3(kSumThreads), 0, s, true, dim3(1, 1, 1), a.partial, a.chunks, K, 2 * int64_t(K),
+                      dgamma, dbeta);
     return launch_status();
 }

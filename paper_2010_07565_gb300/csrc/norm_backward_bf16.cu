@@ -3,6 +3,6 @@
 
 namespace bigcn {
 
-template void launch_backward<__nv_bfloat16>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
+template void launch_backward<__nv_bfloat16, false>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
 
 }  // namespace bigcn

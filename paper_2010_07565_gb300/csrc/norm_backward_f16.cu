@@ -3,6 +3,6 @@
 
 namespace bigcn {
 
-template void launch_backward<__half>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
+template void launch_backward<__half, false>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
 
 }  // namespace bigcn

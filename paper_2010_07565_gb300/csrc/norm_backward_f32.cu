@@ -3,6 +3,6 @@
 
 namespace bigcn {
 
-template void launch_backward<float>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
+template void launch_backward<float, false>(BackwardArgs &, const DeviceInfo &, cudaStream_t);
 
 }  // namespace bigcn

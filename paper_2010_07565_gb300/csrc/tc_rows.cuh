@@ -139,7 +139,7 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
                  : "memory");
 }
 
-// Four bytes from memory to shared memory, zeros where `bytes` is 0; and this thread's
+// The first `bytes` (0 to 4) of four bytes from memory to shared memory, zeros for the rest; and this thread's
 // arrival on bar once all its earlier such copies have landed (at once where it made none), one of
 // those that the barrier was initialised for.
 __device__ __forceinline__ void copy4(uint32_t dst, const void *src, uint32_t bytes) {

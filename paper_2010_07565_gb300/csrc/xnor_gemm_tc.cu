@@ -740,7 +740,8 @@ extern "C" int32_t bigcn_device_timeouts(void) {
         cudaGetLastError();
         return -1;
     }
-    const uint32_t mix = bigcn::take_mix_timeouts(), grad = bigcn::take_grad_timeouts();
-    if (mix == ~0u || grad == ~0u) return -1;
-    return int32_t(n + mix + grad);
+    const uint32_t mix = bigcn::take_mix_timeouts(), grad = bigcn::take_grad_timeouts(),
+                   fp4 = bigcn::take_fp4_timeouts();
+    if (mix == ~0u || grad == ~0u || fp4 == ~0u) return -1;
+    return int32_t(n + mix + grad + fp4);
 }
