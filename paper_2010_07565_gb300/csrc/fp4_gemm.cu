@@ -1,13 +1,14 @@
 // The product of two matrices of microscaled 4-bit rows (bigcn_fp4_gemm), Z = A B^T + bias, on the
 // tensor cores: tcgen05 block-scaled e2m1 x e2m1 with a ue8m0 scale per 32 columns of either
 // operand, fp32 accumulators in tensor memory. Codes go by tensor copies from memory into their
-// swizzled places (128 bytes, 256 columns, of a row a stage); the scale bytes, four groups to a word,
-// by 4-byte copies to where the tensor core's copy into tensor memory wants them: of 128 rows, row r
-// at word (r mod 32) 4 + r / 32.
+// swizzled places (128 bytes, 256 columns, of a row a stage). The scale bytes, four groups to a word,
+// go by way of registers to where the tensor core's copy into tensor memory wants them: of 128
+// rows, row r at word (r mod 32) 4 + r / 32, so a lane's words of rows lane, lane + 32, ... are 16 bytes.
 //
-// Roles of a CTA (8 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
-// codes, warps 2 and 3 A's and B's scale bytes, warp 1 issues the MMAs, warps 4-7 take the sums out.
-// They meet on mbarriers only:
+// Roles of a CTA (12 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
+// codes, warps 2 and 3 bring A's and B's scale bytes, 16 groups (two stages) of a row at a time and
+// loaded while the previous are used, warp 1 issues the MMAs, warps 4-11 take the sums out, each every
+// second 32 columns of the 32 rows that it may read. They meet on mbarriers only:
 //   full[stage]   its copies have landed        empty[stage]  its MMAs are done
 //   summed[acc]   a tile's MMAs are done        taken[acc]    its sums were taken
 #include "fp4.cuh"
@@ -21,8 +22,9 @@ __device__ unsigned int g_fp4_timeouts;
 
 namespace {
 
-constexpr int kGemmThreads = 256;
-constexpr int kStageCols = 256;         // columns of a stage: 128 bytes of a row
+constexpr int kGemmThreads = 384;
+constexpr int kOutWarps = 8;            // that take the sums out
+constexpr int kUnit = 16;               // groups whose scale bytes are loaded at a time: two stages'
 constexpr int kTmemCols = 512;
 constexpr int kScaleChunk = 512;        // bytes: a word of scales of 128 rows
 constexpr int kMaxGemmCols = 1 << 15;   // K: at most 512 accumulating MMAs (see the header)
@@ -33,8 +35,8 @@ struct Fp4Shape {
     static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of B's scales
     static constexpr int kScales = 2 * (1 + kChunks) * kScaleChunk;
     static constexpr int kStage = kA + kB + kScales;
-    static constexpr int kStages = NT >= 256 ? 4 : NT >= 128 ? 6 : 8;
-    static constexpr int kStaging = 4 * 32 * 33 * 4;                // of the four epilogue warps
+    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 5 : 7;
+    static constexpr int kStaging = kOutWarps * 32 * 33 * 4;
     static constexpr int kSmem = 1024 + kStages * kStage + kStaging;
     static constexpr int kAccs = NT > 128 ? 1 : 2;
     static constexpr int kScaleCols = 8 * (1 + kChunks);            // of tensor memory, a stage
@@ -80,26 +82,157 @@ __device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d));
 }
 
-// A warp's 32 rows by 32 columns of words (a word: one fp32 or two 16-bit columns) from shared
-// memory to Z, a row at a time.
+// A warp's 32 rows by 32 columns of sums from shared memory (pitch 33) to Z, with the bias: a row
+// at a time in fp32, two in 16 bits, where `pairs` says that two columns are one aligned word.
 template <typename T>
-__device__ __forceinline__ void store_rows(const uint32_t *stage, T *z, int64_t ldz, int rows, int cols,
-                                           int lane, bool pairs) {
+__device__ __forceinline__ void store_sums(const float *stage, T *z, int64_t ldz, int rows, int cols,
+                                           const float *bias, int lane, bool pairs) {
     if constexpr (sizeof(T) == 4) {
-        if (lane < cols)
-            for (int r = 0; r < rows; ++r)
-                reinterpret_cast<uint32_t *>(z + r * ldz)[lane] = stage[r * 33 + lane];
+        const float b = bias && lane < cols ? __ldg(bias + lane) : 0.0f;
+        T *to = z + lane;
+        if (lane >= cols) return;
+        if (rows == 32) {
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += 16) {
+                float v[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) v[r] = stage[(r0 + r) * 33 + lane] + b;
+#pragma unroll
+                for (int r = 0; r < 16; ++r, to += ldz) *to = v[r];
+            }
+        } else {
+            for (int r = 0; r < rows; ++r, to += ldz) *to = stage[r * 33 + lane] + b;
+        }
     } else {
-        const bool first = 2 * lane < cols, second = 2 * lane + 1 < cols;
-        for (int r = 0; r < rows; ++r) {
-            const uint32_t w = stage[r * 33 + lane];
-            uint16_t *to = reinterpret_cast<uint16_t *>(z + r * ldz) + 2 * lane;
+        const int c = 2 * (lane & 15), r0 = lane >> 4;
+        const bool first = c < cols, second = c + 1 < cols;
+        const float b0 = bias && first ? __ldg(bias + c) : 0.0f;
+        const float b1 = bias && second ? __ldg(bias + c + 1) : 0.0f;
+        T *to = z + r0 * ldz + c;
+        if (!first) return;
+#pragma unroll 8
+        for (int r = r0; r < 32; r += 2, to += 2 * ldz) {
+            if (r >= rows) break;
+            const float v0 = stage[r * 33 + c] + b0, v1 = stage[r * 33 + c + 1] + b1;
             if (pairs && second) {
+                uint32_t w;
+                if constexpr (std::is_same<T, __half>::value) {
+                    const __half2 x = __floats2half2_rn(v0, v1);
+                    w = *reinterpret_cast<const uint32_t *>(&x);
+                } else {
+                    const __nv_bfloat162 x = __floats2bfloat162_rn(v0, v1);
+                    w = *reinterpret_cast<const uint32_t *>(&x);
+                }
                 *reinterpret_cast<uint32_t *>(to) = w;
             } else {
-                if (first) to[0] = uint16_t(w);
-                if (second) to[1] = uint16_t(w >> 16);
+                to[0] = from_f32<T>(v0);
+                if (second) to[1] = from_f32<T>(v1);
             }
+        }
+    }
+}
+
+// Scale bytes of unit u (16 groups) of the rows row0 + lane, + 32, ...: four words a row, zeros behind
+// the last group and the last row, whatever memory holds there. `wide`: rows aligned to 16 bytes.
+template <int R>
+__device__ __forceinline__ void load_scales(uint4 (&w)[R], const uint8_t *exps, int64_t ld, int64_t row0,
+                                            int64_t rows, int groups, int u, int lane, bool wide) {
+    const int left = groups - u * kUnit;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int64_t i = row0 + 32 * j + lane;
+        w[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (i >= rows) continue;
+        const uint8_t *p = exps + i * ld + u * kUnit;
+        if (wide && left >= kUnit) {
+            w[j] = __ldg(reinterpret_cast<const uint4 *>(p));
+        } else {
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(p);
+            auto word = [&](int h) {
+                const int n = left - 4 * h;
+                return n <= 0 ? 0u : n >= 4 ? __ldg(q + h) : __ldg(q + h) & ((1u << (8 * n)) - 1u);
+            };
+            w[j] = make_uint4(word(0), word(1), word(2), word(3));
+        }
+    }
+}
+// Word h of stage `half` of a unit, of rows lane, lane + 32, ...: 16 bytes for each 128 rows.
+template <int R>
+__device__ __forceinline__ void store_scales(uint32_t to, const uint4 (&w)[R], int half, int lane) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < (R + 3) / 4; ++c) {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (4 * c + j < R) {
+                    const uint4 &x = w[4 * c + j < R ? 4 * c + j : 0];
+                    v[j] = half ? (h ? x.w : x.z) : (h ? x.y : x.x);
+                } else {
+                    v[j] = 0u;
+                }
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                             to + uint32_t((h * ((R + 3) / 4) + c) * kScaleChunk + lane * 16)),
+                         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                         : "memory");
+        }
+}
+
+// Tile t: its first row and first column.
+struct Tile {
+    int64_t m0;
+    int n0;
+    __device__ __forceinline__ Tile(int64_t t, int nt, int NT) {
+        if (t >> 32 == 0) {
+            const uint32_t m = uint32_t(t) / uint32_t(nt);
+            m0 = int64_t(m) * kUmmaM;
+            n0 = int(uint32_t(t) - m * uint32_t(nt)) * NT;
+        } else {
+            m0 = t / nt * kUmmaM;
+            n0 = int(t % nt) * NT;
+        }
+    }
+};
+
+// A scale warp's work: R rows a lane, chunks from `offset` of a stage on.
+template <int NT, int R>
+__device__ __forceinline__ void bring_scales(const Fp4GemmArgs &p, bool a, uint32_t base, uint32_t offset,
+                                             const uint64_t *empty, const uint64_t *full,
+                                             volatile uint32_t *stopv, int stages, int lane) {
+    using S = Fp4Shape<NT>;
+    const uint8_t *exps = a ? p.a_exps : p.b_exps;
+    const int64_t rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
+    const bool wide = (reinterpret_cast<uintptr_t>(exps) & 15) == 0 && ld % 16 == 0;
+    auto load = [&](int64_t t, int u, uint4 (&w)[R]) {
+        const Tile tile(t, p.nt, NT);
+        load_scales<R>(w, exps, ld, a ? tile.m0 : tile.n0, rows, p.groups, u, lane, wide);
+    };
+    int s = 0;
+    uint32_t parity = 1u;
+    uint4 next[R];
+    int64_t t = blockIdx.x;
+    int u = 0;
+    const int units = (stages + 1) / 2;
+    if (t < p.tiles) load(t, 0, next);
+    while (t < p.tiles) {
+        uint4 w[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) w[j] = next[j];
+        const int n = min(2, stages - 2 * u);
+        if (++u == units) u = 0, t += gridDim.x;
+        if (t < p.tiles) load(t, u, next);
+        for (int half = 0; half < n; ++half) {
+            if (!__all_sync(kFullMask, wait_unless(smem_addr(&empty[s]), parity, stopv))) {
+                *stopv = 1u;
+                return;
+            }
+            store_scales<R>(base + uint32_t(s * S::kStage) + offset, w, half, lane);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&full[s]));
+            if (++s == S::kStages) s = 0, parity ^= 1u;
         }
     }
 }
@@ -125,12 +258,12 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&full[s]), 65);         // both scale warps' lanes; the boxes' bytes
+            mbar_init(smem_addr(&full[s]), 3);          // both scale warps; the boxes' bytes
             mbar_init(smem_addr(&empty[s]), 1);
         }
         for (int b = 0; b < S::kAccs; ++b) {
             mbar_init(smem_addr(&summed[b]), 1);
-            mbar_init(smem_addr(&taken[b]), 4);
+            mbar_init(smem_addr(&taken[b]), kOutWarps);
         }
         mbar_init(smem_addr(&done), 1);
         stop = 0u;
@@ -143,50 +276,24 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     volatile uint32_t *const stopv = &stop;
     const int stages = (p.groups + 7) / 8;              // of a tile
 
-    if (warp == 0 || warp == 2 || warp == 3) {
+    if (warp == 0) {
         // Copies into the ring of stages.
         int s = 0, issued = 0;
         uint32_t parity = 1u;
         bool ok = true;
         for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-            const int64_t m0 = t / p.nt * kUmmaM;
-            const int n0 = int(t % p.nt) * NT;
+            const Tile tile(t, p.nt, NT);
             for (int st = 0; st < stages; ++st) {
-                const bool go = wait_unless(smem_addr(&empty[s]), parity, stopv);
-                if (!__all_sync(kFullMask, go)) {
+                if (!__all_sync(kFullMask, wait_unless(smem_addr(&empty[s]), parity, stopv))) {
                     *stopv = 1u;
                     ok = false;
                     break;
                 }
                 const uint32_t at = base + uint32_t(s * S::kStage), bar = smem_addr(&full[s]);
-                if (warp == 0) {
-                    if (elect_one()) {
-                        mbar_expect(bar, S::kA + S::kB);
-                        tma_load(at, &p.a_map, st * 128, int(m0), bar);
-                        tma_load(at + S::kA, &p.b_map, st * 128, n0, bar);
-                    }
-                } else {
-                    // Word h of the stage (four groups) of rows lane, lane + 32, ...
-                    const bool a = warp == 2;
-                    const int64_t row0 = a ? m0 : n0, rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
-                    const uint8_t *exps = a ? p.a_exps : p.b_exps;
-                    const uint32_t to = at + S::kA + S::kB + (a ? 0u : 2u * kScaleChunk);
-                    const int words = a ? 4 : (NT + 31) / 32;
-#pragma unroll
-                    for (int j = 0; j < (NT + 31) / 32 || j < 4; ++j) {
-                        if (j >= words) break;
-                        const int64_t i = row0 + 32 * j + lane;
-                        const uint8_t *e = exps + (i < rows ? i * ld : 0);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            // (Zeros behind the last group, whatever memory holds there.)
-                            const int left = i < rows ? min(4, p.groups - st * 8 - h * 4) : 0;
-                            copy4(to + uint32_t((h * (a ? 1 : S::kChunks) + j / 4) * kScaleChunk +
-                                                lane * 16 + j % 4 * 4),
-                                  left > 0 ? e + st * 8 + h * 4 : exps, uint32_t(max(left, 0)));
-                        }
-                    }
-                    copies_arrive(bar);
+                if (elect_one()) {
+                    mbar_expect(bar, S::kA + S::kB);
+                    tma_load(at, &p.a_map, st * 128, int(tile.m0), bar);
+                    tma_load(at + S::kA, &p.b_map, st * 128, tile.n0, bar);
                 }
                 __syncwarp();
                 ++issued;
@@ -196,21 +303,23 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
         // What is still in flight lands before the shared memory is given up.
         for (int it = issued > kStages ? issued - kStages : 0; it < issued; ++it)
             mbar_wait(smem_addr(&full[it % kStages]), uint32_t(it / kStages) & 1u);
+    } else if (warp == 2) {
+        bring_scales<NT, 4>(p, true, base, S::kA + S::kB, empty, full, stopv, stages, lane);
+    } else if (warp == 3) {
+        bring_scales<NT, (NT + 31) / 32>(p, false, base, S::kA + S::kB + 2 * kScaleChunk, empty, full,
+                                         stopv, stages, lane);
     } else if (warp == 1) {
         // The warp stays together, one lane issues.
         int s = 0, b = 0;
         uint32_t parity = 0u, acc_parity = 1u;
         bool any = false, ok = true;
         for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-            const int n0 = int(t % p.nt) * NT, cols = min(NT, p.F - n0);
-            const int n = (cols + 31) / 32 * 32;
+            const int n = (min(NT, p.F - Tile(t, p.nt, NT).n0) + 31) / 32 * 32;
             const uint32_t acc = tmem + uint32_t(b * NT);
             ok = __all_sync(kFullMask, wait_unless(smem_addr(&taken[b]), acc_parity, stopv));
             for (int st = 0; ok && st < stages; ++st) {
                 ok = __all_sync(kFullMask, wait_unless(smem_addr(&full[s]), parity, stopv));
                 if (!ok) break;
-                // The scale bytes came by copies of the generic proxy.
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t at = base + uint32_t(s * S::kStage);
                 const uint32_t scales = at + S::kA + S::kB;
@@ -251,20 +360,20 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
         }
         __syncwarp();
     } else {
-        // Sums out, a warp the 32 lanes of tensor memory that it may read. Tiles whose waits ran out
-        // are NaN.
-        const int quad = warp & 3;
-        uint32_t *const stage = reinterpret_cast<uint32_t *>(
-            smem_raw + (base - raw) + kStages * S::kStage + quad * 32 * 33 * 4);
-        constexpr int kCols = sizeof(T) == 4 ? 32 : 64;         // of a pass
+        // Sums out, a warp the 32 lanes of tensor memory that it may read, every second 32 columns.
+        // Tiles whose waits ran out are NaN.
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        float *const stage = reinterpret_cast<float *>(smem_raw + (base - raw) + kStages * S::kStage) +
+                             (warp - 4) * 32 * 33;
         const bool pairs = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p.Z) & 3) == 0 &&
                            p.ldz % 2 == 0;
         int b = 0;
         uint32_t parity = 0u;
         bool ok = true;
         for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-            const int64_t row0 = t / p.nt * kUmmaM + 32 * quad;
-            const int n0 = int(t % p.nt) * NT, cols = min(NT, p.F - n0);
+            const Tile tile(t, p.nt, NT);
+            const int64_t row0 = tile.m0 + 32 * quad;
+            const int cols = min(NT, p.F - tile.n0);
             const int rows = int(min(int64_t(32), max(int64_t(0), p.N - row0)));
             if (ok) {
                 ok = __all_sync(kFullMask, wait_unless(smem_addr(&summed[b]), parity, stopv));
@@ -272,43 +381,17 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (uint32_t(32 * quad) << 16) + uint32_t(b * NT);
-            T *z = static_cast<T *>(p.Z) + row0 * p.ldz + n0;
+            T *z = static_cast<T *>(p.Z) + row0 * p.ldz + tile.n0;
+            const float *bias = p.bias ? p.bias + tile.n0 : nullptr;
 #pragma unroll 1
-            for (int c = 0; c < cols; c += kCols) {
+            for (int c = 32 * half; c < cols; c += 64) {
+                uint32_t v[32];
+                tmem_ld32(acc + uint32_t(c), v);
 #pragma unroll
-                for (int h = 0; h < kCols / 32; ++h) {
-                    if (c + 32 * h >= cols) break;
-                    uint32_t v[32];
-                    tmem_ld32(acc + uint32_t(c + 32 * h), v);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (!ok) v[e] = 0x7FC00000u;
-                        else if (p.bias && c + 32 * h + e < cols)
-                            v[e] = __float_as_uint(__uint_as_float(v[e]) +
-                                                   __ldg(p.bias + n0 + c + 32 * h + e));
-                    }
-                    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) stage[lane * 33 + e] = v[e];
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            uint32_t w;
-                            if constexpr (std::is_same<T, __half>::value) {
-                                const __half2 x = __floats2half2_rn(__uint_as_float(v[2 * e]),
-                                                                    __uint_as_float(v[2 * e + 1]));
-                                w = *reinterpret_cast<const uint32_t *>(&x);
-                            } else {
-                                const __nv_bfloat162 x = __floats2bfloat162_rn(
-                                    __uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-                                w = *reinterpret_cast<const uint32_t *>(&x);
-                            }
-                            stage[lane * 33 + 16 * h + e] = w;
-                        }
-                    }
-                }
+                for (int e = 0; e < 32; ++e)
+                    stage[lane * 33 + e] = __uint_as_float(ok ? v[e] : 0x7FC00000u);
                 __syncwarp();
-                store_rows<T>(stage, z + c, p.ldz, rows, cols - c, lane, pairs);
+                store_sums<T>(stage, z + c, p.ldz, rows, cols - c, bias ? bias + c : nullptr, lane, pairs);
                 __syncwarp();
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -385,7 +468,9 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     if (st != BIGCN_OK) return st;
 
     const int64_t mt = (N + kUmmaM - 1) / kUmmaM;
-    int NT = F > 128 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
+    // Tiles of 256 columns read A once for twice as many, but leave no room for a second accumulator:
+    // only where the MMAs of a tile are long beside taking its sums out.
+    int NT = F > 128 && K > 2048 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
     while (NT > 32 && mt * ((F + NT - 1) / NT) * 2 <= dev.sm_count) NT /= 2;
     Fp4GemmArgs p;
     p.groups = int(checkpoint_groups(K));
