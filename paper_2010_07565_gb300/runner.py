@@ -15,6 +15,10 @@ The output is the logits (no softmax: Eq. 2 belongs to training).
 :class:`NormedLayer` is one layer in training whose features stay real (only the weights
 binarized) and whose input rows are normalised: layer norm, product, aggregation and their
 gradients, with the normalised rows kept in 8 bits in between.
+
+:class:`ResidualLayer` is one layer of a deep residual stack in training: it adds its input to the
+stream of rows that all layers share, normalises the sum, multiplies in 4 bits and aggregates;
+:class:`GradientClip` scales the gradients of such a stack by their common norm.
 """
 from __future__ import annotations
 
@@ -211,8 +215,128 @@ class NormedLayer:
                                     dbeta=self.dbeta)
         return self.dWb, self.db, self.dgamma, self.dbeta, self.dX
 
+    def gradients(self):
+        return [self.dWb, self.db, self.dgamma, self.dbeta]
+
     def weight_gradient(self):
         """Eq. bp-W of dWb: sign(W) times the column means of dWb sign(W), and beta_j dWb where
         |W| < 1 (the straight-through estimator of sign)."""
         sign = torch.where(self.W >= 0, 1.0, -1.0)
         return sign * (self.dWb * sign).mean(0) + self.w_scale * self.dWb * (self.W.abs() < 1)
+
+
+class ResidualScratch:
+    """What layers of a residual stack need only within a call: the largest layer's Y (and dY), Z
+    (and G), the 4-bit rows of Y, G and the weights, and workspace, for ``sizes``, the layers' (N, K,
+    F). Layers that are given one share it, on one stream."""
+
+    def __init__(self, sizes, device):
+        sizes = list(sizes)
+        e = lambda n, dtype=torch.float32: torch.empty(n, dtype=dtype, device=torch.device(device))
+        most = lambda f: max(f(*size) for size in sizes)
+        self.Y, self.dX = (e(most(lambda N, K, F: N * K)) for _ in range(2))
+        self.Z = e(most(lambda N, K, F: N * F))
+        self.rows4 = e(most(lambda N, K, F: max(_fp4_bytes(N, K), _fp4_bytes(N, F))), torch.uint8)
+        self.weights4 = e(most(lambda N, K, F: max(_fp4_bytes(F, K), _fp4_bytes(K, F))), torch.uint8)
+        self.workspace = e(most(lambda N, K, F: max(
+            B.bigcn_rms_norm_backward_workspace_bytes(N, K),
+            B.bigcn_checkpoint_weight_grad_workspace_bytes(N, K, F), 1)), dtype=torch.uint8)
+
+
+def _fp4_bytes(rows, cols):
+    groups = (cols + 31) // 32
+    return rows * (groups * 16 + (groups + 3) // 4 * 4)
+
+
+def _fp4_views(buf, rows, cols):
+    """(q, exps) of 4-bit rows within a buffer."""
+    groups = (cols + 31) // 32
+    at, wide = rows * groups * 16, (groups + 3) // 4 * 4
+    q = buf[:at].view(rows, groups * 16)[:, :(cols + 1) // 2]
+    return q, buf[at:at + rows * wide].view(rows, wide)[:, :groups]
+
+
+class ResidualLayer:
+    """One layer of a residual stack in training:
+
+        S = R + X (the stream with the previous layer's output added, in R's place),
+        Y = gamma shat, shat the rows of S over their root mean square,
+        H = A~ (Y4 W4 + b),
+
+    Y4 and W4 the normalised rows and the weights' columns in microscaled 4 bits. A stack feeds each
+    layer's H to the next as X and keeps one stream R; the first layer has none (S = X). Between
+    ``forward()`` and ``backward()`` a layer keeps shat's 8-bit checkpoint and each row's rstd.
+
+        G   = A~ dH                                       (the CSR is symmetric)
+        dW  = (gamma v)^T G,   db = sum_i G_i             (v the checkpoint; straight through Y4 and W4)
+        dY  = G4 W4r^T                                    (G's rows and W's rows in 4 bits)
+        dX  = the norm's gradient of dY, plus dS          (of X and of R alike)
+
+    In a stack dX is the dH and the dS of the layer below, which adds to it in place."""
+
+    def __init__(self, N: int, K: int, F: int, device, eps: float = 1e-5, scratch=None):
+        self.N, self.K, self.F, self.eps = N, K, F, eps
+        self.device = torch.device(device)
+        e = lambda *shape: torch.empty(shape, dtype=torch.float32, device=self.device)
+        # parameters
+        self.W, self.b = e(K, F), torch.zeros(F, device=self.device)
+        self.gamma = torch.ones(K, device=self.device)
+        # kept from forward to backward
+        self.q, self.exps = B.checkpoint_buffers(N, K, self.device)
+        self.rstd = e(N)
+        self.H = e(N, F)
+        # scratch: free for other layers between calls (dX until the layer below has run)
+        scratch = scratch or ResidualScratch([(N, K, F)], self.device)
+        take = lambda t, cols: t[:N * cols].view(N, cols)
+        self.Y, self.Z, self.dX = take(scratch.Y, K), take(scratch.Z, F), take(scratch.dX, K)
+        self.G, self.dY = self.Z, self.Y
+        self.y4, self.g4 = _fp4_views(scratch.rows4, N, K), _fp4_views(scratch.rows4, N, F)
+        self.w4 = _fp4_views(scratch.weights4, F, K)
+        self.w4_rows = _fp4_views(scratch.weights4, K, F)
+        self.workspace = scratch.workspace
+        # gradients
+        self.dW, self.db, self.dgamma = e(K, F), e(F), e(K)
+
+    def forward(self, X, rowptr, colidx, R=None, S=None):
+        """H from X (N x K fp32) and the stream R, to which X is added in place (or into S)."""
+        S = R if S is None else S
+        B.bigcn_rms_norm_forward(X, self.gamma, self.eps, R=R, S=S, Y=self.Y, rstd=self.rstd,
+                                 q=self.q, exps=self.exps)
+        B.bigcn_fp4_pack(self.Y, *self.y4)
+        B.bigcn_fp4_pack_columns(self.W, *self.w4)
+        B.bigcn_fp4_gemm(*self.y4, *self.w4, self.K, self.Z, bias=self.b)
+        B.bigcn_spmm_norm(rowptr, colidx, self.Z, self.H)
+        return self.H
+
+    def backward(self, dH, rowptr, colidx, dS=None):
+        """The gradients (dW, db, dgamma, dX) from dH = dL/dH (N x F) and, where the stream goes on
+        behind this layer, dS = dL/dS by that way (N x K), in whose place dX then comes."""
+        B.bigcn_spmm_norm(rowptr, colidx, dH, self.G)
+        B.bigcn_checkpoint_weight_grad(self.q, self.exps, self.G, self.workspace, self.dW,
+                                       gamma=self.gamma, db=self.db)
+        B.bigcn_fp4_pack(self.G, *self.g4)
+        B.bigcn_fp4_pack(self.W, *self.w4_rows)
+        B.bigcn_fp4_gemm(*self.g4, *self.w4_rows, self.F, self.dY)
+        dX = self.dX if dS is None else dS
+        B.bigcn_rms_norm_backward(self.dY, self.gamma, self.rstd, self.workspace, q=self.q,
+                                  exps=self.exps, dS=dS, dX=dX, dgamma=self.dgamma)
+        return self.dW, self.db, self.dgamma, dX
+
+    def gradients(self):
+        return [self.dW, self.db, self.dgamma]
+
+
+class GradientClip:
+    """Scales the gradients of ``layers`` (anything with ``gradients()``), in place, to at most a norm
+    of all together; ``norm`` holds what it was. Their buffers are looked up once."""
+
+    def __init__(self, layers):
+        self.list = B.TensorList([t for layer in layers for t in layer.gradients()])
+        device = self.list.tensors[0].device
+        self.norm = torch.empty(1, dtype=torch.float32, device=device)
+        self.workspace = torch.empty(B.bigcn_grad_norm_workspace_bytes(self.list), dtype=torch.uint8,
+                                     device=device)
+
+    def __call__(self, max_norm):
+        B.bigcn_clip_grad_norm(self.list, max_norm, self.norm, self.workspace)
+        return self.norm
