@@ -7,7 +7,7 @@
 //
 // Roles of a CTA (12 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
 // codes, warps 2 and 3 bring A's and B's scale bytes, 16 groups (two stages) of a row at a time and
-// loaded while the previous are used, warp 1 issues the MMAs, warps 4-11 take the sums out, each every
+// asked for several such units ahead, warp 1 issues the MMAs, warps 4-11 take the sums out, each every
 // second 32 columns of the 32 rows that it may read. They meet on mbarriers only:
 //   full[stage]   its copies have landed        empty[stage]  its MMAs are done
 //   summed[acc]   a tile's MMAs are done        taken[acc]    its sums were taken
@@ -35,9 +35,12 @@ struct Fp4Shape {
     static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of B's scales
     static constexpr int kScales = 2 * (1 + kChunks) * kScaleChunk;
     static constexpr int kStage = kA + kB + kScales;
-    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 5 : 7;
+    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 5 : NT >= 64 ? 6 : 7;
     static constexpr int kStaging = kOutWarps * 32 * 33 * 4;
-    static constexpr int kSmem = 1024 + kStages * kStage + kStaging;
+    static constexpr int kRowsB = (NT + 31) / 32;                   // rows of B a lane of its scale warp has
+    static constexpr int kAheadA = 6, kAheadB = 3;                  // units of scale bytes in flight
+    static constexpr int kRings = (kAheadA * 4 + kAheadB * kRowsB) * 512;
+    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kRings;
     static constexpr int kAccs = NT > 128 ? 1 : 2;
     static constexpr int kScaleCols = 8 * (1 + kChunks);            // of tensor memory, a stage
     static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
@@ -132,29 +135,32 @@ __device__ __forceinline__ void store_sums(const float *stage, T *z, int64_t ldz
     }
 }
 
-// Scale bytes of unit u (16 groups) of the rows row0 + lane, + 32, ...: four words a row, zeros behind
-// the last group and the last row, whatever memory holds there. `wide`: rows aligned to 16 bytes.
+// Asks for the scale bytes of unit u (16 groups) of the rows row0 + lane, + 32, ...: four words a row,
+// zeros behind the last group and the last row, whatever memory holds there, to `to` + 512 j.
+// `wide`: rows aligned to 16 bytes.
 template <int R>
-__device__ __forceinline__ void load_scales(uint4 (&w)[R], const uint8_t *exps, int64_t ld, int64_t row0,
-                                            int64_t rows, int groups, int u, int lane, bool wide) {
+__device__ __forceinline__ void copy_unit(uint32_t to, const uint8_t *exps, int64_t ld, int64_t row0,
+                                          int64_t rows, int groups, int u, int lane, bool wide) {
     const int left = groups - u * kUnit;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int64_t i = row0 + 32 * j + lane;
-        w[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (i >= rows) continue;
-        const uint8_t *p = exps + i * ld + u * kUnit;
-        if (wide && left >= kUnit) {
-            w[j] = __ldg(reinterpret_cast<const uint4 *>(p));
+        const bool in = i < rows;
+        const uint8_t *p = exps + (in ? i * ld + u * kUnit : 0);
+        const uint32_t at = to + uint32_t(j * 512);
+        if (wide) {
+            const uint32_t n = in ? uint32_t(min(left, 16)) : 0u;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(p), "r"(n)
+                         : "memory");
         } else {
-            const uint32_t *q = reinterpret_cast<const uint32_t *>(p);
-            auto word = [&](int h) {
-                const int n = left - 4 * h;
-                return n <= 0 ? 0u : n >= 4 ? __ldg(q + h) : __ldg(q + h) & ((1u << (8 * n)) - 1u);
-            };
-            w[j] = make_uint4(word(0), word(1), word(2), word(3));
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int n = in ? min(max(left - 4 * h, 0), 4) : 0;
+                copy4(at + uint32_t(4 * h), n > 0 ? p + 4 * h : exps, uint32_t(n));
+            }
         }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
 }
 // Word h of stage `half` of a unit, of rows lane, lane + 32, ...: 16 bytes for each 128 rows.
 template <int R>
@@ -196,37 +202,54 @@ struct Tile {
     }
 };
 
-// A scale warp's work: R rows a lane, chunks from `offset` of a stage on.
-template <int NT, int R>
+// A scale warp's work: R rows a lane, chunks from `offset` of a stage on. Each lane has a ring of its own
+// of kAhead units, which it alone fills (by asynchronous copies, kAhead - 1 units ahead) and reads.
+template <int NT, int R, int kAhead>
 __device__ __forceinline__ void bring_scales(const Fp4GemmArgs &p, bool a, uint32_t base, uint32_t offset,
+                                             uint32_t ring,
                                              const uint64_t *empty, const uint64_t *full,
                                              volatile uint32_t *stopv, int stages, int lane) {
     using S = Fp4Shape<NT>;
     const uint8_t *exps = a ? p.a_exps : p.b_exps;
     const int64_t rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
     const bool wide = (reinterpret_cast<uintptr_t>(exps) & 15) == 0 && ld % 16 == 0;
-    auto load = [&](int64_t t, int u, uint4 (&w)[R]) {
-        const Tile tile(t, p.nt, NT);
-        load_scales<R>(w, exps, ld, a ? tile.m0 : tile.n0, rows, p.groups, u, lane, wide);
-    };
-    int s = 0;
-    uint32_t parity = 1u;
-    uint4 next[R];
-    int64_t t = blockIdx.x;
-    int u = 0;
     const int units = (stages + 1) / 2;
-    if (t < p.tiles) load(t, 0, next);
-    while (t < p.tiles) {
+    int64_t t_next = blockIdx.x;
+    int u_next = 0, slot_next = 0;
+    const uint32_t own = ring + uint32_t(lane * 16);
+    auto ask = [&] {
+        if (t_next < p.tiles) {
+            const Tile tile(t_next, p.nt, NT);
+            copy_unit<R>(own + uint32_t(slot_next * R * 512), exps, ld, a ? tile.m0 : tile.n0, rows,
+                         p.groups, u_next, lane, wide);
+            if (++u_next == units) u_next = 0, t_next += gridDim.x;
+        } else {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        if (++slot_next == kAhead) slot_next = 0;
+    };
+#pragma unroll 1
+    for (int i = 0; i < kAhead - 1; ++i) ask();
+    int s = 0, u = 0, slot = 0;
+    uint32_t parity = 1u;
+    for (int64_t t = blockIdx.x; t < p.tiles;) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
         uint4 w[R];
 #pragma unroll
-        for (int j = 0; j < R; ++j) w[j] = next[j];
+        for (int j = 0; j < R; ++j)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[j].x), "=r"(w[j].y), "=r"(w[j].z), "=r"(w[j].w)
+                         : "r"(own + uint32_t((slot * R + j) * 512))
+                         : "memory");
+        if (++slot == kAhead) slot = 0;
+        ask();
         const int n = min(2, stages - 2 * u);
         if (++u == units) u = 0, t += gridDim.x;
-        if (t < p.tiles) load(t, u, next);
         for (int half = 0; half < n; ++half) {
             if (!__all_sync(kFullMask, wait_unless(smem_addr(&empty[s]), parity, stopv))) {
                 *stopv = 1u;
-                return;
+                t = p.tiles;
+                break;
             }
             store_scales<R>(base + uint32_t(s * S::kStage) + offset, w, half, lane);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -235,6 +258,8 @@ __device__ __forceinline__ void bring_scales(const Fp4GemmArgs &p, bool a, uint3
             if (++s == S::kStages) s = 0, parity ^= 1u;
         }
     }
+    // What is still in flight lands before the shared memory is given up.
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename T, int NT>
@@ -275,6 +300,7 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     const uint32_t tmem = tmem_base;
     volatile uint32_t *const stopv = &stop;
     const int stages = (p.groups + 7) / 8;              // of a tile
+    const uint32_t rings = base + uint32_t(kStages * S::kStage + S::kStaging);
 
     if (warp == 0) {
         // Copies into the ring of stages.
@@ -304,10 +330,11 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
         for (int it = issued > kStages ? issued - kStages : 0; it < issued; ++it)
             mbar_wait(smem_addr(&full[it % kStages]), uint32_t(it / kStages) & 1u);
     } else if (warp == 2) {
-        bring_scales<NT, 4>(p, true, base, S::kA + S::kB, empty, full, stopv, stages, lane);
+        bring_scales<NT, 4, S::kAheadA>(p, true, base, S::kA + S::kB, rings, empty, full, stopv, stages, lane);
     } else if (warp == 3) {
-        bring_scales<NT, (NT + 31) / 32>(p, false, base, S::kA + S::kB + 2 * kScaleChunk, empty, full,
-                                         stopv, stages, lane);
+        bring_scales<NT, S::kRowsB, S::kAheadB>(p, false, base, S::kA + S::kB + 2 * kScaleChunk,
+                                                rings + S::kAheadA * 4 * 512, empty, full, stopv, stages,
+                                                lane);
     } else if (warp == 1) {
         // The warp stays together, one lane issues.
         int s = 0, b = 0;
