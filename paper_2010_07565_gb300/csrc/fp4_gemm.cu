@@ -2,15 +2,20 @@
 // tensor cores: tcgen05 block-scaled e2m1 x e2m1 with a ue8m0 scale per 32 columns of either
 // operand, fp32 accumulators in tensor memory. Codes go by tensor copies from memory into their
 // swizzled places (128 bytes, 256 columns, of a row a stage). The scale bytes, four groups to a word,
-// go by way of registers to where the tensor core's copy into tensor memory wants them: of 128
-// rows, row r at word (r mod 32) 4 + r / 32, so a lane's words of rows lane, lane + 32, ... are 16 bytes.
+// go to tensor memory as the MMAs read them: of 128 rows, row r's word in column r / 32 and in lane r
+// mod 32 of each quarter of the lanes, written by a warp of each quarter.
 //
-// Roles of a CTA (12 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
-// codes, warps 2 and 3 bring A's and B's scale bytes, 16 groups (two stages) of a row at a time and
-// asked for several such units ahead, warp 1 issues the MMAs, warps 4-11 take the sums out, each every
-// second 32 columns of the 32 rows that it may read. They meet on mbarriers only:
-//   full[stage]   its copies have landed        empty[stage]  its MMAs are done
-//   summed[acc]   a tile's MMAs are done        taken[acc]    its sums were taken
+// Roles of a CTA (16 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
+// codes; warps 2 and 3 ask for A's and B's scale bytes, a unit of 16 groups (two stages) of a row at a
+// time and several units ahead; warps 12-15 put them into tensor memory; warp 1 issues the MMAs; warps
+// 4-11 take the sums out, each kBatch columns at a time of the 32 rows that it may read. They
+// meet on mbarriers only:
+//   full[stage]    its codes have landed         empty[stage]    its MMAs are done
+//   loaded[slot]   a unit's scale bytes landed   freed[slot]     they were read
+//   filled[unit]   they are in tensor memory     used[unit]      the unit's MMAs are done
+//   summed[acc]    a tile's MMAs are done        taken[acc]      its sums were taken
+// (By way of shared memory, places filled by the threads that had asked for the bytes, each unit cost 1500
+// cycles: the fence before the tensor core's own copy waits for all that its thread still has under way.)
 #include "fp4.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -22,30 +27,33 @@ __device__ unsigned int g_fp4_timeouts;
 
 namespace {
 
-constexpr int kGemmThreads = 384;
 constexpr int kOutWarps = 8;            // that take the sums out
-constexpr int kUnit = 16;               // groups whose scale bytes are loaded at a time: two stages'
+constexpr int kUnit = 16;               // groups whose scale bytes are brought at a time: two stages'
+constexpr int kUnits = 4;               // of scale bytes in tensor memory
+constexpr int kSlots = 6;               // units of scale bytes on their way or in shared memory
 constexpr int kTmemCols = 512;
-constexpr int kScaleChunk = 512;        // bytes: a word of scales of 128 rows
+constexpr int kGemmThreads = 512;
 constexpr int kMaxGemmCols = 1 << 15;   // K: at most 512 accumulating MMAs (see the header)
 
 template <int NT>
 struct Fp4Shape {
     static constexpr int kA = kUmmaM * 128, kB = NT * 128;
-    static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of B's scales
-    static constexpr int kScales = 2 * (1 + kChunks) * kScaleChunk;
-    static constexpr int kStage = kA + kB + kScales;
-    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 5 : NT >= 64 ? 6 : 7;
-    static constexpr int kStaging = kOutWarps * 32 * 33 * 4;
-    static constexpr int kRowsB = (NT + 31) / 32;                   // rows of B a lane of its scale warp has
-    static constexpr int kAheadA = 6, kAheadB = 3;                  // units of scale bytes in flight
-    static constexpr int kRings = (kAheadA * 4 + kAheadB * kRowsB) * 512;
-    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kRings;
+    static constexpr int kStage = kA + kB;
+    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 4 : NT >= 64 ? 5 : 6;
+    static constexpr int kRowsB = NT / 32;                          // a lane of B's scales has
+    static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of 128 rows of B
+    static constexpr int kSlot = (4 + kRowsB) * 512;                // 16 bytes of each row
+    static constexpr int kScaleCols = 16 * (1 + kChunks);           // of tensor memory, a unit
+    // Columns that a warp stages at a time, and words from one staged row to the next: accesses of 4, 8
+    // and 16 bytes of a lane's row, or of a row by neighbouring lanes, then fall into different banks.
+    static constexpr int kBatch = NT >= 256 ? 32 : NT >= 64 ? 64 : 32;
+    static constexpr int kPitch = kBatch + 4;
+    static constexpr int kStaging = kOutWarps * 32 * kPitch * 4;
+    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kSlots * kSlot;
     static constexpr int kAccs = NT > 128 ? 1 : 2;
-    static constexpr int kScaleCols = 8 * (1 + kChunks);            // of tensor memory, a stage
     static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
     static_assert(kSmem <= 227 * 1024 - 1024, "shared memory per CTA");
-    static_assert(kAccs * NT + kStages * kScaleCols <= kTmemCols, "tensor memory per CTA");
+    static_assert(kAccs * NT + kUnits * kScaleCols <= kTmemCols, "tensor memory per CTA");
 };
 
 struct Fp4GemmArgs {
@@ -60,6 +68,7 @@ struct Fp4GemmArgs {
     const float *bias;       // nullable
     void *Z;
     int64_t ldz;
+    int vec;                 // bytes that Z and its rows are aligned to, at most 16
 };
 
 // Instruction descriptor of the block-scaled product: e2m1 x e2m1, both K-major, ue8m0 scales, M =
@@ -77,113 +86,74 @@ __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint
         "p;\n}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate ? 1u : 0u));
 }
-// 512 bytes, 32 rows of 16, to four columns of tensor memory, the same in each quarter of its lanes.
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr) {
-    uint64_t d = uint64_t((saddr >> 4) & 0x3FFFu);
-    d |= uint64_t(128 >> 4) << 32;              // groups of 8 rows 128 bytes apart, no swizzle
-    d |= uint64_t(1) << 46;
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d));
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
 }
 
-// A warp's 32 rows by 32 columns of sums from shared memory (pitch 33) to Z, with the bias: a row
-// at a time in fp32, two in 16 bits, where `pairs` says that two columns are one aligned word.
-template <typename T>
+// A warp's rows of sums, kBatch columns from shared memory to Z, with the bias: VB bytes of a row a lane
+// (Z's rows are aligned to them), neighbouring lanes along the row.
+template <typename T, int kBatch, int VB>
 __device__ __forceinline__ void store_sums(const float *stage, T *z, int64_t ldz, int rows, int cols,
-                                           const float *bias, int lane, bool pairs) {
-    if constexpr (sizeof(T) == 4) {
-        const float b = bias && lane < cols ? __ldg(bias + lane) : 0.0f;
-        T *to = z + lane;
-        if (lane >= cols) return;
-        if (rows == 32) {
+                                           const float *bias, int lane) {
+    constexpr int kPitch = kBatch + 4, kCols = VB / int(sizeof(T));
+    constexpr int kLanes = kBatch / kCols < 32 ? kBatch / kCols : 32;       // of a row
+    constexpr int kParts = kBatch / kCols / kLanes, kRows = 32 / kLanes;
+    const int r0 = lane / kLanes, c0 = lane % kLanes * kCols;
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += 16) {
-                float v[16];
+    for (int part = 0; part < kParts; ++part) {
+        const int c = c0 + part * kLanes * kCols, n = cols - c;
+        if (n <= 0) continue;
+        float b[kCols];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) v[r] = stage[(r0 + r) * 33 + lane] + b;
-#pragma unroll
-                for (int r = 0; r < 16; ++r, to += ldz) *to = v[r];
-            }
-        } else {
-            for (int r = 0; r < rows; ++r, to += ldz) *to = stage[r * 33 + lane] + b;
-        }
-    } else {
-        const int c = 2 * (lane & 15), r0 = lane >> 4;
-        const bool first = c < cols, second = c + 1 < cols;
-        const float b0 = bias && first ? __ldg(bias + c) : 0.0f;
-        const float b1 = bias && second ? __ldg(bias + c + 1) : 0.0f;
+        for (int e = 0; e < kCols; ++e) b[e] = bias && e < n ? __ldg(bias + c + e) : 0.0f;
+        const float *from = stage + r0 * kPitch + c;
         T *to = z + r0 * ldz + c;
-        if (!first) return;
-#pragma unroll 8
-        for (int r = r0; r < 32; r += 2, to += 2 * ldz) {
-            if (r >= rows) break;
-            const float v0 = stage[r * 33 + c] + b0, v1 = stage[r * 33 + c + 1] + b1;
-            if (pairs && second) {
-                uint32_t w;
-                if constexpr (std::is_same<T, __half>::value) {
-                    const __half2 x = __floats2half2_rn(v0, v1);
-                    w = *reinterpret_cast<const uint32_t *>(&x);
+        constexpr int kAtOnce = kCols >= 4 ? 4 : 8;
+#pragma unroll 1
+        for (int r = r0; r < rows; r += kAtOnce * kRows) {
+            float v[kAtOnce][kCols];
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                const float *f = from + q * kRows * kPitch;
+                if constexpr (kCols % 4 == 0) {
+#pragma unroll
+                    for (int e = 0; e < kCols; e += 4)
+                        *reinterpret_cast<float4 *>(&v[q][e]) = *reinterpret_cast<const float4 *>(f + e);
+                } else if constexpr (kCols == 2) {
+                    *reinterpret_cast<float2 *>(&v[q][0]) = *reinterpret_cast<const float2 *>(f);
                 } else {
-                    const __nv_bfloat162 x = __floats2bfloat162_rn(v0, v1);
-                    w = *reinterpret_cast<const uint32_t *>(&x);
-                }
-                *reinterpret_cast<uint32_t *>(to) = w;
-            } else {
-                to[0] = from_f32<T>(v0);
-                if (second) to[1] = from_f32<T>(v1);
-            }
-        }
-    }
-}
-
-// Asks for the scale bytes of unit u (16 groups) of the rows row0 + lane, + 32, ...: four words a row,
-// zeros behind the last group and the last row, whatever memory holds there, to `to` + 512 j.
-// `wide`: rows aligned to 16 bytes.
-template <int R>
-__device__ __forceinline__ void copy_unit(uint32_t to, const uint8_t *exps, int64_t ld, int64_t row0,
-                                          int64_t rows, int groups, int u, int lane, bool wide) {
-    const int left = groups - u * kUnit;
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int64_t i = row0 + 32 * j + lane;
-        const bool in = i < rows;
-        const uint8_t *p = exps + (in ? i * ld + u * kUnit : 0);
-        const uint32_t at = to + uint32_t(j * 512);
-        if (wide) {
-            const uint32_t n = in ? uint32_t(min(left, 16)) : 0u;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(p), "r"(n)
-                         : "memory");
-        } else {
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const int n = in ? min(max(left - 4 * h, 0), 4) : 0;
-                copy4(at + uint32_t(4 * h), n > 0 ? p + 4 * h : exps, uint32_t(n));
-            }
-        }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-}
-// Word h of stage `half` of a unit, of rows lane, lane + 32, ...: 16 bytes for each 128 rows.
-template <int R>
-__device__ __forceinline__ void store_scales(uint32_t to, const uint4 (&w)[R], int half, int lane) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < (R + 3) / 4; ++c) {
-            uint32_t v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (4 * c + j < R) {
-                    const uint4 &x = w[4 * c + j < R ? 4 * c + j : 0];
-                    v[j] = half ? (h ? x.w : x.z) : (h ? x.y : x.x);
-                } else {
-                    v[j] = 0u;
+                    v[q][0] = *f;
                 }
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                             to + uint32_t((h * ((R + 3) / 4) + c) * kScaleChunk + lane * 16)),
-                         "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
-                         : "memory");
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                if (r + q * kRows >= rows) break;
+                T out[kCols];
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) out[e] = from_f32<T>(v[q][e] + b[e]);
+                if (n >= kCols) {
+                    if constexpr (VB == 16)
+                        *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(out);
+                    else if constexpr (VB == 8)
+                        *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(out);
+                    else if constexpr (VB == 4)
+                        *reinterpret_cast<uint32_t *>(to) = *reinterpret_cast<const uint32_t *>(out);
+                    else *to = out[0];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kCols; ++e)
+                        if (e < n) to[e] = out[e];
+                }
+                to += kRows * ldz;
+            }
+            from += kAtOnce * kRows * kPitch;
         }
+    }
 }
 
 // Tile t: its first row and first column.
@@ -202,64 +172,118 @@ struct Tile {
     }
 };
 
-// A scale warp's work: R rows a lane, chunks from `offset` of a stage on. Each lane has a ring of its own
-// of kAhead units, which it alone fills (by asynchronous copies, kAhead - 1 units ahead) and reads.
-template <int NT, int R, int kAhead>
-__device__ __forceinline__ void bring_scales(const Fp4GemmArgs &p, bool a, uint32_t base, uint32_t offset,
-                                             uint32_t ring,
-                                             const uint64_t *empty, const uint64_t *full,
-                                             volatile uint32_t *stopv, int stages, int lane) {
-    using S = Fp4Shape<NT>;
-    const uint8_t *exps = a ? p.a_exps : p.b_exps;
+// A's or B's scale warp: 16 bytes of R rows a lane, unit after unit, into its part of the ring of slots.
+// One lane arrives for all once a unit has landed, kLag units behind what is asked for.
+template <int NT, int R>
+__device__ __forceinline__ void ask_scales(const Fp4GemmArgs &p, bool a, uint32_t slots,
+                                           const uint64_t *freed, const uint64_t *loaded,
+                                           volatile uint32_t *stopv, int lane) {
+    const uint8_t *const exps = a ? p.a_exps : p.b_exps;
     const int64_t rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
     const bool wide = (reinterpret_cast<uintptr_t>(exps) & 15) == 0 && ld % 16 == 0;
-    const int units = (stages + 1) / 2;
-    int64_t t_next = blockIdx.x;
-    int u_next = 0, slot_next = 0;
-    const uint32_t own = ring + uint32_t(lane * 16);
-    auto ask = [&] {
-        if (t_next < p.tiles) {
-            const Tile tile(t_next, p.nt, NT);
-            copy_unit<R>(own + uint32_t(slot_next * R * 512), exps, ld, a ? tile.m0 : tile.n0, rows,
-                         p.groups, u_next, lane, wide);
-            if (++u_next == units) u_next = 0, t_next += gridDim.x;
-        } else {
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-        if (++slot_next == kAhead) slot_next = 0;
-    };
-#pragma unroll 1
-    for (int i = 0; i < kAhead - 1; ++i) ask();
-    int s = 0, u = 0, slot = 0;
+    const int units = (p.groups + kUnit - 1) / kUnit;
+    constexpr int kLag = kSlots - 2;
+    int slot = 0, asked = 0;
     uint32_t parity = 1u;
-    for (int64_t t = blockIdx.x; t < p.tiles;) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
-        uint4 w[R];
+    bool ok = true;
+    auto landed = [&](int n) {              // the n-th unit of all
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&loaded[n % kSlots]));
+    };
+    for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+        const Tile tile(t, p.nt, NT);
+        const uint8_t *row[R];
+        bool in[R];
 #pragma unroll
-        for (int j = 0; j < R; ++j)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(w[j].x), "=r"(w[j].y), "=r"(w[j].z), "=r"(w[j].w)
-                         : "r"(own + uint32_t((slot * R + j) * 512))
-                         : "memory");
-        if (++slot == kAhead) slot = 0;
-        ask();
-        const int n = min(2, stages - 2 * u);
-        if (++u == units) u = 0, t += gridDim.x;
-        for (int half = 0; half < n; ++half) {
-            if (!__all_sync(kFullMask, wait_unless(smem_addr(&empty[s]), parity, stopv))) {
+        for (int j = 0; j < R; ++j) {
+            const int64_t i = (a ? tile.m0 : tile.n0) + 32 * j + lane;
+            in[j] = i < rows;
+            row[j] = exps + (in[j] ? i * ld : 0);
+        }
+        for (int u = 0; u < units; ++u) {
+            ok = __all_sync(kFullMask, wait_unless(smem_addr(&freed[slot]), parity, stopv));
+            if (!ok) {
                 *stopv = 1u;
-                t = p.tiles;
                 break;
             }
-            store_scales<R>(base + uint32_t(s * S::kStage) + offset, w, half, lane);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&full[s]));
-            if (++s == S::kStages) s = 0, parity ^= 1u;
+            const int left = p.groups - u * kUnit;
+            const uint32_t to = slots + uint32_t(slot * Fp4Shape<NT>::kSlot + lane * 16);
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                // (Zeros behind the last group and the last row, whatever memory holds there; the
+                // words behind the last group's are never used.)
+                const uint8_t *from = row[j] + u * kUnit;
+                if (wide) {
+                    const uint32_t n = in[j] ? uint32_t(min(left, kUnit)) : 0u;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + uint32_t(j * 512)),
+                                 "l"(from), "r"(n)
+                                 : "memory");
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (left > 4 * h)
+                            copy4(to + uint32_t(j * 512 + 4 * h), from + 4 * h,
+                                  in[j] ? uint32_t(min(left - 4 * h, 4)) : 0u);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (asked >= kLag) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+                landed(asked - kLag);
+            }
+            ++asked;
+            if (++slot == kSlots) slot = 0, parity ^= 1u;
         }
     }
-    // What is still in flight lands before the shared memory is given up.
     asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int n = asked > kLag ? asked - kLag : 0; n < asked; ++n) landed(n);
+}
+
+// A placing warp: a unit's words to tensor memory, in the quarter of its lanes that the warp may write.
+// Word h of 128 rows is four columns; A's and B's of a word lie together.
+template <int NT>
+__device__ __forceinline__ void place_scales(const Fp4GemmArgs &p, uint32_t slots, uint32_t tmem,
+                                             const uint64_t *freed, const uint64_t *loaded,
+                                             const uint64_t *used, const uint64_t *filled,
+                                             volatile uint32_t *stopv, int lane) {
+    using S = Fp4Shape<NT>;
+    const int units = (p.groups + kUnit - 1) / kUnit;
+    int slot = 0, q = 0;
+    uint32_t slot_parity = 0u, parity = 1u;
+    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x)
+        for (int u = 0; u < units; ++u) {
+            const bool go = wait_unless(smem_addr(&loaded[slot]), slot_parity, stopv) &&
+                            wait_unless(smem_addr(&used[q]), parity, stopv);
+            if (!__all_sync(kFullMask, go)) {
+                *stopv = 1u;
+                return;
+            }
+            uint32_t v[S::kScaleCols];
+#pragma unroll
+            for (int j = 0; j < 4 * (1 + S::kChunks); ++j) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+                if (j < 4 + S::kRowsB)
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(slots + uint32_t(slot * S::kSlot + j * 512 + lane * 16))
+                                 : "memory");
+#pragma unroll
+                for (int h = 0; h < 4; ++h) v[h * 4 * (1 + S::kChunks) + j] = w[h];
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t to = tmem + uint32_t(q * S::kScaleCols);
+#pragma unroll
+            for (int c = 0; c < S::kScaleCols; c += 16) tmem_st16(to + uint32_t(c), v + c);
+            tmem_wait_st();
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_addr(&filled[q]));
+                mbar_arrive(smem_addr(&freed[slot]));
+            }
+            if (++slot == kSlots) slot = 0, slot_parity ^= 1u;
+            if (++q == kUnits) q = 0, parity ^= 1u;
+        }
 }
 
 template <typename T, int NT>
@@ -268,12 +292,14 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     using S = Fp4Shape<NT>;
     constexpr int kStages = S::kStages;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], summed[S::kAccs], taken[S::kAccs],
-        done;
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], loaded[kSlots], freed[kSlots],
+        filled[kUnits], used[kUnits], summed[S::kAccs], taken[S::kAccs], done;
     __shared__ uint32_t tmem_base, stop;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    const uint32_t staging = base + uint32_t(kStages * S::kStage);
+    const uint32_t slots = staging + uint32_t(S::kStaging);
 
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
@@ -283,8 +309,16 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&full[s]), 3);          // both scale warps; the boxes' bytes
+            mbar_init(smem_addr(&full[s]), 1);
             mbar_init(smem_addr(&empty[s]), 1);
+        }
+        for (int q = 0; q < kSlots; ++q) {
+            mbar_init(smem_addr(&loaded[q]), 2);            // both scale warps
+            mbar_init(smem_addr(&freed[q]), 4);
+        }
+        for (int q = 0; q < kUnits; ++q) {
+            mbar_init(smem_addr(&filled[q]), 4);
+            mbar_init(smem_addr(&used[q]), 1);
         }
         for (int b = 0; b < S::kAccs; ++b) {
             mbar_init(smem_addr(&summed[b]), 1);
@@ -300,7 +334,6 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     const uint32_t tmem = tmem_base;
     volatile uint32_t *const stopv = &stop;
     const int stages = (p.groups + 7) / 8;              // of a tile
-    const uint32_t rings = base + uint32_t(kStages * S::kStage + S::kStaging);
 
     if (warp == 0) {
         // Copies into the ring of stages.
@@ -330,70 +363,69 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
         for (int it = issued > kStages ? issued - kStages : 0; it < issued; ++it)
             mbar_wait(smem_addr(&full[it % kStages]), uint32_t(it / kStages) & 1u);
     } else if (warp == 2) {
-        bring_scales<NT, 4, S::kAheadA>(p, true, base, S::kA + S::kB, rings, empty, full, stopv, stages, lane);
+        ask_scales<NT, 4>(p, true, slots, freed, loaded, stopv, lane);
     } else if (warp == 3) {
-        bring_scales<NT, S::kRowsB, S::kAheadB>(p, false, base, S::kA + S::kB + 2 * kScaleChunk,
-                                                rings + S::kAheadA * 4 * 512, empty, full, stopv, stages,
-                                                lane);
+        ask_scales<NT, S::kRowsB>(p, false, slots + 4 * 512, freed, loaded, stopv, lane);
+    } else if (warp >= 12) {
+        place_scales<NT>(p, slots, tmem + (uint32_t(32 * (warp & 3)) << 16) + S::kAccs * NT, freed, loaded,
+                         used, filled, stopv, lane);
     } else if (warp == 1) {
-        // The warp stays together, one lane issues.
-        int s = 0, b = 0;
-        uint32_t parity = 0u, acc_parity = 1u;
-        bool any = false, ok = true;
-        for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-            const int n = (min(NT, p.F - Tile(t, p.nt, NT).n0) + 31) / 32 * 32;
-            const uint32_t acc = tmem + uint32_t(b * NT);
-            ok = __all_sync(kFullMask, wait_unless(smem_addr(&taken[b]), acc_parity, stopv));
-            for (int st = 0; ok && st < stages; ++st) {
-                ok = __all_sync(kFullMask, wait_unless(smem_addr(&full[s]), parity, stopv));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t at = base + uint32_t(s * S::kStage);
-                const uint32_t scales = at + S::kA + S::kB;
-                // A stage has columns of tensor memory of its own: its MMAs have ended when it is
-                // filled again.
-                const uint32_t sa = tmem + uint32_t(S::kAccs * NT + s * S::kScaleCols), sb = sa + 8;
-                const uint64_t da = sw128_desc(at), db = sw128_desc(at + S::kA);
-                const int steps = min(4, (p.groups - st * 8 + 1) / 2);
-                if (elect_one()) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        copy_scales(sa + uint32_t(4 * h), scales + uint32_t(h * kScaleChunk));
-#pragma unroll
-                        for (int c = 0; c < S::kChunks; ++c)
-                            copy_scales(sb + uint32_t(4 * (h * S::kChunks + c)),
-                                        scales + uint32_t((2 + h * S::kChunks + c) * kScaleChunk));
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (k >= steps) break;
-                        mma_fp4(acc, da + uint32_t(2 * k), db + uint32_t(2 * k),
-                                fp4_idesc(n, uint32_t(k % 2) * 2u), sa + uint32_t(4 * (k / 2)),
-                                sb + uint32_t(4 * S::kChunks * (k / 2)), st > 0 || k > 0);
-                    }
-                    mma_commit(smem_addr(&empty[s]));
-                    if (st == stages - 1) mma_commit(smem_addr(&summed[b]));
-                }
-                __syncwarp();
-                any = true;
-                if (++s == kStages) s = 0, parity ^= 1u;
-            }
-            if (++b == S::kAccs) b = 0, acc_parity ^= 1u;
-        }
-        if (!ok) *stopv = 1u;
+        // One thread issues. A stage of 256 columns takes the tensor core 256 or 512 cycles; this loop
+        // has to stay below that, at four cycles and more an instruction.
         if (elect_one()) {
-            if (any) mma_commit(smem_addr(&done));
-            else mbar_arrive(smem_addr(&done));
+            const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty);
+            const uint32_t filled0 = smem_addr(filled), used0 = smem_addr(used);
+            const uint32_t scales0 = tmem + uint32_t(S::kAccs * NT);
+            const uint64_t desc0 = sw128_desc(base);
+            uint32_t s = 0, b = 0, q = 0, parity = 0u, acc_parity = 1u, unit_parity = 0u;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+                const int n = (min(NT, p.F - (p.nt == 1 ? 0 : Tile(t, p.nt, NT).n0)) + 31) / 32 * 32;
+                const uint32_t idesc = fp4_idesc(n, 0u), idesc2 = fp4_idesc(n, 2u);
+                const uint32_t acc = tmem + b * NT;
+                ok = wait_unless(smem_addr(&taken[b]), acc_parity, stopv);
+                if (!ok) break;
+                uint32_t word = 0u;             // the stage's scales, in tensor memory
+                bool more = false;              // (the first MMA starts the sum)
+                for (int left = p.groups, odd = 0; left > 0; left -= 8, odd ^= 1) {
+                    if (odd) {
+                        word += 8 * (1 + S::kChunks);
+                    } else {
+                        ok = wait_unless(filled0 + 8 * q, unit_parity, stopv);
+                        word = scales0 + q * S::kScaleCols;
+                    }
+                    ok = ok && wait_unless(full0 + 8 * s, parity, stopv);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = desc0 + s * (S::kStage / 16), db = da + S::kA / 16;
+                    constexpr uint32_t kNext = 4 * (1 + S::kChunks), kB = 4;
+                    mma_fp4(acc, da, db, idesc, word, word + kB, more);
+                    more = true;
+                    if (left > 2) mma_fp4(acc, da + 2, db + 2, idesc2, word, word + kB, true);
+                    if (left > 4) mma_fp4(acc, da + 4, db + 4, idesc, word + kNext, word + kNext + kB, true);
+                    if (left > 6) mma_fp4(acc, da + 6, db + 6, idesc2, word + kNext, word + kNext + kB, true);
+                    mma_commit(empty0 + 8 * s);
+                    if (++s == kStages) s = 0, parity ^= 1u;
+                    if (odd || left <= 8) {
+                        mma_commit(used0 + 8 * q);
+                        if (++q == kUnits) q = 0, unit_parity ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                mma_commit(smem_addr(&summed[b]));
+                if (++b == S::kAccs) b = 0, acc_parity ^= 1u;
+            }
+            if (!ok) *stopv = 1u;
+            mma_commit(smem_addr(&done));
         }
         __syncwarp();
     } else {
-        // Sums out, a warp the 32 lanes of tensor memory that it may read, every second 32 columns.
+        // Sums out, a warp the 32 lanes of tensor memory that it may read, every second kBatch columns.
         // Tiles whose waits ran out are NaN.
+        constexpr int kBatch = S::kBatch, kPitch = S::kPitch;
         const int quad = warp & 3, half = (warp - 4) >> 2;
-        float *const stage = reinterpret_cast<float *>(smem_raw + (base - raw) + kStages * S::kStage) +
-                             (warp - 4) * 32 * 33;
-        const bool pairs = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p.Z) & 3) == 0 &&
-                           p.ldz % 2 == 0;
+        float *const stage = reinterpret_cast<float *>(smem_raw + (staging - raw)) +
+                             (warp - 4) * 32 * kPitch;
         int b = 0;
         uint32_t parity = 0u;
         bool ok = true;
@@ -411,19 +443,36 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             T *z = static_cast<T *>(p.Z) + row0 * p.ldz + tile.n0;
             const float *bias = p.bias ? p.bias + tile.n0 : nullptr;
 #pragma unroll 1
-            for (int c = 32 * half; c < cols; c += 64) {
-                uint32_t v[32];
-                tmem_ld32(acc + uint32_t(c), v);
+            for (int c = kBatch * half; c < cols; c += 2 * kBatch) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    stage[lane * 33 + e] = __uint_as_float(ok ? v[e] : 0x7FC00000u);
+                for (int h = 0; h < kBatch; h += 32) {
+                    if (c + h >= cols) break;
+                    uint32_t v[32];
+                    tmem_ld32(acc + uint32_t(c + h), v);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4 *>(stage + lane * kPitch + h + e) =
+                            ok ? make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3])
+                               : make_uint4(0x7FC00000u, 0x7FC00000u, 0x7FC00000u, 0x7FC00000u);
+                }
+                if (c + 2 * kBatch >= cols) {       // the warp's last of this tile
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
+                }
                 __syncwarp();
-                store_sums<T>(stage, z + c, p.ldz, rows, cols - c, bias ? bias + c : nullptr, lane, pairs);
+                const float *bc = bias ? bias + c : nullptr;
+                if (p.vec == 16) store_sums<T, kBatch, 16>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
+                else if (p.vec == 8) store_sums<T, kBatch, 8>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
+                else if (p.vec == 4) store_sums<T, kBatch, 4>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
+                else if constexpr (sizeof(T) == 2)
+                    store_sums<T, kBatch, 2>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
                 __syncwarp();
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
+            if (kBatch * half >= cols) {            // no columns of this tile
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
+            }
             if (++b == S::kAccs) b = 0, parity ^= 1u;
         }
     }
@@ -518,6 +567,8 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     p.bias = bias;
     p.Z = Z;
     p.ldz = ldz;
+    const uint64_t where = uint64_t(uintptr_t(Z)) | uint64_t(N > 1 ? ldz : 0) * es | 16;
+    p.vec = int(where & (~where + 1));
     const unsigned grid = unsigned(p.tiles < dev.sm_count ? p.tiles : dev.sm_count);
     const cudaStream_t s = as_stream(stream);
     if (dtype == BIGCN_F32) launch_gemm<float>(p, NT, grid, s);
