@@ -5,17 +5,19 @@
 // go to tensor memory as the MMAs read them: of 128 rows, row r's word in column r / 32 and in lane r
 // mod 32 of each quarter of the lanes, written by a warp of each quarter.
 //
-// Roles of a CTA (16 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
+// Roles of a CTA (16 or 24 warps), which takes tiles of 128 rows by NT columns in turn: warp 0 copies the
 // codes; warps 2 and 3 ask for A's and B's scale bytes, a unit of 16 groups (two stages) of a row at a
-// time and several units ahead; warps 12-15 put them into tensor memory; warp 1 issues the MMAs; warps
-// 4-11 take the sums out, each kBatch columns at a time of the 32 rows that it may read. They
-// meet on mbarriers only:
-//   full[stage]    its codes have landed         empty[stage]    its MMAs are done
-//   loaded[slot]   a unit's scale bytes landed   freed[slot]     they were read
-//   filled[unit]   they are in tensor memory     used[unit]      the unit's MMAs are done
-//   summed[acc]    a tile's MMAs are done        taken[acc]      its sums were taken
-// (By way of shared memory, places filled by the threads that had asked for the bytes, each unit cost 1500
-// cycles: the fence before the tensor core's own copy waits for all that its thread still has under way.)
+// time and several units ahead; warps 4-7 put them into tensor memory; warp 1 issues the MMAs; the others
+// take the sums out, kBatch columns at a time of the 32 rows that a warp may read. They meet on
+// mbarriers:
+//   ready[stage]   its codes and scales are there    free[stage]   its MMAs are done
+//   loaded[slot]   a unit's scale bytes landed       read[slot]    they were read
+//   summed[acc]    a tile's MMAs are done            taken[acc]    its sums were taken
+// The thread that issues is the one to spare: 100 cycles a wait that finds its phase complete, 50 an MMA, 40
+// a commit (with barriers of their own for A, B and the scales it took 700 cycles a stage, of which
+// the MMAs need 512 with 256 columns). Scale bytes that came by way of shared memory, in places filled
+// by the threads that had asked for them, cost 1500 cycles a unit: the fence before the tensor core's
+// own copy waits for all that its thread still has under way.
 #include "fp4.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -27,33 +29,38 @@ __device__ unsigned int g_fp4_timeouts;
 
 namespace {
 
-constexpr int kOutWarps = 8;            // that take the sums out
 constexpr int kUnit = 16;               // groups whose scale bytes are brought at a time: two stages'
-constexpr int kUnits = 4;               // of scale bytes in tensor memory
-constexpr int kSlots = 6;               // units of scale bytes on their way or in shared memory
 constexpr int kTmemCols = 512;
-constexpr int kGemmThreads = 512;
 constexpr int kMaxGemmCols = 1 << 15;   // K: at most 512 accumulating MMAs (see the header)
 
-template <int NT>
+// kOnce: a CTA's columns are always the same and B's stages, at most kHeld, stay in shared memory.
+template <int NT, bool kOnce>
 struct Fp4Shape {
     static constexpr int kA = kUmmaM * 128, kB = NT * 128;
-    static constexpr int kStage = kA + kB;
-    static constexpr int kStages = NT >= 256 ? 3 : NT >= 128 ? 4 : NT >= 64 ? 5 : 6;
+    static constexpr int kHeld = kOnce ? 3 : 0;
+    static constexpr int kStage = kOnce ? kA : kA + kB;
+    static constexpr int kStages = NT >= 256 ? 4 : kOnce ? 5 : NT >= 128 ? 4 : 5;
     static constexpr int kRowsB = NT / 32;                          // a lane of B's scales has
     static constexpr int kChunks = NT > 128 ? NT / 128 : 1;         // of 128 rows of B
+    static constexpr int kSlots = NT >= 256 ? 2 : 6;                // units on their way or in shared memory
     static constexpr int kSlot = (4 + kRowsB) * 512;                // 16 bytes of each row
-    static constexpr int kScaleCols = 16 * (1 + kChunks);           // of tensor memory, a unit
-    // Columns that a warp stages at a time, and words from one staged row to the next: accesses of 4, 8
+    static constexpr int kScaleCols = 8 * (1 + kChunks);            // of tensor memory, a stage
+    // Warps that take the sums out. With kPair two of them, of the same quarter of the lanes, stage 64 columns
+    // together, half each, and store half the rows each: longer runs of a row at a time, and twice the
+    // warps to wait on memory.
+    static constexpr int kOutWarps = NT == 64 || NT == 128 ? 16 : 8;
+    static constexpr bool kPair = kOutWarps == 16;
+    static constexpr int kThreads = (8 + kOutWarps) * 32;
+    // Columns that are staged at a time, and words from one staged row to the next: accesses of 4, 8
     // and 16 bytes of a lane's row, or of a row by neighbouring lanes, then fall into different banks.
-    static constexpr int kBatch = NT >= 256 ? 32 : NT >= 64 ? 64 : 32;
+    static constexpr int kBatch = NT >= 256 ? 16 : NT >= 64 ? 64 : 32;
     static constexpr int kPitch = kBatch + 4;
-    static constexpr int kStaging = kOutWarps * 32 * kPitch * 4;
-    static constexpr int kSmem = 1024 + kStages * kStage + kStaging + kSlots * kSlot;
+    static constexpr int kStaging = 8 * 32 * kPitch * 4;
+    static constexpr int kSmem = 1024 + kStages * kStage + kHeld * kB + kStaging + kSlots * kSlot;
     static constexpr int kAccs = NT > 128 ? 1 : 2;
-    static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
+    static_assert(kA % 1024 == 0 && kB % 1024 == 0, "swizzled tiles start on 1024 bytes");
     static_assert(kSmem <= 227 * 1024 - 1024, "shared memory per CTA");
-    static_assert(kAccs * NT + kUnits * kScaleCols <= kTmemCols, "tensor memory per CTA");
+    static_assert(kAccs * NT + kStages * kScaleCols <= kTmemCols, "tensor memory per CTA");
 };
 
 struct Fp4GemmArgs {
@@ -64,11 +71,13 @@ struct Fp4GemmArgs {
     int F;
     int groups;              // of 32 columns
     int nt;                  // column tiles
-    int64_t tiles;
+    uint32_t mt;             // row tiles
+    uint32_t step_m, step_n; // from a CTA's tile to its next
     const float *bias;       // nullable
     void *Z;
     int64_t ldz;
-    int vec;                 // bytes that Z and its rows are aligned to, at most 16
+    int vec;                 // bytes that Z and its rows are aligned to, at most 32
+    bool direct;             // sums go straight to Z (store_direct)
 };
 
 // Instruction descriptor of the block-scaled product: e2m1 x e2m1, both K-major, ue8m0 scales, M =
@@ -86,103 +95,172 @@ __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint
         "p;\n}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate ? 1u : 0u));
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 
-// A warp's rows of sums, kBatch columns from shared memory to Z, with the bias: VB bytes of a row a lane
-// (Z's rows are aligned to them), neighbouring lanes along the row.
-template <typename T, int kBatch, int VB>
+template <typename T, int kCols>
+__device__ __forceinline__ void load_staged(const float *f, float (&v)[kCols]) {
+    if constexpr (kCols % 4 == 0) {
+#pragma unroll
+        for (int e = 0; e < kCols; e += 4)
+            *reinterpret_cast<float4 *>(&v[e]) = *reinterpret_cast<const float4 *>(f + e);
+    } else if constexpr (kCols == 2) {
+        *reinterpret_cast<float2 *>(&v[0]) = *reinterpret_cast<const float2 *>(f);
+    } else {
+        v[0] = *f;
+    }
+}
+template <typename T, int kCols>
+__device__ __forceinline__ void store_staged(T *to, const float (&v)[kCols], const float (&b)[kCols]) {
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (kCols == 4)
+            *reinterpret_cast<float4 *>(to) =
+                make_float4(v[0] + b[0], v[1] + b[1], v[2] + b[2], v[3] + b[3]);
+        else if constexpr (kCols == 2)
+            *reinterpret_cast<float2 *>(to) = make_float2(v[0] + b[0], v[1] + b[1]);
+        else *to = v[0] + b[0];
+    } else if constexpr (kCols == 1) {
+        *to = from_f32<T>(v[0] + b[0]);
+    } else {
+        uint32_t w[kCols / 2];
+#pragma unroll
+        for (int e = 0; e < kCols; e += 2) {
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 x = __floats2half2_rn(v[e] + b[e], v[e + 1] + b[e + 1]);
+                w[e / 2] = *reinterpret_cast<const uint32_t *>(&x);
+            } else {
+                const __nv_bfloat162 x = __floats2bfloat162_rn(v[e] + b[e], v[e + 1] + b[e + 1]);
+                w[e / 2] = *reinterpret_cast<const uint32_t *>(&x);
+            }
+        }
+        if constexpr (kCols == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (kCols == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(to) = w[0];
+    }
+}
+// kStore rows of sums, kBatch columns from shared memory to Z, with the bias: VB bytes of a row a lane (Z's
+// rows are aligned to them), neighbouring lanes along the row.
+template <typename T, int kBatch, int kStore, int VB>
 __device__ __forceinline__ void store_sums(const float *stage, T *z, int64_t ldz, int rows, int cols,
                                            const float *bias, int lane) {
     constexpr int kPitch = kBatch + 4, kCols = VB / int(sizeof(T));
     constexpr int kLanes = kBatch / kCols < 32 ? kBatch / kCols : 32;       // of a row
-    constexpr int kParts = kBatch / kCols / kLanes, kRows = 32 / kLanes;
+    constexpr int kParts = kBatch / kCols / kLanes, kRows = 32 / kLanes, kTurns = kStore / kRows;
+    constexpr int kMost = kCols >= 8 ? 4 : 8, kAtOnce = kTurns < kMost ? kTurns : kMost;
+    static_assert(kTurns > 0 && kTurns % kAtOnce == 0, "whole turns");
     const int r0 = lane / kLanes, c0 = lane % kLanes * kCols;
-#pragma unroll
+    const int64_t step = kRows * ldz;
+#pragma unroll 1
     for (int part = 0; part < kParts; ++part) {
         const int c = c0 + part * kLanes * kCols, n = cols - c;
-        if (n <= 0) continue;
         float b[kCols];
 #pragma unroll
         for (int e = 0; e < kCols; ++e) b[e] = bias && e < n ? __ldg(bias + c + e) : 0.0f;
         const float *from = stage + r0 * kPitch + c;
         T *to = z + r0 * ldz + c;
-        constexpr int kAtOnce = kCols >= 4 ? 4 : 8;
+        if (n >= kCols) {
 #pragma unroll 1
-        for (int r = r0; r < rows; r += kAtOnce * kRows) {
-            float v[kAtOnce][kCols];
+            for (int r = r0; r < rows; r += kAtOnce * kRows, from += kAtOnce * kRows * kPitch) {
+                float v[kAtOnce][kCols];
 #pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) {
-                const float *f = from + q * kRows * kPitch;
-                if constexpr (kCols % 4 == 0) {
+                for (int q = 0; q < kAtOnce; ++q) load_staged<T>(from + q * kRows * kPitch, v[q]);
 #pragma unroll
-                    for (int e = 0; e < kCols; e += 4)
-                        *reinterpret_cast<float4 *>(&v[q][e]) = *reinterpret_cast<const float4 *>(f + e);
-                } else if constexpr (kCols == 2) {
-                    *reinterpret_cast<float2 *>(&v[q][0]) = *reinterpret_cast<const float2 *>(f);
-                } else {
-                    v[q][0] = *f;
-                }
+                for (int q = 0; q < kAtOnce; ++q, to += step)
+                    if (r + q * kRows < rows) store_staged<T>(to, v[q], b);
             }
-#pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) {
-                if (r + q * kRows >= rows) break;
-                T out[kCols];
-#pragma unroll
-                for (int e = 0; e < kCols; ++e) out[e] = from_f32<T>(v[q][e] + b[e]);
-                if (n >= kCols) {
-                    if constexpr (VB == 16)
-                        *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(out);
-                    else if constexpr (VB == 8)
-                        *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(out);
-                    else if constexpr (VB == 4)
-                        *reinterpret_cast<uint32_t *>(to) = *reinterpret_cast<const uint32_t *>(out);
-                    else *to = out[0];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kCols; ++e)
-                        if (e < n) to[e] = out[e];
-                }
-                to += kRows * ldz;
-            }
-            from += kAtOnce * kRows * kPitch;
+        } else {
+#pragma unroll 1
+            for (int e = 0; e < n; ++e)
+                for (int r = r0; r < rows; r += kRows)
+                    to[(r - r0) * ldz + e] = from_f32<T>(from[(r - r0) * kPitch + e] +
+                                                         (bias ? __ldg(bias + c + e) : 0.0f));
         }
     }
 }
 
-// Tile t: its first row and first column.
-struct Tile {
-    int64_t m0;
-    int n0;
-    __device__ __forceinline__ Tile(int64_t t, int nt, int NT) {
-        if (t >> 32 == 0) {
-            const uint32_t m = uint32_t(t) / uint32_t(nt);
-            m0 = int64_t(m) * kUmmaM;
-            n0 = int(uint32_t(t) - m * uint32_t(nt)) * NT;
-        } else {
-            m0 = t / nt * kUmmaM;
-            n0 = int(t % nt) * NT;
+// 32 columns of sums, a row a lane, straight to Z's rows where these are aligned to 32 bytes: whole sectors,
+// each lane's own. `stage`: 32 floats, for the bias.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+                 "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void store_direct(uint32_t (&v)[32], T *row, bool in, int cols, const float *bias,
+                                             float *stage, int lane) {
+    if (bias) {
+        __syncwarp();
+        stage[lane] = lane < cols ? __ldg(bias + lane) : 0.0f;
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+            const float4 b = *reinterpret_cast<const float4 *>(stage + e);
+            v[e] = __float_as_uint(__uint_as_float(v[e]) + b.x);
+            v[e + 1] = __float_as_uint(__uint_as_float(v[e + 1]) + b.y);
+            v[e + 2] = __float_as_uint(__uint_as_float(v[e + 2]) + b.z);
+            v[e + 3] = __float_as_uint(__uint_as_float(v[e + 3]) + b.w);
         }
     }
+    if (!in) return;
+    constexpr int kCols = 32 / int(sizeof(T));          // of 32 bytes
+#pragma unroll
+    for (int c = 0; c < 32; c += kCols) {
+        if (c + kCols <= cols) {
+            uint32_t w[8];
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = v[c + e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __uint_as_float(v[c + 2 * e]), y = __uint_as_float(v[c + 2 * e + 1]);
+                    if constexpr (std::is_same<T, __half>::value) {
+                        const __half2 h = __floats2half2_rn(x, y);
+                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                    } else {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+                        w[e] = *reinterpret_cast<const uint32_t *>(&h);
+                    }
+                }
+            }
+            store32(row + c, w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                if (c + e < cols) row[c + e] = from_f32<T>(__uint_as_float(v[c + e]));
+        }
+    }
+}
+
+// A CTA's tiles, blockIdx.x, + gridDim.x, ...: m and n in tiles. (A division a tile costs each role 300
+// cycles and more.)
+struct Tiles {
+    uint32_t m, n;
+    __device__ __forceinline__ explicit Tiles(const Fp4GemmArgs &p)
+        : m(blockIdx.x / uint32_t(p.nt)), n(blockIdx.x % uint32_t(p.nt)) {}
+    __device__ __forceinline__ bool more(const Fp4GemmArgs &p) const { return m < p.mt; }
+    __device__ __forceinline__ void next(const Fp4GemmArgs &p) {
+        m += p.step_m;
+        n += p.step_n;
+        if (n >= uint32_t(p.nt)) n -= uint32_t(p.nt), ++m;
+    }
+    __device__ __forceinline__ int64_t m0() const { return int64_t(m) * kUmmaM; }
 };
 
 // A's or B's scale warp: 16 bytes of R rows a lane, unit after unit, into its part of the ring of slots.
 // One lane arrives for all once a unit has landed, kLag units behind what is asked for.
-template <int NT, int R>
+template <int NT, int kSlots, int R>
 __device__ __forceinline__ void ask_scales(const Fp4GemmArgs &p, bool a, uint32_t slots,
-                                           const uint64_t *freed, const uint64_t *loaded,
+                                           const uint64_t *read, const uint64_t *loaded,
                                            volatile uint32_t *stopv, int lane) {
     const uint8_t *const exps = a ? p.a_exps : p.b_exps;
     const int64_t rows = a ? p.N : p.F, ld = a ? p.lda_e : p.ldb_e;
     const bool wide = (reinterpret_cast<uintptr_t>(exps) & 15) == 0 && ld % 16 == 0;
     const int units = (p.groups + kUnit - 1) / kUnit;
-    constexpr int kLag = kSlots - 2;
+    constexpr int kSlot = (4 + NT / 32) * 512, kLag = kSlots > 2 ? kSlots - 2 : 1;
     int slot = 0, asked = 0;
     uint32_t parity = 1u;
     bool ok = true;
@@ -190,24 +268,23 @@ __device__ __forceinline__ void ask_scales(const Fp4GemmArgs &p, bool a, uint32_
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&loaded[n % kSlots]));
     };
-    for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-        const Tile tile(t, p.nt, NT);
+    for (Tiles t(p); ok && t.more(p); t.next(p)) {
         const uint8_t *row[R];
         bool in[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int64_t i = (a ? tile.m0 : tile.n0) + 32 * j + lane;
+            const int64_t i = (a ? t.m0() : int64_t(t.n) * NT) + 32 * j + lane;
             in[j] = i < rows;
             row[j] = exps + (in[j] ? i * ld : 0);
         }
         for (int u = 0; u < units; ++u) {
-            ok = __all_sync(kFullMask, wait_unless(smem_addr(&freed[slot]), parity, stopv));
+            ok = __all_sync(kFullMask, wait_unless(smem_addr(&read[slot]), parity, stopv));
             if (!ok) {
                 *stopv = 1u;
                 break;
             }
             const int left = p.groups - u * kUnit;
-            const uint32_t to = slots + uint32_t(slot * Fp4Shape<NT>::kSlot + lane * 16);
+            const uint32_t to = slots + uint32_t(slot * kSlot + lane * 16);
 #pragma unroll
             for (int j = 0; j < R; ++j) {
                 // (Zeros behind the last group and the last row, whatever memory holds there; the
@@ -239,28 +316,26 @@ __device__ __forceinline__ void ask_scales(const Fp4GemmArgs &p, bool a, uint32_
     for (int n = asked > kLag ? asked - kLag : 0; n < asked; ++n) landed(n);
 }
 
-// A placing warp: a unit's words to tensor memory, in the quarter of its lanes that the warp may write.
-// Word h of 128 rows is four columns; A's and B's of a word lie together.
-template <int NT>
+// A placing warp: the scale words of a unit's stages to tensor memory, in the quarter of its lanes that the
+// warp may write. Word h of 128 rows is four columns; A's and B's of a word lie together.
+template <int NT, bool kOnce>
 __device__ __forceinline__ void place_scales(const Fp4GemmArgs &p, uint32_t slots, uint32_t tmem,
-                                             const uint64_t *freed, const uint64_t *loaded,
-                                             const uint64_t *used, const uint64_t *filled,
-                                             volatile uint32_t *stopv, int lane) {
-    using S = Fp4Shape<NT>;
-    const int units = (p.groups + kUnit - 1) / kUnit;
-    int slot = 0, q = 0;
+                                             const uint64_t *read, const uint64_t *loaded,
+                                             const uint64_t *free, const uint64_t *ready,
+                                             volatile uint32_t *stopv, int stages, int lane) {
+    using S = Fp4Shape<NT, kOnce>;
+    constexpr int kCols = 4 * (1 + S::kChunks);         // of a word
+    int slot = 0, s = 0;
     uint32_t slot_parity = 0u, parity = 1u;
-    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x)
-        for (int u = 0; u < units; ++u) {
-            const bool go = wait_unless(smem_addr(&loaded[slot]), slot_parity, stopv) &&
-                            wait_unless(smem_addr(&used[q]), parity, stopv);
-            if (!__all_sync(kFullMask, go)) {
+    for (Tiles t(p); t.more(p); t.next(p))
+        for (int st = 0; st < stages; st += 2) {
+            if (!__all_sync(kFullMask, wait_unless(smem_addr(&loaded[slot]), slot_parity, stopv))) {
                 *stopv = 1u;
                 return;
             }
-            uint32_t v[S::kScaleCols];
+            uint32_t v[4 * kCols];
 #pragma unroll
-            for (int j = 0; j < 4 * (1 + S::kChunks); ++j) {
+            for (int j = 0; j < kCols; ++j) {
                 uint32_t w[4] = {0u, 0u, 0u, 0u};
                 if (j < 4 + S::kRowsB)
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
@@ -268,37 +343,45 @@ __device__ __forceinline__ void place_scales(const Fp4GemmArgs &p, uint32_t slot
                                  : "r"(slots + uint32_t(slot * S::kSlot + j * 512 + lane * 16))
                                  : "memory");
 #pragma unroll
-                for (int h = 0; h < 4; ++h) v[h * 4 * (1 + S::kChunks) + j] = w[h];
+                for (int h = 0; h < 4; ++h) v[h * kCols + j] = w[h];
             }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t to = tmem + uint32_t(q * S::kScaleCols);
-#pragma unroll
-            for (int c = 0; c < S::kScaleCols; c += 16) tmem_st16(to + uint32_t(c), v + c);
-            tmem_wait_st();
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_addr(&filled[q]));
-                mbar_arrive(smem_addr(&freed[slot]));
+            if (lane == 0) mbar_arrive(smem_addr(&read[slot]));
+            if (++slot == S::kSlots) slot = 0, slot_parity ^= 1u;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (st + half >= stages) break;
+                if (!__all_sync(kFullMask, wait_unless(smem_addr(&free[s]), parity, stopv))) {
+                    *stopv = 1u;
+                    return;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t to = tmem + uint32_t(s * S::kScaleCols);
+#pragma unroll
+                for (int c = 0; c < S::kScaleCols; c += 8)
+                    tmem_st8(to + uint32_t(c), v + half * S::kScaleCols + c);
+                tmem_wait_st();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&ready[s]));
+                if (++s == S::kStages) s = 0, parity ^= 1u;
             }
-            if (++slot == kSlots) slot = 0, slot_parity ^= 1u;
-            if (++q == kUnits) q = 0, parity ^= 1u;
         }
 }
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+template <typename T, int NT, bool kOnce>
+__global__ void __launch_bounds__(Fp4Shape<NT, kOnce>::kThreads, 1)
 fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
-    using S = Fp4Shape<NT>;
-    constexpr int kStages = S::kStages;
+    using S = Fp4Shape<NT, kOnce>;
+    constexpr int kStages = S::kStages, kSlots = S::kSlots;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], loaded[kSlots], freed[kSlots],
-        filled[kUnits], used[kUnits], summed[S::kAccs], taken[S::kAccs], done;
+    __shared__ __align__(8) uint64_t ready[kStages], free[kStages], loaded[kSlots], read[kSlots],
+        summed[S::kAccs], taken[S::kAccs], done;
     __shared__ uint32_t tmem_base, stop;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
-    const uint32_t staging = base + uint32_t(kStages * S::kStage);
+    const uint32_t held = base + uint32_t(kStages * S::kStage), staging = held + uint32_t(S::kHeld * S::kB);
     const uint32_t slots = staging + uint32_t(S::kStaging);
 
     if (warp == 1) {
@@ -309,20 +392,16 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_addr(&full[s]), 1);
-            mbar_init(smem_addr(&empty[s]), 1);
+            mbar_init(smem_addr(&ready[s]), 5);             // the boxes' bytes, the placing warps
+            mbar_init(smem_addr(&free[s]), 1);
         }
         for (int q = 0; q < kSlots; ++q) {
             mbar_init(smem_addr(&loaded[q]), 2);            // both scale warps
-            mbar_init(smem_addr(&freed[q]), 4);
-        }
-        for (int q = 0; q < kUnits; ++q) {
-            mbar_init(smem_addr(&filled[q]), 4);
-            mbar_init(smem_addr(&used[q]), 1);
+            mbar_init(smem_addr(&read[q]), 4);
         }
         for (int b = 0; b < S::kAccs; ++b) {
             mbar_init(smem_addr(&summed[b]), 1);
-            mbar_init(smem_addr(&taken[b]), kOutWarps);
+            mbar_init(smem_addr(&taken[b]), S::kOutWarps);
         }
         mbar_init(smem_addr(&done), 1);
         stop = 0u;
@@ -335,81 +414,79 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     volatile uint32_t *const stopv = &stop;
     const int stages = (p.groups + 7) / 8;              // of a tile
 
+
     if (warp == 0) {
         // Copies into the ring of stages.
         int s = 0, issued = 0;
         uint32_t parity = 1u;
         bool ok = true;
-        for (int64_t t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-            const Tile tile(t, p.nt, NT);
+        bool bring_b = true;
+        for (Tiles t(p); ok && t.more(p); t.next(p)) {
             for (int st = 0; st < stages; ++st) {
-                if (!__all_sync(kFullMask, wait_unless(smem_addr(&empty[s]), parity, stopv))) {
+                if (!__all_sync(kFullMask, wait_unless(smem_addr(&free[s]), parity, stopv))) {
                     *stopv = 1u;
                     ok = false;
                     break;
                 }
-                const uint32_t at = base + uint32_t(s * S::kStage), bar = smem_addr(&full[s]);
+                const uint32_t at = base + uint32_t(s * S::kStage), bar = smem_addr(&ready[s]);
                 if (elect_one()) {
-                    mbar_expect(bar, S::kA + S::kB);
-                    tma_load(at, &p.a_map, st * 128, int(tile.m0), bar);
-                    tma_load(at + S::kA, &p.b_map, st * 128, tile.n0, bar);
+                    mbar_expect(bar, bring_b ? S::kA + S::kB : S::kA);
+                    tma_load(at, &p.a_map, st * 128, int(t.m0()), bar);
+                    if (bring_b)
+                        tma_load(kOnce ? held + uint32_t(st * S::kB) : at + S::kA, &p.b_map, st * 128,
+                                 int(t.n) * NT, bar);
                 }
                 __syncwarp();
                 ++issued;
                 if (++s == kStages) s = 0, parity ^= 1u;
             }
+            if (kOnce) bring_b = false;
         }
         // What is still in flight lands before the shared memory is given up.
         for (int it = issued > kStages ? issued - kStages : 0; it < issued; ++it)
-            mbar_wait(smem_addr(&full[it % kStages]), uint32_t(it / kStages) & 1u);
+            mbar_wait(smem_addr(&ready[it % kStages]), uint32_t(it / kStages) & 1u);
     } else if (warp == 2) {
-        ask_scales<NT, 4>(p, true, slots, freed, loaded, stopv, lane);
+        ask_scales<NT, kSlots, 4>(p, true, slots, read, loaded, stopv, lane);
     } else if (warp == 3) {
-        ask_scales<NT, S::kRowsB>(p, false, slots + 4 * 512, freed, loaded, stopv, lane);
-    } else if (warp >= 12) {
-        place_scales<NT>(p, slots, tmem + (uint32_t(32 * (warp & 3)) << 16) + S::kAccs * NT, freed, loaded,
-                         used, filled, stopv, lane);
+        ask_scales<NT, kSlots, S::kRowsB>(p, false, slots + 4 * 512, read, loaded, stopv, lane);
+    } else if (warp >= 4 && warp < 8) {
+        place_scales<NT, kOnce>(p, slots, tmem + (uint32_t(32 * (warp & 3)) << 16) + S::kAccs * NT, read,
+                                loaded, free, ready, stopv, stages, lane);
     } else if (warp == 1) {
         // One thread issues. A stage of 256 columns takes the tensor core 256 or 512 cycles; this loop
         // has to stay below that, at four cycles and more an instruction.
         if (elect_one()) {
-            const uint32_t full0 = smem_addr(full), empty0 = smem_addr(empty);
-            const uint32_t filled0 = smem_addr(filled), used0 = smem_addr(used);
+            const uint32_t ready0 = smem_addr(ready), free0 = smem_addr(free);
             const uint32_t scales0 = tmem + uint32_t(S::kAccs * NT);
-            const uint64_t desc0 = sw128_desc(base);
-            uint32_t s = 0, b = 0, q = 0, parity = 0u, acc_parity = 1u, unit_parity = 0u;
+            const uint64_t desc0 = sw128_desc(base), desc_held = sw128_desc(held);
+            uint32_t s = 0, b = 0, parity = 0u, acc_parity = 1u;
             bool ok = true;
-            for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-                const int n = (min(NT, p.F - (p.nt == 1 ? 0 : Tile(t, p.nt, NT).n0)) + 31) / 32 * 32;
-                const uint32_t idesc = fp4_idesc(n, 0u), idesc2 = fp4_idesc(n, 2u);
+            // Columns of the last tile, rounded up to what an MMA takes.
+            const uint32_t whole = fp4_idesc(NT, 0u);
+            const uint32_t last = fp4_idesc((p.F - (p.nt - 1) * NT + 31) / 32 * 32, 0u);
+            for (Tiles t(p); t.more(p); t.next(p)) {
+                const uint32_t idesc = t.n + 1 == uint32_t(p.nt) ? last : whole;
+                const uint32_t idesc2 = idesc | fp4_idesc(0, 2u);
                 const uint32_t acc = tmem + b * NT;
                 ok = wait_unless(smem_addr(&taken[b]), acc_parity, stopv);
-                if (!ok) break;
-                uint32_t word = 0u;             // the stage's scales, in tensor memory
                 bool more = false;              // (the first MMA starts the sum)
-                for (int left = p.groups, odd = 0; left > 0; left -= 8, odd ^= 1) {
-                    if (odd) {
-                        word += 8 * (1 + S::kChunks);
-                    } else {
-                        ok = wait_unless(filled0 + 8 * q, unit_parity, stopv);
-                        word = scales0 + q * S::kScaleCols;
-                    }
-                    ok = ok && wait_unless(full0 + 8 * s, parity, stopv);
+                uint64_t db = desc_held;
+                for (int left = p.groups; ok && left > 0; left -= 8) {
+                    ok = wait_unless(ready0 + 8 * s, parity, stopv);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = desc0 + s * (S::kStage / 16), db = da + S::kA / 16;
-                    constexpr uint32_t kNext = 4 * (1 + S::kChunks), kB = 4;
-                    mma_fp4(acc, da, db, idesc, word, word + kB, more);
+                    const uint64_t da = desc0 + s * (S::kStage / 16);
+                    if (!kOnce) db = da + S::kA / 16;
+                    const uint32_t sa = scales0 + s * S::kScaleCols, sb = sa + 4;
+                    constexpr uint32_t kNext = 4 * (1 + S::kChunks);
+                    mma_fp4(acc, da, db, idesc, sa, sb, more);
                     more = true;
-                    if (left > 2) mma_fp4(acc, da + 2, db + 2, idesc2, word, word + kB, true);
-                    if (left > 4) mma_fp4(acc, da + 4, db + 4, idesc, word + kNext, word + kNext + kB, true);
-                    if (left > 6) mma_fp4(acc, da + 6, db + 6, idesc2, word + kNext, word + kNext + kB, true);
-                    mma_commit(empty0 + 8 * s);
+                    if (left > 2) mma_fp4(acc, da + 2, db + 2, idesc2, sa, sb, true);
+                    if (left > 4) mma_fp4(acc, da + 4, db + 4, idesc, sa + kNext, sb + kNext, true);
+                    if (left > 6) mma_fp4(acc, da + 6, db + 6, idesc2, sa + kNext, sb + kNext, true);
+                    mma_commit(free0 + 8 * s);
                     if (++s == kStages) s = 0, parity ^= 1u;
-                    if (odd || left <= 8) {
-                        mma_commit(used0 + 8 * q);
-                        if (++q == kUnits) q = 0, unit_parity ^= 1u;
-                    }
+                    if (kOnce) db += S::kB / 16;
                 }
                 if (!ok) break;
                 mma_commit(smem_addr(&summed[b]));
@@ -420,19 +497,26 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
         }
         __syncwarp();
     } else {
-        // Sums out, a warp the 32 lanes of tensor memory that it may read, every second kBatch columns.
+        // Sums out, a warp the 32 lanes of tensor memory that it may read, every second batch of columns.
         // Tiles whose waits ran out are NaN.
         constexpr int kBatch = S::kBatch, kPitch = S::kPitch;
-        const int quad = warp & 3, half = (warp - 4) >> 2;
+        constexpr int kLoad = kBatch / (S::kPair ? 2 : 1), kStore = S::kPair ? 16 : 32;
+        constexpr int kWidth = S::kPair ? kLoad : 32;       // columns of a direct store
+        const int quad = warp & 3, out = (warp - 8) >> 2;
+        const int half = S::kPair ? out >> 1 : out, mate = S::kPair ? out & 1 : 0;
         float *const stage = reinterpret_cast<float *>(smem_raw + (staging - raw)) +
-                             (warp - 4) * 32 * kPitch;
+                             (quad + 4 * half) * 32 * kPitch;
+        auto meet = [&] {                                   // with the other warp of the pair
+            if constexpr (S::kPair)
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + quad + 4 * half) : "memory");
+            else __syncwarp();
+        };
         int b = 0;
         uint32_t parity = 0u;
         bool ok = true;
-        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-            const Tile tile(t, p.nt, NT);
-            const int64_t row0 = tile.m0 + 32 * quad;
-            const int cols = min(NT, p.F - tile.n0);
+        for (Tiles t(p); t.more(p); t.next(p)) {
+            const int64_t row0 = t.m0() + 32 * quad;
+            const int n0 = int(t.n) * NT, cols = min(NT, p.F - n0);
             const int rows = int(min(int64_t(32), max(int64_t(0), p.N - row0)));
             if (ok) {
                 ok = __all_sync(kFullMask, wait_unless(smem_addr(&summed[b]), parity, stopv));
@@ -440,38 +524,55 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (uint32_t(32 * quad) << 16) + uint32_t(b * NT);
-            T *z = static_cast<T *>(p.Z) + row0 * p.ldz + tile.n0;
-            const float *bias = p.bias ? p.bias + tile.n0 : nullptr;
-#pragma unroll 1
-            for (int c = kBatch * half; c < cols; c += 2 * kBatch) {
-#pragma unroll
-                for (int h = 0; h < kBatch; h += 32) {
-                    if (c + h >= cols) break;
-                    uint32_t v[32];
-                    tmem_ld32(acc + uint32_t(c + h), v);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4 *>(stage + lane * kPitch + h + e) =
-                            ok ? make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3])
-                               : make_uint4(0x7FC00000u, 0x7FC00000u, 0x7FC00000u, 0x7FC00000u);
-                }
-                if (c + 2 * kBatch >= cols) {       // the warp's last of this tile
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
-                }
-                __syncwarp();
-                const float *bc = bias ? bias + c : nullptr;
-                if (p.vec == 16) store_sums<T, kBatch, 16>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
-                else if (p.vec == 8) store_sums<T, kBatch, 8>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
-                else if (p.vec == 4) store_sums<T, kBatch, 4>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
-                else if constexpr (sizeof(T) == 2)
-                    store_sums<T, kBatch, 2>(stage, z + c, p.ldz, rows, cols - c, bc, lane);
-                __syncwarp();
-            }
-            if (kBatch * half >= cols) {            // no columns of this tile
+            T *z = static_cast<T *>(p.Z) + row0 * p.ldz + n0;
+            const float *bias = p.bias ? p.bias + n0 : nullptr;
+            auto taken_out = [&] {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
+            };
+            if (p.direct) {
+#pragma unroll 1
+                for (int c = kWidth * (S::kPair ? out : half); c < cols; c += S::kOutWarps / 4 * kWidth) {
+                    uint32_t v[32];
+                    tmem_ld32(acc + uint32_t(c), v);
+                    if (!ok)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0x7FC00000u;
+                    store_direct<T>(v, z + lane * p.ldz + c, lane < rows, cols - c, bias ? bias + c : nullptr,
+                                    stage + 36 * mate, lane);
+                }
+                taken_out();
+            } else {
+#pragma unroll 1
+                for (int c = kBatch * half; c < cols; c += 2 * kBatch) {
+                    const int h = kLoad * mate;
+                    if (c + h < cols) {
+                        uint32_t v[kLoad];
+                        if constexpr (kLoad == 32) tmem_ld32(acc + uint32_t(c + h), v);
+                        else tmem_ld16(acc + uint32_t(c + h), v);
+                        uint4 *const to = reinterpret_cast<uint4 *>(stage + lane * kPitch + h);
+#pragma unroll
+                        for (int e = 0; e < kLoad / 4; ++e)
+                            to[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        if (!ok)
+                            for (int e = 0; e < kLoad; ++e)
+                                stage[lane * kPitch + h + e] = __uint_as_float(0x7FC00000u);
+                    }
+                    if (c + 2 * kBatch >= cols) taken_out();        // the warp's last of this tile
+                    meet();
+                    const float *bc = bias ? bias + c : nullptr;
+                    const float *from = stage + kStore * mate * kPitch;
+                    T *zc = z + kStore * mate * p.ldz + c;
+                    const int nr = min(kStore, rows - kStore * mate), nc = cols - c;
+                    if (p.vec >= 16) store_sums<T, kBatch, kStore, 16>(from, zc, p.ldz, nr, nc, bc, lane);
+                    else if (p.vec == 8) store_sums<T, kBatch, kStore, 8>(from, zc, p.ldz, nr, nc, bc, lane);
+                    else if (p.vec == 4) store_sums<T, kBatch, kStore, 4>(from, zc, p.ldz, nr, nc, bc, lane);
+                    else if constexpr (sizeof(T) == 2)
+                        store_sums<T, kBatch, kStore, 2>(from, zc, p.ldz, nr, nc, bc, lane);
+                    meet();
+                }
+                if (kBatch * half >= cols) taken_out();             // no columns of this tile
             }
             if (++b == S::kAccs) b = 0, parity ^= 1u;
         }
@@ -487,19 +588,23 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
                      "r"(kTmemCols));
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool kOnce>
 void launch_nt(const Fp4GemmArgs &p, unsigned grid, cudaStream_t s) {
-    using S = Fp4Shape<NT>;
-    cudaFuncSetAttribute(fp4_gemm_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    fp4_gemm_kernel<T, NT><<<grid, kGemmThreads, S::kSmem, s>>>(p);
+    using S = Fp4Shape<NT, kOnce>;
+    cudaFuncSetAttribute(fp4_gemm_kernel<T, NT, kOnce>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         S::kSmem);
+    fp4_gemm_kernel<T, NT, kOnce><<<grid, S::kThreads, S::kSmem, s>>>(p);
 }
 
 template <typename T>
 void launch_gemm(const Fp4GemmArgs &p, int NT, unsigned grid, cudaStream_t s) {
-    if (NT == 256) launch_nt<T, 256>(p, grid, s);
-    else if (NT == 128) launch_nt<T, 128>(p, grid, s);
-    else if (NT == 64) launch_nt<T, 64>(p, grid, s);
-    else launch_nt<T, 32>(p, grid, s);
+    const bool once = p.nt == 1 && p.groups <= 8 * Fp4Shape<128, true>::kHeld && p.mt > grid;
+    if (NT == 256) launch_nt<T, 256, false>(p, grid, s);
+    else if (NT == 128 && once) launch_nt<T, 128, true>(p, grid, s);
+    else if (NT == 128) launch_nt<T, 128, false>(p, grid, s);
+    else if (NT == 64 && once) launch_nt<T, 64, true>(p, grid, s);
+    else if (NT == 64) launch_nt<T, 64, false>(p, grid, s);
+    else launch_nt<T, 32, false>(p, grid, s);
 }
 
 }  // namespace
@@ -563,13 +668,17 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     p.N = N;
     p.F = F;
     p.nt = (F + NT - 1) / NT;
-    p.tiles = mt * p.nt;
+    p.mt = uint32_t(mt);
+    const int64_t tiles = mt * p.nt;
     p.bias = bias;
     p.Z = Z;
     p.ldz = ldz;
-    const uint64_t where = uint64_t(uintptr_t(Z)) | uint64_t(N > 1 ? ldz : 0) * es | 16;
+    const uint64_t where = uint64_t(uintptr_t(Z)) | uint64_t(N > 1 ? ldz : 0) * es | 32;
     p.vec = int(where & (~where + 1));
-    const unsigned grid = unsigned(p.tiles < dev.sm_count ? p.tiles : dev.sm_count);
+    p.direct = p.vec == 32 && (es == 2 || NT == 256);
+    const unsigned grid = unsigned(tiles < dev.sm_count ? tiles : dev.sm_count);
+    p.step_m = grid / uint32_t(p.nt);
+    p.step_n = grid % uint32_t(p.nt);
     const cudaStream_t s = as_stream(stream);
     if (dtype == BIGCN_F32) launch_gemm<float>(p, NT, grid, s);
     else if (dtype == BIGCN_BF16) launch_gemm<__nv_bfloat16>(p, NT, grid, s);
