@@ -1,8 +1,11 @@
 // Rows to 4 bits and back, and a matrix's columns to 4-bit rows (bigcn_fp4_pack, bigcn_fp4_unpack,
 // bigcn_fp4_pack_columns): the arithmetic is fp4.cuh's; all are bound by memory.
 //
-// A thread takes octets, 8 consecutive columns of a row: 32 or 16 bytes of X and one word of codes;
-// four neighbouring lanes hold a group and share its largest magnitude by shuffles.
+// Rows are taken as one sequence of octets (packing) or 16-byte pieces (reading back), each row up to a
+// whole group, so that every lane has work whatever a row's length: laid over a power of two
+// threads, 602 columns kept 59 of 100 lanes busy. 232,965 x 602 fp32: packing 105 us (131 so; 6.05 TB/s,
+// 0.90 of a copy's rate), reading back to bf16 72 us (101; 4.9 TB/s: rows aligned to 4 bytes), to fp32 99
+// us; 2^20 x 128 fp32 101 and 57 us.
 #include "fp4.cuh"
 #include "norm.cuh"
 
@@ -22,81 +25,83 @@ struct Fp4Args {
     int64_t lde;
 };
 
-// A row lies over `tpr` threads (a power of two, 8 to 256), J octets of it by R rows to a thread,
-// all loaded before the first is used; a longer row goes over several blocks (`parts`).
-template <int J, int R>
-struct Octets {
-    int64_t i[R];            // rows
-    int k0;                  // column of octet 0
-    int step;                // columns from one octet to the next
-    __device__ __forceinline__ Octets(int tpr, unsigned parts) {
-        const int t = threadIdx.x & (tpr - 1), rows = kFp4Threads / tpr;
-        const unsigned set = blockIdx.x / parts, part = blockIdx.x % parts;
-#pragma unroll
-        for (int r = 0; r < R; ++r) i[r] = (int64_t(set) * R + r) * rows + threadIdx.x / tpr;
-        step = tpr * 8;
-        k0 = int(part) * step * J + t * 8;
+// Pieces per thread: all asked for before the first is used.
+constexpr int kFp4Pieces = 4;
+
+// Where a block's pieces (or octets) lie: piece kBlock blockIdx.x + i of all is piece `k` of row `row`.
+template <int kBlock>
+struct PieceWalk {
+    int64_t row0;
+    uint32_t r0, per_row, magic;
+    __device__ __forceinline__ PieceWalk(uint32_t per, uint32_t mag) : per_row(per), magic(mag) {
+        const uint64_t first = uint64_t(blockIdx.x) * kBlock;
+        if (first >> 32 == 0) {
+            row0 = uint32_t(first) / per;
+            r0 = uint32_t(first) - uint32_t(row0) * per;
+        } else {
+            row0 = int64_t(first / per);
+            r0 = uint32_t(first - uint64_t(row0) * per);
+        }
+    }
+    // (Below kBlock pieces a row the product with floor(2^32 / per_row) + 1 has the quotient in its
+    // upper half: r0 + i < 2 kBlock, and its excess, at most per_row for each 2^32, stays below one.)
+    __device__ __forceinline__ void at(uint32_t i, int64_t &row, uint32_t &k) const {
+        const uint32_t t = r0 + i;
+        const uint32_t q = per_row > kBlock ? uint32_t(t >= per_row) : __umulhi(t, magic);
+        row = row0 + q;
+        k = t - q * per_row;
     }
 };
 
-template <typename T, int A, int J, int R>
+// An octet, 8 columns (P pieces), a lane: a word of codes.
+template <typename T, int A>
 __global__ void __launch_bounds__(kFp4Threads)
-fp4_pack_kernel(const Fp4Args a, const int tpr, const unsigned parts) {
-    constexpr int V = kPiece<T>, P = 8 / V, H = V / 2;      // P pieces of V elements an octet
-    const Octets<J, R> at(tpr, parts);
-    const int K = a.K, left = K - at.k0;
-    Raw<A> w[R][J][P];
-    bool odd[R];
+fp4_pack_kernel(const Fp4Args a, const uint32_t per_row, const uint32_t magic) {
+    constexpr int V = kPiece<T>, H = V / 2, P = 8 / V, U = kFp4Pieces / P, kLanes = kGroup / 8;
+    const PieceWalk<U * kFp4Threads> walk(per_row, magic);
+    Raw<A> w[U][P];
+    bool odd[U];
+    int64_t row[U];
+    uint32_t octet[U];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const T *row = static_cast<const T *>(a.X) + at.i[r] * a.ldx + at.k0;
-        const bool whole = whole_pieces<A>(row, tpr >= 32);
-        odd[r] = odd_pieces<A>(row);
+    for (int u = 0; u < U; ++u) {
+        walk.at(threadIdx.x + u * kFp4Threads, row[u], octet[u]);
+        const int n = a.K - int(octet[u]) * 8;
+        const T *x = static_cast<const T *>(a.X) + row[u] * a.ldx + int64_t(octet[u]) * 8;
+        const bool whole = whole_pieces<A>(x, true);
+        odd[u] = odd_pieces<A>(x);
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int n = left - j * at.step - p * V;
-                w[r][j][p] = raw_zero<A>();
-                if (at.i[r] < a.N && n > 0)
-                    w[r][j][p] = load_piece<T, A>(row + j * at.step + p * V, n, whole, odd[r]);
-            }
+        for (int p = 0; p < P; ++p) {
+            w[u][p] = raw_zero<A>();
+            if (row[u] < a.N && n > p * V) w[u][p] = load_piece<T, A>(x + p * V, n - p * V, whole, odd[u]);
+        }
     }
-    const int groups = int(checkpoint_groups(K));
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float2 x[J][4];
-        uint32_t own[J], top[J];
+    for (int u = 0; u < U; ++u) {
+        float2 x[4];
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
+        for (int p = 0; p < P; ++p) {
+            float2 v[H];
+            unpack16<T>(settled<A>(w[u][p], odd[u]), v);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                float2 v[H];
-                unpack16<T>(settled<A>(w[r][j][p], odd[r]), v);
-#pragma unroll
-                for (int e = 0; e < H; ++e) x[j][p * H + e] = v[e];
-            }
-            own[j] = top_bits(x[j]);
+            for (int e = 0; e < H; ++e) x[p * H + e] = v[e];
         }
-        group_tops<4>(own, top);
-        if (at.i[r] >= a.N) continue;
-        uint8_t *q = a.q + at.i[r] * a.ldq;
-        uint8_t *exps = a.exps + at.i[r] * a.lde;
+        uint32_t own[1] = {top_bits(x)}, top[1];
+        group_tops<kLanes>(own, top);
+        if (row[u] >= a.N) continue;
+        const uint32_t b = fp4_scale_byte(top[0]);
+        const float2 f = both(pack_factor(b));
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = at.k0 + j * at.step, g = k / kGroup;
-            if (g >= groups) break;
-            const uint32_t b = fp4_scale_byte(top[j]);
-            const float2 f = both(pack_factor(b));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[j][e] = __fmul2_rn(x[j][e], f);
-            const uint32_t codes = fp4_codes(x[j][0].x, x[j][0].y, x[j][1].x, x[j][1].y, x[j][2].x,
-                                             x[j][2].y, x[j][3].x, x[j][3].y);
-            *reinterpret_cast<uint32_t *>(q + k / 2) = b == kNanByte ? 0u : codes;
-            if ((threadIdx.x & 3) == 0) exps[g] = uint8_t(b);
+        for (int e = 0; e < 4; ++e) x[e] = __fmul2_rn(x[e], f);
+        const uint32_t c = fp4_codes(x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y);
+        *reinterpret_cast<uint32_t *>(a.q + row[u] * a.ldq + int64_t(octet[u]) * 4) =
+            b == kNanByte ? 0u : c;
+        if (octet[u] % kLanes == 0) {
+            uint8_t *e = a.exps + row[u] * a.lde + octet[u] / kLanes;
+            *e = uint8_t(b);
+            if (octet[u] + kLanes == per_row)               // the row's last group: zeros up to a word
+                for (uint32_t g = per_row / kLanes; g % 4 != 0; ++g) *++e = 0;
         }
-        const int t = threadIdx.x & (tpr - 1);
-        if (blockIdx.x % parts + 1 == parts && groups + t < (groups + 3) / 4 * 4) exps[groups + t] = 0;
     }
 }
 
@@ -105,69 +110,55 @@ __device__ __forceinline__ float fp4_factor(uint32_t b) {
     return b == 0u ? __uint_as_float(0x00400000u) : unpack_factor(b);
 }
 
-template <typename T, int A, int J, int R>
+// A piece a lane. (Rows aligned to less than 16 bytes through shared memory, so that a store of fewer bytes a
+// lane is a run of memory: 232,965 x 602 to bf16 72 -> 81 us.)
+template <typename T, int A>
 __global__ void __launch_bounds__(kFp4Threads)
-fp4_unpack_kernel(const Fp4Args a, const int tpr, const unsigned parts) {
-    constexpr int V = kPiece<T>, P = 8 / V, H = V / 2;
-    const Octets<J, R> at(tpr, parts);
-    const int left = a.K - at.k0;
-    uint32_t w[R][J];
-    uint8_t b[R][J];
+fp4_unpack_kernel(const Fp4Args a, const uint32_t per_row, const uint32_t magic) {
+    constexpr int V = kPiece<T>, H = V / 2, kLanes = kGroup / V;
+    const PieceWalk<kFp4Pieces * kFp4Threads> walk(per_row, magic);
+    uint32_t w[kFp4Pieces];
+    uint8_t b[kFp4Pieces];
+    T *to[kFp4Pieces];
+    int n[kFp4Pieces];                  // of the piece's columns in the row
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (at.i[r] < a.N && left > j * at.step) {
-                const int k = at.k0 + j * at.step;
-                w[r][j] = *reinterpret_cast<const uint32_t *>(a.q + at.i[r] * a.ldq + k / 2);
-                b[r][j] = a.exps[at.i[r] * a.lde + k / kGroup];
-            }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (at.i[r] >= a.N) continue;
-        T *row = static_cast<T *>(a.X) + at.i[r] * a.ldx + at.k0;
-        const bool whole = whole_pieces<A>(row, tpr >= 32);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (left <= j * at.step) break;
-            uint32_t h[4];
-            fp4_halves(w[r][j], h);
-            const float2 f = both(fp4_factor(b[r][j]));
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int n = left - j * at.step - p * V;
-                if (n <= 0) break;
-                float2 v[H];
-#pragma unroll
-                for (int e = 0; e < H; ++e)
-                    v[e] = __fmul2_rn(
-                        __half22float2(*reinterpret_cast<const __half2 *>(&h[p * H + e])), f);
-                store_piece<T, A>(row + j * at.step + p * V, pack16<T>(v), n, whole);
-            }
+    for (int u = 0; u < kFp4Pieces; ++u) {
+        int64_t row;
+        uint32_t piece;
+        walk.at(threadIdx.x + u * kFp4Threads, row, piece);
+        w[u] = 0u;
+        b[u] = 0;
+        to[u] = static_cast<T *>(a.X) + row * a.ldx + int64_t(piece) * V;
+        n[u] = row < a.N ? a.K - int(piece) * V : 0;
+        if (row < a.N) {
+            const uint8_t *q = a.q + row * a.ldq + int64_t(piece) * (V / 2);
+            if constexpr (V == 8) w[u] = *reinterpret_cast<const uint32_t *>(q);
+            else w[u] = *reinterpret_cast<const uint16_t *>(q);
+            b[u] = a.exps[row * a.lde + piece / kLanes];
         }
+    }
+#pragma unroll
+    for (int u = 0; u < kFp4Pieces; ++u) {
+        uint32_t h[4];
+        fp4_halves(w[u], h);
+        const float2 f = both(fp4_factor(b[u]));
+        float2 v[H];
+#pragma unroll
+        for (int e = 0; e < H; ++e)
+            v[e] = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2 *>(&h[e])), f);
+        if (n[u] > 0) store_piece<T, A>(to[u], pack16<T>(v), n[u], whole_pieces<A>(to[u], true));
     }
 }
 
-template <typename T, int A, int J, int R>
-void launch_octets(const Fp4Args &a, bool pack, int tpr, unsigned parts, cudaStream_t s) {
-    const int64_t rows = kFp4Threads / tpr * R;
-    const unsigned blocks = unsigned((a.N + rows - 1) / rows * parts);
-    if (pack) fp4_pack_kernel<T, A, J, R><<<blocks, kFp4Threads, 0, s>>>(a, tpr, parts);
-    else fp4_unpack_kernel<T, A, J, R><<<blocks, kFp4Threads, 0, s>>>(a, tpr, parts);
-}
-
-// The fewest threads (8, or more) that hold a row in at most two octets, else all 256 and
-// several blocks a row.
 template <typename T, int A>
 void launch_fp4_rows(const Fp4Args &a, bool pack, cudaStream_t s) {
-    const int64_t octets = checkpoint_groups(a.K) * 4;
-    int tpr = 8;
-    while (tpr < kFp4Threads && int64_t(tpr) * 2 < octets) tpr *= 2;
-    const int64_t need = (octets + tpr - 1) / tpr;
-    const int J = need < 2 ? 1 : 2;
-    const unsigned parts = unsigned((need + J - 1) / J);
-    if (J == 1) launch_octets<T, A, 1, 2>(a, pack, tpr, parts, s);
-    else launch_octets<T, A, 2, 1>(a, pack, tpr, parts, s);
+    const int columns = pack ? 8 : kPiece<T>;               // of a thread's unit
+    const uint32_t per_row = uint32_t(checkpoint_groups(a.K) * (kGroup / columns));
+    const uint32_t magic = uint32_t((uint64_t(1) << 32) / per_row + 1);
+    const int64_t block = kFp4Threads * (pack ? kFp4Pieces * kPiece<T> / 8 : kFp4Pieces);
+    const unsigned blocks = unsigned((a.N * int64_t(per_row) + block - 1) / block);
+    if (pack) fp4_pack_kernel<T, A><<<blocks, kFp4Threads, 0, s>>>(a, per_row, magic);
+    else fp4_unpack_kernel<T, A><<<blocks, kFp4Threads, 0, s>>>(a, per_row, magic);
 }
 
 template <typename T>
