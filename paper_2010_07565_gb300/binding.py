@@ -609,12 +609,63 @@ def bigcn_checkpoint_weight_grad(q, exps, dZ, workspace, dW, gamma=None, beta=No
         _ptr(workspace), _bytes(workspace), _stream(stream)))
 
 
-def _on_device(*tensors):
-    """Refuses tensors that are not on the current CUDA device, whose stream the call takes."""
-    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("expected tensors on the current CUDA device")
+# The calls below check a tensor's device along with its type and shape, each in as few torch calls
+# as do it: on one row a call's time is these checks' (9.5 us, of which the argument passing is 3).
+def _current(stream):
+    """(the current CUDA device, or None before CUDA is up; the stream's handle)."""
+    if not torch.cuda.is_initialized():
+        return None, stream
+    device = torch._C._cuda_getDevice()
+    if stream is None:
+        return device, torch._C._cuda_getCurrentRawStream(device)
+    return device, _stream(stream)
+
+
+def _elsewhere(what):
+    raise ValueError(f"{what} must be on the current CUDA device, whose stream the call takes")
+
+
+def _rows(t, shape, dtype, device, what):
+    """(pointer, row stride) of a matrix of ``shape`` and ``dtype`` (None: NULL)."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{what} must be {tuple(shape)} {dtype}")
+    ld, unit = t.stride()
+    if unit != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    if t.get_device() != device:
+        _elsewhere(what)
+    return t.data_ptr(), ld
+
+
+def _floats(t, n, device, what):
+    """Pointer of a contiguous fp32 vector of n entries (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 vector of {n} entries")
+    if t.get_device() != device:
+        _elsewhere(what)
+    return t.data_ptr()
+
+
+def _room(workspace, device):
+    """(pointer, bytes) of a workspace (None: NULL)."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        _elsewhere("workspace")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _checkpoint(q, exps, N, K, device):
+    if q is None or exps is None:
+        return _ptr(q), 0, _ptr(exps), 0
+    kept = _kept(q, exps, N, K)
+    if q.get_device() != device or exps.get_device() != device:
+        _elsewhere("a checkpoint")
+    return kept
 
 
 def bigcn_rms_norm_forward(X, gamma, eps, R=None, S=None, Y=None, rstd=None, q=None, exps=None,
@@ -622,15 +673,18 @@ def bigcn_rms_norm_forward(X, gamma, eps, R=None, S=None, Y=None, rstd=None, q=N
     """S = X + R (X without R), Y = gamma shat with shat the rows of S over their root mean
     square; rstd (N fp32) and the checkpoint of shat where given. S may be R or X. gamma: None
     for 1."""
-    N, K = X.shape
-    r, ldr = _matrix(R, N, K, "R", X)
-    s, lds = _matrix(S, N, K, "S", X)
-    y, ldy = _matrix(Y, N, K, "Y", X)
-    g, out, kept = _vector(gamma, K, "gamma"), _vector(rstd, N, "rstd"), _kept(q, exps, N, K)
-    dtype, ldx = _dtype(X), _ld(X)
-    _on_device(X, gamma, R, S, Y, rstd, q, exps)
+    device, stream = _current(stream)
+    shape, t = X.shape, X.dtype
+    N, K = shape
+    dtype = _dtype(X)
+    x, ldx = _rows(X, shape, t, device, "X")
+    r, ldr = _rows(R, shape, t, device, "R")
+    s, lds = _rows(S, shape, t, device, "S")
+    y, ldy = _rows(Y, shape, t, device, "Y")
+    g, out = _floats(gamma, K, device, "gamma"), _floats(rstd, N, device, "rstd")
+    q, ldq, exps, lde = _checkpoint(q, exps, N, K, device)
     _check("bigcn_rms_norm_forward", lib().bigcn_rms_norm_forward(
-        dtype, _ptr(X), N, K, ldx, r, ldr, g, eps, s, lds, y, ldy, out, *kept, _stream(stream)))
+        dtype, x, N, K, ldx, r, ldr, g, eps, s, lds, y, ldy, out, q, ldq, exps, lde, stream))
 
 
 def bigcn_rms_norm_backward_workspace_bytes(N: int, K: int) -> int:
@@ -642,63 +696,76 @@ def bigcn_rms_norm_backward(dY, gamma, rstd, workspace, S=None, q=None, exps=Non
     """dX (of the sum's addends alike) and dgamma (those given) from dY, with shat from the sum S or
     from the checkpoint q, exps; dS, which dX may be, is added to dX. workspace: None where dgamma is
     not given."""
-    N, K = dY.shape
-    s, lds = _matrix(S, N, K, "S", dY)
-    ds, ldds = _matrix(dS, N, K, "dS", dY)
-    dx, lddx = _matrix(dX, N, K, "dX", dY)
-    g, out, kept = _vector(gamma, K, "gamma"), _vector(dgamma, K, "dgamma"), _kept(q, exps, N, K)
-    dtype, lddy, r = _dtype(dY), _ld(dY), _vector(rstd, N, "rstd")
-    _on_device(dY, gamma, rstd, workspace, S, q, exps, dS, dX, dgamma)
+    device, stream = _current(stream)
+    shape, t = dY.shape, dY.dtype
+    N, K = shape
+    dtype = _dtype(dY)
+    dy, lddy = _rows(dY, shape, t, device, "dY")
+    s, lds = _rows(S, shape, t, device, "S")
+    ds, ldds = _rows(dS, shape, t, device, "dS")
+    dx, lddx = _rows(dX, shape, t, device, "dX")
+    g, r = _floats(gamma, K, device, "gamma"), _floats(rstd, N, device, "rstd")
+    out = _floats(dgamma, K, device, "dgamma")
+    q, ldq, exps, lde = _checkpoint(q, exps, N, K, device)
+    ws, ws_bytes = _room(workspace, device)
     _check("bigcn_rms_norm_backward", lib().bigcn_rms_norm_backward(
-        dtype, _ptr(dY), N, K, lddy, g, s, lds, *kept, r, ds, ldds, dx, lddx, out,
-        _ptr(workspace), _bytes(workspace), _stream(stream)))
+        dtype, dy, N, K, lddy, g, s, lds, q, ldq, exps, lde, r, ds, ldds, dx, lddx, out, ws,
+        ws_bytes, stream))
 
 
-def _fp4(q, exps, N, K, what):
+def _fp4(q, exps, N, K, device, what):
     """(q, ldq, exps, lde) of N 4-bit rows of K columns."""
-    if q.dtype != torch.uint8 or exps.dtype != torch.uint8 or q.shape != (N, (K + 1) // 2) or \
-            exps.shape != (N, (K + 31) // 32):
+    if q.dtype is not torch.uint8 or exps.dtype is not torch.uint8 or \
+            q.shape != (N, (K + 1) // 2) or exps.shape != (N, (K + 31) // 32):
         raise ValueError(f"{what}: 4-bit rows are q (N x ceil(K / 2)) and exps (N x ceil(K / 32)), "
                          "both uint8")
-    return _ptr(q), _ld(q), _ptr(exps), _ld(exps)
+    ldq, unit = q.stride()
+    lde, unit_e = exps.stride()
+    if unit != 1 or unit_e != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    if q.get_device() != device or exps.get_device() != device:
+        _elsewhere(what)
+    return q.data_ptr(), ldq, exps.data_ptr(), lde
 
 
 def bigcn_fp4_pack(X, q, exps, stream=None):
     """X (N x K, fp32, bf16 or fp16) to 4 bits: q (N x ceil(K/2) uint8) and exps (N x ceil(K/32)
     uint8), views of rows of the strides that the header asks for (:func:`fp4_buffers`)."""
+    device, stream = _current(stream)
     N, K = X.shape
-    dtype, ldx, rows = _dtype(X), _ld(X), _fp4(q, exps, N, K, "X")
-    _on_device(X, q, exps)
+    dtype, (x, ldx) = _dtype(X), _rows(X, X.shape, X.dtype, device, "X")
     _check("bigcn_fp4_pack", lib().bigcn_fp4_pack(
-        dtype, _ptr(X), N, K, ldx, *rows, _stream(stream)))
+        dtype, x, N, K, ldx, *_fp4(q, exps, N, K, device, "X"), stream))
 
 
 def bigcn_fp4_pack_columns(W, q, exps, stream=None):
     """The columns of W (K x F) to F 4-bit rows of K."""
+    device, stream = _current(stream)
     K, F = W.shape
-    dtype, ldw, rows = _dtype(W), _ld(W), _fp4(q, exps, F, K, "W")
-    _on_device(W, q, exps)
+    dtype, (w, ldw) = _dtype(W), _rows(W, W.shape, W.dtype, device, "W")
     _check("bigcn_fp4_pack_columns", lib().bigcn_fp4_pack_columns(
-        dtype, _ptr(W), K, F, ldw, *rows, _stream(stream)))
+        dtype, w, K, F, ldw, *_fp4(q, exps, F, K, device, "W"), stream))
 
 
 def bigcn_fp4_unpack(q, exps, X, stream=None):
     """X (N x K) from its 4 bits."""
+    device, stream = _current(stream)
     N, K = X.shape
-    dtype, ldx, rows = _dtype(X), _ld(X), _fp4(q, exps, N, K, "X")
-    _on_device(X, q, exps)
+    dtype, (x, ldx) = _dtype(X), _rows(X, X.shape, X.dtype, device, "X")
     _check("bigcn_fp4_unpack", lib().bigcn_fp4_unpack(
-        dtype, *rows, N, K, _ptr(X), ldx, _stream(stream)))
+        dtype, *_fp4(q, exps, N, K, device, "X"), N, K, x, ldx, stream))
 
 
 def bigcn_fp4_gemm(aq, a_exps, bq, b_exps, K, Z, bias=None, stream=None):
     """Z = A B^T + bias (N x F) of the 4-bit rows A (N x K) and B (F x K)."""
+    device, stream = _current(stream)
     N, F = Z.shape
-    dtype, ldz, b = _dtype(Z), _ld(Z), _vector(bias, F, "bias")
-    rows_a, rows_b = _fp4(aq, a_exps, N, K, "A"), _fp4(bq, b_exps, F, K, "B")
-    _on_device(aq, a_exps, bq, b_exps, Z, bias)
+    dtype, (z, ldz) = _dtype(Z), _rows(Z, Z.shape, Z.dtype, device, "Z")
+    a, lda, ae, ldae = _fp4(aq, a_exps, N, K, device, "A")
+    b, ldb, be, ldbe = _fp4(bq, b_exps, F, K, device, "B")
     _check("bigcn_fp4_gemm", lib().bigcn_fp4_gemm(
-        dtype, *rows_a, N, *rows_b, F, K, b, _ptr(Z), ldz, _stream(stream)))
+        dtype, a, lda, ae, ldae, N, b, ldb, be, ldbe, F, K, _floats(bias, F, device, "bias"), z, ldz,
+        stream))
 
 
 class TensorList:
@@ -724,13 +791,6 @@ def _list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
-def _lists_on_device(*lists):
-    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
-    for t in lists:
-        if t.devices - {device}:
-            raise ValueError("expected tensors on the current CUDA device")
-
-
 def bigcn_grad_norm_workspace_bytes(tensors) -> int:
     """For a list of tensors (or their number)."""
     n = tensors if isinstance(tensors, int) else len(tensors)
@@ -739,25 +799,27 @@ def bigcn_grad_norm_workspace_bytes(tensors) -> int:
 
 def bigcn_grad_norm(tensors, norm, workspace, stream=None):
     """norm (one fp32) = the norm of all tensors together (a :class:`TensorList` or tensors)."""
-    t, out = _list(tensors), _vector(norm, 1, "norm")
-    _lists_on_device(t)
-    _on_device(norm, workspace)
+    device, stream = _current(stream)
+    t, out = _list(tensors), _floats(norm, 1, device, "norm")
+    if t.devices and t.devices != {device}:
+        _elsewhere("tensors")
+    ws, ws_bytes = _room(workspace, device)
     _check("bigcn_grad_norm", lib().bigcn_grad_norm(
-        len(t), t.dtypes, t.pointers, t.counts, out, _ptr(workspace), _bytes(workspace),
-        _stream(stream)))
+        len(t), t.dtypes, t.pointers, t.counts, out, ws, ws_bytes, stream))
 
 
 def bigcn_clip_grad_norm(tensors, max_norm, norm, workspace, out=None, stream=None):
     """norm as above, and out (None: the tensors themselves) = tensors min(1, max_norm / norm)."""
-    t, n = _list(tensors), _vector(norm, 1, "norm")
+    device, stream = _current(stream)
+    t, n = _list(tensors), _floats(norm, 1, device, "norm")
     o = t if out is None else _list(out)
     if o is not t and (bytes(o.counts) != bytes(t.counts) or bytes(o.dtypes) != bytes(t.dtypes)):
         raise ValueError("out must be tensors of the same types and lengths")
-    _lists_on_device(t, o)
-    _on_device(norm, workspace)
+    if t.devices and (t.devices != {device} or o.devices != {device}):
+        _elsewhere("tensors")
+    ws, ws_bytes = _room(workspace, device)
     _check("bigcn_clip_grad_norm", lib().bigcn_clip_grad_norm(
-        len(t), t.dtypes, t.pointers, o.pointers, t.counts, max_norm, n, _ptr(workspace),
-        _bytes(workspace), _stream(stream)))
+        len(t), t.dtypes, t.pointers, o.pointers, t.counts, max_norm, n, ws, ws_bytes, stream))
 
 
 # ------------------------------------------------- allocating conveniences ---
