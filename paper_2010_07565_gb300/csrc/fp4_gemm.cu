@@ -649,9 +649,11 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     if (st != BIGCN_OK) return st;
 
     const int64_t mt = (N + kUmmaM - 1) / kUmmaM;
-    // Tiles of 256 columns read A once for twice as many, but leave no room for a second accumulator:
-    // only where the MMAs of a tile are long beside taking its sums out.
-    int NT = F > 128 && K > 2048 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
+    // Tiles of 256 columns read A once for twice as many, but leave no room for a second accumulator: only
+    // where a tile's MMAs are long beside taking its sums out, and the last tile is more than half full
+    // (2^17 rows, 256 columns of bf16: K = 8192 134 us, by 128 columns 167; K = 4096 97 and 101; K = 1024
+    // fp32 60 and 50; 219,247 x 2106 x 274 fp16 187 and 154).
+    int NT = F > 128 && K > 2048 && (F + 127) / 128 % 2 == 0 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
     while (NT > 32 && mt * ((F + NT - 1) / NT) * 2 <= dev.sm_count) NT /= 2;
     Fp4GemmArgs p;
     p.groups = int(checkpoint_groups(K));

@@ -89,7 +89,7 @@ template <int A, int J, int H, bool kKept> struct RawRow {
 // row is one warp's. kAhead: the next row is loaded before the present one is worked on, where
 // the registers allow it (16 warps an SM wait on memory otherwise).
 template <typename T, bool kRms, int A, int J, bool kKept, bool kWarp, bool kAhead>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? (kRms && J == 1 ? 4 : 2) : 1)
 backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool aligned) {
     constexpr int V = kPiece<T>, H = V / 2, kFull = full_pieces(V, J);
     __shared__ float red[2][2][kMostRowThreads / 32];
@@ -311,11 +311,17 @@ void launch_rows(BackwardArgs &a, int tpr, bool aligned, const DeviceInfo &dev, 
 template <typename T, bool kRms, int A>
 bool launch_aligned(BackwardArgs &a, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
     constexpr bool kWide = sizeof(T) == 4;      // pieces of four columns
-    const RowLayout r = row_layout(a.N, a.K, kPiece<T>, 16, kWide ? 24 : 16, dev);
+    // Up to 24 columns a thread where a row is a warp's; layer norm's, with two sums for each column, up
+    // to 16 of 16 bits (100,000 x 601 bf16 by the RMS norm: 64 threads a row 285 us, 32 185). Rows of
+    // 16 bits that a warp holds with one piece a lane, mostly filled, run at twice the warps an SM (2^20
+    // x 250 bf16 726 -> 588 us, x 256 402 -> 392; x 130 would lose, 532 -> 568).
+    const bool one = kRms && !kWide && a.K > 24 * kPiece<T> && a.K <= 32 * kPiece<T>;
+    const RowLayout r = row_layout(a.N, a.K, kPiece<T>, one ? kPiece<T> : 16,
+                                   one ? kPiece<T> : kWide || kRms ? 24 : 16, dev);
     switch (r.J) {
     case 1: launch_rows<T, kRms, A, 1>(a, r.tpr, aligned, dev, s); return true;
     case 2: launch_rows<T, kRms, A, 2>(a, r.tpr, aligned, dev, s); return true;
-    case 3: launch_rows<T, kRms, A, kWide ? 3 : 1>(a, r.tpr, aligned, dev, s); return true;
+    case 3: launch_rows<T, kRms, A, kWide || kRms ? 3 : 1>(a, r.tpr, aligned, dev, s); return true;
     case 4: launch_rows<T, kRms, A, kWide ? 4 : 1>(a, r.tpr, aligned, dev, s); return true;
     case 5: launch_rows<T, kRms, A, kWide ? 5 : 1>(a, r.tpr, aligned, dev, s); return true;
     case 6: launch_rows<T, kRms, A, kWide ? 6 : 1>(a, r.tpr, aligned, dev, s); return true;
