@@ -75,21 +75,22 @@ __global__ void __launch_bounds__(kRowThreads) param_any_kernel(const BackwardAr
 }
 
 // What a row's pieces are read as: dy, and x or the checkpoint's bytes.
-template <int A, int J, int H, bool kKept> struct RawRow {
+template <int A, int J, int H, bool kKept, bool kPast> struct RawRow {
     Raw<A> dy[J];
     Raw<A> x[kKept ? 1 : J];
     QPiece<H> q[kKept ? J : 1];
     uint8_t b[kKept ? J : 1];
+    Raw<A> ds[kPast ? J : 1];
     float rstd, mean;
-    bool dy_odd, x_odd;
+    bool dy_odd, x_odd, ds_odd;
 };
 
 // Rows in registers (norm.cuh); a.chunks blocks, block b takes the sets of rows b, b + chunks,
 // ... and keeps their sums of dy xhat and dy in the registers that hold the columns. kWarp: a
 // row is one warp's. kAhead: the next row is loaded before the present one is worked on, where
 // the registers allow it (16 warps an SM wait on memory otherwise).
-template <typename T, bool kRms, int A, int J, bool kKept, bool kWarp, bool kAhead>
-__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? (kRms && J == 1 ? 4 : 2) : 1)
+template <typename T, bool kRms, bool kPast, int A, int J, bool kKept, bool kWarp, bool kAhead>
+__global__ void __launch_bounds__(kWarp ? kRowThreads : kMostRowThreads, kWarp ? (kRms && J == 1 ? (kPast ? 3 : 4) : 2) : 1)
 backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool aligned) {
     constexpr int V = kPiece<T>, H = V / 2, kFull = full_pieces(V, J);
     __shared__ float red[2][2][kMostRowThreads / 32];
@@ -107,7 +108,7 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
     const int gstep = a.gamma ? step : 0;
 
     const bool together = kWarp || tpr >= 32;
-    auto load = [&](int64_t i, RawRow<A, J, H, kKept> &r) {
+    auto load = [&](int64_t i, RawRow<A, J, H, kKept, kPast> &r) {
         if (i >= a.N) return;
         const T *dy = static_cast<const T *>(a.dY) + i * a.lddy + k0;
         const bool dy_whole = whole_pieces<A>(dy, together);
@@ -139,18 +140,29 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
             }
             if constexpr (!kRms) r.mean = a.mean[i];
         }
+        if constexpr (kPast) {
+            const T *ds = static_cast<const T *>(a.dS) + i * a.ldds + k0;
+            const bool whole = whole_pieces<A>(ds, together);
+            r.ds_odd = odd_pieces<A>(ds);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                if (j < kFull) r.ds[j] = load16<A>(ds + j * step, whole, r.ds_odd);
+                else if (left > j * step)
+                    r.ds[j] = load_piece<T, A>(ds + j * step, left - j * step, whole, r.ds_odd);
+            }
+        }
         r.rstd = a.rstd[i];
     };
 
     const int64_t stride = int64_t(a.chunks) * rows;
     int turn = 0;
-    RawRow<A, J, H, kKept> next;
+    RawRow<A, J, H, kKept, kPast> next;
     if (kAhead) load(int64_t(blockIdx.x) * rows + slot, next);
     for (int64_t i0 = int64_t(blockIdx.x) * rows; i0 < a.N; i0 += stride) {
         const int64_t i = i0 + slot;
         const bool live = i < a.N;
         if (kWarp && !live) break;
-        RawRow<A, J, H, kKept> r;
+        RawRow<A, J, H, kKept, kPast> r;
         if (kAhead) {
             r = next;
             load(i + stride, next);
@@ -198,20 +210,6 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
             }
         }
         if (!a.dX) continue;
-        // What comes past the norm, on its way while the sums are taken.
-        Raw<A> ds[kRms ? J : 1];
-        bool ds_odd = false;
-        if constexpr (kRms) {
-            const T *p = static_cast<const T *>(a.dS) + i * a.ldds + k0;
-            const bool whole = whole_pieces<A>(p, together);
-            ds_odd = odd_pieces<A>(p);
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                ds[j] = raw_zero<A>();
-                if (a.dS && (kWarp || live) && left > j * step)
-                    ds[j] = load_piece<T, A>(p + j * step, left - j * step, whole, ds_odd);
-            }
-        }
         // Two sets of sums in turn: a set is written again only after the next one's barrier.
         float2 c0 = both(0.0f), c1;
         if constexpr (kRms) {
@@ -235,7 +233,12 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
             float2 d[H], h[H], m[H];
             if constexpr (!kHold) take(j, n, d, h, m);
             float2 past[H];
-            if constexpr (kRms) unpack16<T>(settled<A>(ds[j], ds_odd), past);
+            if constexpr (kPast) {
+                unpack16<T>(settled<A>(r.ds[j], r.ds_odd), past);
+            } else {
+#pragma unroll
+                for (int e = 0; e < H; ++e) past[e] = both(0.0f);
+            }
 #pragma unroll
             for (int e = 0; e < H; ++e) {
                 const float2 g = kHold ? gk[kHold ? j : 0][e] : __fmul2_rn(d[e], m[e]);
@@ -276,16 +279,16 @@ backward_rows_kernel(const BackwardArgs a, const int row_threads, const bool ali
     }
 }
 
-template <typename T, bool kRms, int A, int J, bool kKept, bool kWarp>
+template <typename T, bool kRms, bool kPast, int A, int J, bool kKept, bool kWarp>
 void launch_kept(BackwardArgs &a, int tpr, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
     // A row ahead where its registers and the sums' leave room for two blocks.
     constexpr bool kAhead = J * kPiece<T> <= (sizeof(T) == 4 ? 12 : 16);
-    const auto kernel = backward_rows_kernel<T, kRms, A, J, kKept, kWarp, kAhead>;
+    const auto kernel = backward_rows_kernel<T, kRms, kPast, A, J, kKept, kWarp, kAhead>;
     const int threads = tpr > kRowThreads ? tpr : kRowThreads, rows = threads / tpr;
     static const auto blocks_per_sm = [](int n) {
         int per = 1;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(
-                &per, backward_rows_kernel<T, kRms, A, J, kKept, kWarp, kAhead>, n, 0) != cudaSuccess)
+                &per, backward_rows_kernel<T, kRms, kPast, A, J, kKept, kWarp, kAhead>, n, 0) != cudaSuccess)
             cudaGetLastError();
         return per > 1 ? per : 1;
     };
@@ -297,18 +300,18 @@ void launch_kept(BackwardArgs &a, int tpr, bool aligned, const DeviceInfo &dev, 
     kernel<<<unsigned(a.chunks), threads, 0, s>>>(a, tpr, aligned);
 }
 
-template <typename T, bool kRms, int A, int J>
+template <typename T, bool kRms, bool kPast, int A, int J>
 void launch_rows(BackwardArgs &a, int tpr, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
     if (tpr == 32) {
-        if (a.X) launch_kept<T, kRms, A, J, false, true>(a, tpr, aligned, dev, s);
-        else launch_kept<T, kRms, A, J, true, true>(a, tpr, aligned, dev, s);
+        if (a.X) launch_kept<T, kRms, kPast, A, J, false, true>(a, tpr, aligned, dev, s);
+        else launch_kept<T, kRms, kPast, A, J, true, true>(a, tpr, aligned, dev, s);
     } else if constexpr (J * kPiece<T> <= 16) {
-        if (a.X) launch_kept<T, kRms, A, J, false, false>(a, tpr, aligned, dev, s);
-        else launch_kept<T, kRms, A, J, true, false>(a, tpr, aligned, dev, s);
+        if (a.X) launch_kept<T, kRms, kPast, A, J, false, false>(a, tpr, aligned, dev, s);
+        else launch_kept<T, kRms, kPast, A, J, true, false>(a, tpr, aligned, dev, s);
     }
 }
 
-template <typename T, bool kRms, int A>
+template <typename T, bool kRms, bool kPast, int A>
 bool launch_aligned(BackwardArgs &a, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
     constexpr bool kWide = sizeof(T) == 4;      // pieces of four columns
     // Up to 24 columns a thread where a row is a warp's; layer norm's, with two sums for each column, up
@@ -319,17 +322,27 @@ bool launch_aligned(BackwardArgs &a, bool aligned, const DeviceInfo &dev, cudaSt
     const RowLayout r = row_layout(a.N, a.K, kPiece<T>, one ? kPiece<T> : 16,
                                    one ? kPiece<T> : kWide || kRms ? 24 : 16, dev);
     switch (r.J) {
-    case 1: launch_rows<T, kRms, A, 1>(a, r.tpr, aligned, dev, s); return true;
-    case 2: launch_rows<T, kRms, A, 2>(a, r.tpr, aligned, dev, s); return true;
-    case 3: launch_rows<T, kRms, A, kWide || kRms ? 3 : 1>(a, r.tpr, aligned, dev, s); return true;
-    case 4: launch_rows<T, kRms, A, kWide ? 4 : 1>(a, r.tpr, aligned, dev, s); return true;
-    case 5: launch_rows<T, kRms, A, kWide ? 5 : 1>(a, r.tpr, aligned, dev, s); return true;
-    case 6: launch_rows<T, kRms, A, kWide ? 6 : 1>(a, r.tpr, aligned, dev, s); return true;
+    case 1: launch_rows<T, kRms, kPast, A, 1>(a, r.tpr, aligned, dev, s); return true;
+    case 2: launch_rows<T, kRms, kPast, A, 2>(a, r.tpr, aligned, dev, s); return true;
+    case 3: launch_rows<T, kRms, kPast, A, kWide || kRms ? 3 : 1>(a, r.tpr, aligned, dev, s); return true;
+    case 4: launch_rows<T, kRms, kPast, A, kWide ? 4 : 1>(a, r.tpr, aligned, dev, s); return true;
+    case 5: launch_rows<T, kRms, kPast, A, kWide ? 5 : 1>(a, r.tpr, aligned, dev, s); return true;
+    case 6: launch_rows<T, kRms, kPast, A, kWide ? 6 : 1>(a, r.tpr, aligned, dev, s); return true;
     }
     return false;
 }
 
 }  // namespace
+
+// kPast: with dS, whose registers the others can do without.
+template <typename T, bool kRms, bool kPast>
+bool launch_any_alignment(BackwardArgs &a, int A, bool aligned, const DeviceInfo &dev, cudaStream_t s) {
+    constexpr int kLeast = sizeof(T) == 2 ? 2 : 4;
+    return A == 16  ? launch_aligned<T, kRms, kPast, 16>(a, aligned, dev, s)
+           : A == 8 ? launch_aligned<T, kRms, kPast, 8>(a, aligned, dev, s)
+           : A == 4 ? launch_aligned<T, kRms, kPast, 4>(a, aligned, dev, s)
+                    : launch_aligned<T, kRms, kPast, kLeast>(a, aligned, dev, s);
+}
 
 template <typename T, bool kRms>
 void launch_backward(BackwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
@@ -340,10 +353,11 @@ void launch_backward(BackwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
                               uint64_t(uintptr_t(a.dS)), a.dS ? uint64_t(a.ldds) * es : 0};
     const bool aligned = aligned_to(a.gamma, 32);
     const int A = alignment_of(where, 8);
-    const bool done = A == 16  ? launch_aligned<T, kRms, 16>(a, aligned, dev, s)
-                      : A == 8 ? launch_aligned<T, kRms, 8>(a, aligned, dev, s)
-                      : A == 4 ? launch_aligned<T, kRms, 4>(a, aligned, dev, s)
-                               : launch_aligned<T, kRms, es == 2 ? 2 : 4>(a, aligned, dev, s);
+    bool done;
+    if constexpr (kRms)
+        done = a.dS ? launch_any_alignment<T, kRms, true>(a, A, aligned, dev, s)
+                    : launch_any_alignment<T, kRms, false>(a, A, aligned, dev, s);
+    else done = launch_any_alignment<T, kRms, false>(a, A, aligned, dev, s);
     if (done) return;
     const int64_t most = int64_t(dev.sm_count) * 64;
     if (a.dX) backward_any_kernel<T, kRms><<<unsigned(a.N < most ? a.N : most), kRowThreads, 0, s>>>(a);
