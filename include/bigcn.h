@@ -169,7 +169,8 @@ bigcn_status bigcn_spmm_prescaled(const int64_t *rowptr, const int32_t *colidx,
  * as FP8 +-1, exact fp32 integer sums) when K >= 128, F >= 32 and N is at
  * least 128 rows per SM, and on the CUDA cores (XOR + popcount) otherwise;
  * the dots are identical either way.
- * Its kernels, and those of the ablation products below, wait on
+ * Its kernels, and those of the ablation products, the checkpoints' weight
+ * gradient and the 4-bit product below, wait on
  * shared-memory barriers with a bounded number of tries.
  * bigcn_device_timeouts synchronizes the current device, returns how
  * many such waits ran out since its last call (0 in correct operation; a
@@ -795,7 +796,9 @@ bigcn_status bigcn_fp4_unpack(int32_t dtype, const uint8_t *q, int64_t ldq, cons
  *
  * Z     N x F of `dtype`, row stride ldz >= F, rounded once.   bias  F fp32, nullable (0).
  * The operands enter exactly; the sums are fp32, those of 64 columns at a time taken and added by
- * the tensor core, which truncates. A group of NaN makes every sum that it is part of NaN.
+ * the tensor core, which truncates: within 1.2e-7 of sum_k |a_ik b_jk| for every 64 columns, and half that
+ * for the bias. A sum's bits do not depend on the other rows and columns. A group of NaN makes every sum
+ * that it is part of NaN; sums past fp32's range are infinities.
  * The kernel waits on shared-memory barriers a bounded number of times: where a wait runs out, the
  * tile's part of Z is NaN (0 waits in correct operation; bigcn_device_timeouts counts them).
  * 0 <= N < 2^31, 1 <= K <= 32768, 1 <= F <= 2^30. Z may not overlap an input.

@@ -13,11 +13,20 @@
 //   ready[stage]   its codes and scales are there    free[stage]   its MMAs are done
 //   loaded[slot]   a unit's scale bytes landed       read[slot]    they were read
 //   summed[acc]    a tile's MMAs are done            taken[acc]    its sums were taken
-// The thread that issues is the one to spare: 100 cycles a wait that finds its phase complete, 50 an MMA, 40
-// a commit (with barriers of their own for A, B and the scales it took 700 cycles a stage, of which
-// the MMAs need 512 with 256 columns). Scale bytes that came by way of shared memory, in places filled
-// by the threads that had asked for them, cost 1500 cycles a unit: the fence before the tensor core's
-// own copy waits for all that its thread still has under way.
+// The thread that issues is the one to spare: about 50 cycles an MMA, and at first 575 a stage beside them
+// for its waits, commits and arithmetic, of the 512 that a stage's MMAs take the tensor core with 256
+// columns; 700 with barriers of their own for A, B and the scales. So one barrier says that a stage is
+// there, one that it is free, and nothing is divided or recomputed for it. (Scale bytes by way of shared memory
+// and the tensor core's own copy took as long, with one proxy fence and four more copies a unit.)
+//
+// What bounds it (L2 flushed before each call; floors at a copy's 6754 GB/s):
+//   232,965 x 602 x 128 fp32: 37 us of 28.7. Start and end of 12 tiles a CTA; B stays in shared memory
+//     (46 us when it was copied for every tile).
+//   232,965 x 128 x 602 fp32: 115 us of 85. Stores: Z's rows are aligned to 8 bytes, a store of 256 bytes
+//     touches three lines, L1 at 83 %. x 604: 110, x 640: 104, x 601 (4 bytes a lane): 191.
+//   2^17 x 8192 x 256 bf16: 138 us of 95. A's copies are 128 bytes of rows 4 KB apart and four stages of 48 KB
+//     are on their way (three: 156); a tile's sums are taken out while nothing is multiplied, 16 us of
+//     all. Tensor pipe 43 %. Prefetches of A to L2 made it slower (154 -> 173 us by boxes).
 #include "fp4.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
