@@ -202,9 +202,9 @@ def test_gemm_special_groups(cuda_device):
     within(np.where(out, 0.0, Z), np.where(out, 0.0, ref), bound, "Z")
 
 
-def test_gemm_rows_do_not_depend_on_others(cuda_device):
+@pytest.mark.parametrize("K,F", [(1000, 300), (4100, 256)])
+def test_gemm_rows_do_not_depend_on_others(cuda_device, K, F):
     """A row's products are the same bits alone, among others, and in another tile of columns."""
-    K, F = 1000, 300
     (qa, ea), (qb, eb), _, _ = operands(2000, K, F, cuda_device)
     Z = B.fp4_gemm(qa, ea, qb, eb, K)
     for i in (0, 127, 128, 1999):
