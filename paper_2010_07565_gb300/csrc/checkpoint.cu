@@ -1,8 +1,6 @@
 // Activations to 8 bits and back (bigcn_checkpoint_pack, bigcn_checkpoint_unpack): the arithmetic
 // is checkpoint.cuh's, a few operations a column; both are bound by memory. 2^20 x 512 bf16: packing
-// 247 us (0.95 of a copy's rate), unpacking 362 us (0.66: two bytes written for one read, DRAM at
-// half its rate; neither streaming stores nor more or fewer pieces a thread changed that), 395 with
-// gamma and beta.
+// 247 us (0.95 of a copy's rate), unpacking 267 us (0.90), 395 with gamma and beta.
 #include "norm.cuh"
 
 namespace bigcn {
@@ -131,6 +129,46 @@ unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
     }
 }
 
+// Without gamma and beta: rows as one sequence of pieces, so that every lane has work whatever a row's length
+// (232,965 x 602 to bf16 111 -> 80 us, to fp32 173 -> 108; 2^20 x 512 bf16 363 -> 267, 298 with four pieces a
+// thread).
+template <typename T> constexpr int kValuePieces = sizeof(T) == 4 ? 3 : 2;      // a thread's
+template <typename T, int A>
+__global__ void __launch_bounds__(kCkThreads)
+values_kernel(const CkArgs a, const uint32_t per_row, const uint32_t magic) {
+    constexpr int V = kPiece<T>, H = V / 2, kUnits = kValuePieces<T>;
+    const PieceWalk<kUnits * kCkThreads> walk(per_row, magic);
+    QPiece<H> w[kUnits];
+    uint8_t b[kUnits];
+    T *to[kUnits];
+    int n[kUnits];                // of the piece's columns in the row
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        int64_t row;
+        uint32_t piece;
+        walk.at(threadIdx.x + u * kCkThreads, row, piece);
+        to[u] = static_cast<T *>(a.X) + row * a.ldx + int64_t(piece) * V;
+        n[u] = row < a.N ? a.K - int(piece) * V : 0;
+        if (n[u] > 0) {
+            w[u] = *reinterpret_cast<const QPiece<H> *>(a.q + row * a.ldq + int64_t(piece) * V);
+            b[u] = a.exps[row * a.lde + piece / (kGroup / V)];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        if (n[u] <= 0) continue;
+        float2 v[H];
+        dequantise_piece<H>(w[u], unpack_factor(b[u]), v);
+        store_piece<T, A>(to[u], pack16<T>(v), n[u], whole_pieces<A>(to[u], true));
+    }
+}
+template <typename T, int A> void launch_values(const CkArgs &a, cudaStream_t s) {
+    const uint32_t per_row = uint32_t(checkpoint_groups(a.K) * (kGroup / kPiece<T>));
+    const int64_t block = kValuePieces<T> * kCkThreads;
+    values_kernel<T, A><<<unsigned((a.N * int64_t(per_row) + block - 1) / block), kCkThreads, 0, s>>>(
+        a, per_row, piece_magic(per_row));
+}
+
 template <typename T, int A, int J, int R>
 void launch_pieces(const CkArgs &a, bool pack, int tpr, unsigned parts, cudaStream_t s) {
     const int64_t rows = kCkThreads / tpr * R;
@@ -143,6 +181,7 @@ void launch_pieces(const CkArgs &a, bool pack, int tpr, unsigned parts, cudaStre
 // several blocks a row.
 template <typename T, int A>
 void launch_checkpoint_rows(const CkArgs &a, bool pack, cudaStream_t s) {
+    if (!pack && !a.gamma && !a.beta) return launch_values<T, A>(a, s);
     const int64_t pieces = (int64_t(a.K) + kPiece<T> - 1) / kPiece<T>;
     int tpr = 8;
     while (tpr < kCkThreads && int64_t(tpr) * 4 < pieces) tpr *= 2;

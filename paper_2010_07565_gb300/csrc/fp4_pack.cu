@@ -28,31 +28,6 @@ struct Fp4Args {
 // Pieces per thread: all asked for before the first is used.
 constexpr int kFp4Pieces = 4;
 
-// Where a block's pieces (or octets) lie: piece kBlock blockIdx.x + i of all is piece `k` of row `row`.
-template <int kBlock>
-struct PieceWalk {
-    int64_t row0;
-    uint32_t r0, per_row, magic;
-    __device__ __forceinline__ PieceWalk(uint32_t per, uint32_t mag) : per_row(per), magic(mag) {
-        const uint64_t first = uint64_t(blockIdx.x) * kBlock;
-        if (first >> 32 == 0) {
-            row0 = uint32_t(first) / per;
-            r0 = uint32_t(first) - uint32_t(row0) * per;
-        } else {
-            row0 = int64_t(first / per);
-            r0 = uint32_t(first - uint64_t(row0) * per);
-        }
-    }
-    // (Below kBlock pieces a row the product with floor(2^32 / per_row) + 1 has the quotient in its
-    // upper half: r0 + i < 2 kBlock, and its excess, at most per_row for each 2^32, stays below one.)
-    __device__ __forceinline__ void at(uint32_t i, int64_t &row, uint32_t &k) const {
-        const uint32_t t = r0 + i;
-        const uint32_t q = per_row > kBlock ? uint32_t(t >= per_row) : __umulhi(t, magic);
-        row = row0 + q;
-        k = t - q * per_row;
-    }
-};
-
 // An octet, 8 columns (P pieces), a lane: a word of codes.
 template <typename T, int A>
 __global__ void __launch_bounds__(kFp4Threads)
@@ -154,7 +129,7 @@ template <typename T, int A>
 void launch_fp4_rows(const Fp4Args &a, bool pack, cudaStream_t s) {
     const int columns = pack ? 8 : kPiece<T>;               // of a thread's unit
     const uint32_t per_row = uint32_t(checkpoint_groups(a.K) * (kGroup / columns));
-    const uint32_t magic = uint32_t((uint64_t(1) << 32) / per_row + 1);
+    const uint32_t magic = piece_magic(per_row);
     const int64_t block = kFp4Threads * (pack ? kFp4Pieces * kPiece<T> / 8 : kFp4Pieces);
     const unsigned blocks = unsigned((a.N * int64_t(per_row) + block - 1) / block);
     if (pack) fp4_pack_kernel<T, A><<<blocks, kFp4Threads, 0, s>>>(a, per_row, magic);

@@ -338,6 +338,34 @@ inline RowLayout row_layout(int64_t N, int K, int V, int most, int warp_most, co
     return {tpr, fit(tpr)};
 }
 
+// Rows as one sequence of pieces (or octets), per_row of them a row, whole groups: piece kBlock blockIdx.x +
+// i of all is piece `k` of row `row`. `magic` is piece_magic(per_row).
+template <int kBlock>
+struct PieceWalk {
+    int64_t row0;
+    uint32_t r0, per_row, magic;
+    __device__ __forceinline__ PieceWalk(uint32_t per, uint32_t mag) : per_row(per), magic(mag) {
+        const uint64_t first = uint64_t(blockIdx.x) * kBlock;
+        if (first >> 32 == 0) {
+            row0 = uint32_t(first) / per;
+            r0 = uint32_t(first) - uint32_t(row0) * per;
+        } else {
+            row0 = int64_t(first / per);
+            r0 = uint32_t(first - uint64_t(row0) * per);
+        }
+    }
+    // (Below kBlock pieces a row the product with floor(2^32 / per_row) + 1 has the quotient in its
+    // upper half: r0 + i < 2 kBlock, and its excess, at most per_row for each 2^32, stays below one.)
+    __device__ __forceinline__ void at(uint32_t i, int64_t &row, uint32_t &k) const {
+        const uint32_t t = r0 + i;
+        const uint32_t q = per_row > kBlock ? uint32_t(t >= per_row) : __umulhi(t, magic);
+        row = row0 + q;
+        k = t - q * per_row;
+    }
+};
+
+inline uint32_t piece_magic(uint32_t per_row) { return uint32_t((uint64_t(1) << 32) / per_row + 1); }
+
 // The alignment in bytes, at most 16, of everything in `addresses` (pointers and byte strides).
 inline int alignment_of(const uint64_t *addresses, int n) {
     uint64_t all = 16;
