@@ -20,13 +20,14 @@
 // and the tensor core's own copy took as long, with one proxy fence and four more copies a unit.)
 //
 // What bounds it (L2 flushed before each call; floors at a copy's 6754 GB/s):
-//   232,965 x 602 x 128 fp32: 37 us of 28.7. Start and end of 12 tiles a CTA; B stays in shared memory
+//   232,965 x 602 x 128 fp32: 38 us of 28.7. Start and end of 12 tiles a CTA; B stays in shared memory
 //     (46 us when it was copied for every tile).
-//   232,965 x 128 x 602 fp32: 115 us of 85. Stores: Z's rows are aligned to 8 bytes, a store of 256 bytes
-//     touches three lines, L1 at 83 %. x 604: 110, x 640: 104, x 601 (4 bytes a lane): 191.
-//   2^17 x 8192 x 256 bf16: 138 us of 95. A's copies are 128 bytes of rows 4 KB apart and four stages of 48 KB
-//     are on their way (three: 156); a tile's sums are taken out while nothing is multiplied, 16 us of
-//     all. Tensor pipe 43 %. Prefetches of A to L2 made it slower (154 -> 173 us by boxes).
+//   232,965 x 128 x 602 fp32: 116 us of 85. Stores: Z's rows are aligned to 8 bytes, a store of 256 bytes
+//     touches three lines, L1 at 83 %. x 604: 109, x 640: 103, x 601 (4 bytes a lane): 191.
+//   2^17 x 8192 x 256 bf16: 132 us of 95. A's copies are 128 bytes of rows 4 KB apart, and a stage's boxes and
+//     MMAs wait for each other 40 % of the issuing thread's time; sums are taken out while nothing is
+//     multiplied, 10 to 16 us of all. More of A on its way did not help (six stages of A beside three of
+//     B 159, boxes of two stages at a time 165, prefetches to L2 by a warp of their own 148, all for 142).
 #include "fp4.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -86,7 +87,7 @@ struct Fp4GemmArgs {
     void *Z;
     int64_t ldz;
     int vec;                 // bytes that Z and its rows are aligned to, at most 32
-    bool direct;             // sums go straight to Z (store_direct)
+    bool direct;             // 16-bit sums, or those of 256 columns, go straight to Z (store_direct)
 };
 
 // Instruction descriptor of the block-scaled product: e2m1 x e2m1, both K-major, ue8m0 scales, M =
@@ -158,7 +159,9 @@ __device__ __forceinline__ void store_sums(const float *stage, T *z, int64_t ldz
     constexpr int kPitch = kBatch + 4, kCols = VB / int(sizeof(T));
     constexpr int kLanes = kBatch / kCols < 32 ? kBatch / kCols : 32;       // of a row
     constexpr int kParts = kBatch / kCols / kLanes, kRows = 32 / kLanes, kTurns = kStore / kRows;
-    constexpr int kMost = kCols >= 8 ? 4 : 8, kAtOnce = kTurns < kMost ? kTurns : kMost;
+    // (Few rows at once: the roles' code together is more than the instruction caches like. Sixteen rows of two
+    // columns 123 to 126 us, eight 122, four and two 117, 232,965 x 128 x 602 fp32.)
+    constexpr int kMost = kCols >= 4 && kCols < 8 ? 8 : 4, kAtOnce = kTurns < kMost ? kTurns : kMost;
     static_assert(kTurns > 0 && kTurns % kAtOnce == 0, "whole turns");
     const int r0 = lane / kLanes, c0 = lane % kLanes * kCols;
     const int64_t step = kRows * ldz;
@@ -197,10 +200,10 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
                  "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                  : "memory");
 }
-__device__ __forceinline__ void add_bias(uint32_t (&v)[32], int cols, const float *bias, float *stage,
-                                         int lane) {
+// The columns' biases, each lane's own in `bias`, to 32 sums of a row.
+__device__ __forceinline__ void add_bias(uint32_t (&v)[32], float bias, float *stage, int lane) {
     __syncwarp();
-    stage[lane] = lane < cols ? __ldg(bias + lane) : 0.0f;
+    stage[lane] = bias;
     __syncwarp();
 #pragma unroll
     for (int e = 0; e < 32; e += 4) {
@@ -539,6 +542,20 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             const int64_t row0 = t.m0() + 32 * quad;
             const int n0 = int(t.n) * NT, cols = min(NT, p.F - n0);
             const int rows = int(min(int64_t(32), max(int64_t(0), p.N - row0)));
+            const float *bias = p.bias ? p.bias + n0 : nullptr;
+            // Straight stores: parts of 32 columns, kStep apart; the biases of several come while the MMAs are on their way.
+            constexpr bool kDirect = sizeof(T) == 2 || NT >= 256;
+            constexpr int kStep = S::kOutWarps / 4 * kWidth, kParts = NT > kStep ? NT / kStep : 1;
+            const int c0 = kWidth * (S::kPair ? out : half);
+            float own[kParts];
+            auto load_own = [&] {
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) {
+                    const int c = c0 + q * kStep + lane;
+                    own[q] = bias && c < cols ? __ldg(bias + c) : 0.0f;
+                }
+            };
+            if (kDirect && kParts > 1 && p.direct) load_own();
             if (ok) {
                 ok = __all_sync(kFullMask, wait_unless(smem_addr(&summed[b]), parity, stopv));
                 if (!ok) *stopv = 1u;
@@ -546,28 +563,39 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (uint32_t(32 * quad) << 16) + uint32_t(b * NT);
             T *z = static_cast<T *>(p.Z) + row0 * p.ldz + n0;
-            const float *bias = p.bias ? p.bias + n0 : nullptr;
             auto taken_out = [&] {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&taken[b]));
             };
-            if (p.direct) {
-                // (The accumulator given back before the stores, or all columns' 16-bit sums held until
-                // then: 2^17 x 8192 x 256 bf16 134 and 136 us for 134, 232,965 x 128 x 640 87 for 83.)
+            if (kDirect && p.direct) {
+                // With one accumulator 16-bit sums are held until it has been given back (with the biases loaded
+                // ahead 2^17 x 8192 x 256 bf16 142 -> 136 us).
+                constexpr bool kHold = S::kAccs == 1 && sizeof(T) == 2;
+                if (kParts == 1) load_own();
                 T *row = z + lane * p.ldz;
-#pragma unroll 1
-                for (int c = kWidth * (S::kPair ? out : half); c < cols; c += S::kOutWarps / 4 * kWidth) {
-                    uint32_t v[32], w[kWordsOut<T>];
+                uint32_t w[kHold ? kParts : 1][kWordsOut<T>];
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) {
+                    const int c = c0 + q * kStep;
+                    if (c >= cols) break;
+                    uint32_t v[32];
                     tmem_ld32(acc + uint32_t(c), v);
                     if (!ok)
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0x7FC00000u;
-                    if (bias) add_bias(v, cols - c, bias + c, stage + 36 * mate, lane);
-                    pack_sums<T>(v, w);
-                    if (lane < rows) store_direct<T>(w, row + c, cols - c);
+                    if (bias) add_bias(v, own[q], stage + 36 * mate, lane);
+                    pack_sums<T>(v, w[kHold ? q : 0]);
+                    if (!kHold && lane < rows) store_direct<T>(w[0], row + c, cols - c);
                 }
                 taken_out();
+                if constexpr (kHold) {
+#pragma unroll
+                    for (int q = 0; q < kParts; ++q) {
+                        const int c = c0 + q * kStep;
+                        if (c < cols && lane < rows) store_direct<T>(w[q], row + c, cols - c);
+                    }
+                }
             } else {
 #pragma unroll 1
                 for (int c = kBatch * half; c < cols; c += 2 * kBatch) {
@@ -702,7 +730,7 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     p.ldz = ldz;
     const uint64_t where = uint64_t(uintptr_t(Z)) | uint64_t(N > 1 ? ldz : 0) * es | 32;
     p.vec = int(where & (~where + 1));
-    p.direct = p.vec == 32 && (es == 2 || NT == 256);
+    p.direct = p.vec == 32;
     const unsigned grid = unsigned(tiles < dev.sm_count ? tiles : dev.sm_count);
     p.step_m = grid / uint32_t(p.nt);
     p.step_n = grid % uint32_t(p.nt);
