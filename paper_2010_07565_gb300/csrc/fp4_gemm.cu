@@ -438,7 +438,6 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
     volatile uint32_t *const stopv = &stop;
     const int stages = (p.groups + 7) / 8;              // of a tile
 
-
     if (warp == 0) {
         // Copies into the ring of stages.
         int s = 0, issued = 0;
@@ -543,7 +542,8 @@ fp4_gemm_kernel(const __grid_constant__ Fp4GemmArgs p) {
             const int n0 = int(t.n) * NT, cols = min(NT, p.F - n0);
             const int rows = int(min(int64_t(32), max(int64_t(0), p.N - row0)));
             const float *bias = p.bias ? p.bias + n0 : nullptr;
-            // Straight stores: parts of 32 columns, kStep apart; the biases of several come while the MMAs are on their way.
+            // Straight stores: parts of 32 columns, kStep apart; the biases of several come while the MMAs
+            // are on their way.
             constexpr bool kDirect = sizeof(T) == 2 || NT >= 256;
             constexpr int kStep = S::kOutWarps / 4 * kWidth, kParts = NT > kStep ? NT / kStep : 1;
             const int c0 = kWidth * (S::kPair ? out : half);
