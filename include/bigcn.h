@@ -677,10 +677,11 @@ bigcn_status bigcn_layer_norm_backward(int32_t dtype, const void *dY, int64_t N,
  * X, R, S, Y   N x K of `dtype`, row strides ldx, ldr, lds, ldy >= K. R nullable (s = x; S is then
  *        NULL too). S, Y nullable. S may take the place of R or of X: the same pointer and row stride.
  * gamma  K fp32, nullable (1).   eps finite, >= 0 (0 with a row of zeros divides by zero: that
- *        row is NaN).
- * rstd   N fp32, nullable: the backward's input. Right for every finite row: where single squares
- *        would leave fp32's range the sum is taken of scaled values (above 2^126 in magnitude rstd is
- *        subnormal and has fewer bits).
+ *        row's shat is NaN, its rstd infinite).
+ * rstd   N fp32, nullable: the backward's input. Where single squares would leave fp32's range the sum is
+ *        taken of scaled values, so that shat, Y and the checkpoint are right for every finite row (above 2^126
+ *        in root mean square rstd is subnormal, and they have fewer bits). Below 2^-128 without an eps rstd
+ *        passes fp32's range and is infinite: the backward of such a row is not finite.
  * q, exps (nullable, both or neither)   receive the checkpoint of shat.
  * A row with a NaN or an infinity (of the sum, which may pass fp16's range) has rstd NaN, and so its
  * shat and Y. At least one output is given. 0 <= N < 2^31, 1 <= K <= 2^30. No output may overlap another

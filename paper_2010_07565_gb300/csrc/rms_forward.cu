@@ -36,18 +36,36 @@ struct RmsForwardArgs {
 };
 
 // rstd from the sum of squares. Where that has left the range in which single squares keep fp32's
-// precision, it is taken again of s 2^-96 or, where eps does not cover it, of s 2^96: `again` is a
-// factor's sum of squares. A row with a NaN or an infinity gets NaN.
+// precision, it is taken again of s 2^-96 or, where eps does not cover it, of s 2^110 (whose sum stays below
+// 2^124, eps's share below 2^126): `again` is a factor's sum of squares. A row with a NaN or an infinity gets NaN.
+constexpr float kDown = 0x1p-96f, kUp = 0x1p110f;
+__device__ __forceinline__ float squares_factor(float ss, float eps) {
+    return !(ss <= 0x1p100f) ? kDown : ss < 0x1p-96f && eps < 0x1p-94f ? kUp : 1.0f;
+}
+// `by`: shat is s by, or (s 2^110) by where the sum was taken of that, as rstd = 2^110 by may be infinite.
+struct Rstd {
+    float rstd, by;
+    bool up;
+};
 template <typename Again>
-__device__ __forceinline__ float rstd_of(float ss, int K, float inv_k, float eps, Again again) {
-    float f = 1.0f;
-    if (!(ss <= 0x1p100f)) f = 0x1p-96f;
-    else if (ss < 0x1p-96f && eps < 0x1p-66f) f = 0x1p96f;
+__device__ __forceinline__ Rstd rstd_of(float ss, int K, float inv_k, float eps, Again again) {
+    const float f = squares_factor(ss, eps);
     if (f != 1.0f) {
         ss = again(f);
-        if (!(ss < __int_as_float(0x7F800000))) return __int_as_float(0x7FC00000);
+        if (!(ss < __int_as_float(0x7F800000))) {
+            const float nan = __int_as_float(0x7FC00000);
+            return {nan, nan, false};
+        }
     }
-    return f / sqrtf(fmaf(eps * f, f, ss * inv_k));
+    const float root = sqrtf(fmaf(eps * f, f, ss * inv_k)), rstd = f / root;
+    return {rstd, f == kUp ? 1.0f / root : rstd, f == kUp};
+}
+
+// A word of a row times 2^110.
+template <typename T> __device__ __forceinline__ uint32_t word_up(uint32_t w) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(__uint_as_float(w) * kUp);
+    const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __float2bfloat162_rn(kUp));
+    return *reinterpret_cast<const uint32_t *>(&v);
 }
 
 // Rows that do not fit registers: a block per row, which walks it two or three times; the later
@@ -75,7 +93,7 @@ __global__ void __launch_bounds__(kRowThreads) rms_forward_any_kernel(const RmsF
             s[0] = fmaf(to_f32(v), to_f32(v), s[0]);
         }
         block_sum(s);
-        const float rstd = rstd_of(s[0], K, inv_k, a.eps, [&](float f) {
+        const Rstd r_of = rstd_of(s[0], K, inv_k, a.eps, [&](float f) {
             float again[1] = {0.0f};
             for (int g = warp; g < groups; g += kWarps) {
                 const int k = g * kGroup + lane;
@@ -86,12 +104,13 @@ __global__ void __launch_bounds__(kRowThreads) rms_forward_any_kernel(const RmsF
             block_sum(again);
             return again[0];
         });
-        if (threadIdx.x == 0 && a.rstd) a.rstd[i] = rstd;
+        if (threadIdx.x == 0 && a.rstd) a.rstd[i] = r_of.rstd;
+        const float up = r_of.up ? kUp : 1.0f;
         for (int g = warp; g < groups; g += kWarps) {
             const int k = g * kGroup + lane;
             float v = 0.0f;
             if (k < K) {
-                v = at(k) * rstd;
+                v = at(k) * up * r_of.by;
                 if (a.Y)
                     static_cast<T *>(a.Y)[i * a.ldy + k] =
                         from_f32<T>(v * (a.gamma ? __ldg(a.gamma + k) : 1.0f));
@@ -176,19 +195,25 @@ rms_forward_kernel(const RmsForwardArgs a, const int row_threads, const bool ali
     // Whether a row's sum is taken again is decided by its warps alike, but rows of a block's other
     // warps, or of other lanes, may differ: where a row is not one warp's, all take the sum again where any must.
     const float ss = squares(1.0f, red0);
-    float rstd;
+    Rstd r;
     if constexpr (kWarp) {
-        rstd = rstd_of(ss, K, inv_k, a.eps, [&](float f) { return squares(f, red1); });
+        r = rstd_of(ss, K, inv_k, a.eps, [&](float f) { return squares(f, red1); });
     } else {
-        const float f = !(ss <= 0x1p100f)                              ? 0x1p-96f
-                        : ss < 0x1p-96f && a.eps < 0x1p-66f ? 0x1p96f
-                                                            : 1.0f;
+        const float f = squares_factor(ss, a.eps);
         float again = ss;
         if (__syncthreads_or(live && f != 1.0f)) again = squares(f, red1);
-        rstd = rstd_of(ss, K, inv_k, a.eps, [&](float) { return again; });
+        r = rstd_of(ss, K, inv_k, a.eps, [&](float) { return again; });
         if (!kKeep && !live) return;            // (with a checkpoint lanes still meet below)
     }
-    if (live && t == 0 && a.rstd) a.rstd[i] = rstd;
+    if (live && t == 0 && a.rstd) a.rstd[i] = r.rstd;
+    // (The sum has been stored; a power of two is exact on such rows. fp16 has no magnitude as small.)
+    if constexpr (!std::is_same<T, __half>::value) {
+        if (r.up) {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                w[j] = make_uint4(word_up<T>(w[j].x), word_up<T>(w[j].y), word_up<T>(w[j].z), word_up<T>(w[j].w));
+        }
+    }
     T *out = static_cast<T *>(a.Y) + i * a.ldy + k0;
     const bool y_whole = whole_pieces<A>(out, together);
     int8_t *q = a.q + i * a.ldq + k0;
@@ -209,7 +234,7 @@ rms_forward_kernel(const RmsForwardArgs a, const int row_threads, const bool ali
             const int j = j0 + u, n = j < kFull ? V : left - j * step;
             unpack16<T>(w[j], x[u]);
 #pragma unroll
-            for (int e = 0; e < H; ++e) x[u][e] = __fmul2_rn(x[u][e], both(rstd));
+            for (int e = 0; e < H; ++e) x[u][e] = __fmul2_rn(x[u][e], both(r.by));
             if (kKeep) {
                 // (Behind the row a zero stays one, whatever rstd is.)
                 if (j >= kFull && n < V) clear_from(x[u], n);
