@@ -29,12 +29,12 @@ __global__ void __launch_bounds__(kRowThreads) backward_any_kernel(const Backwar
         T *dx = static_cast<T *>(a.dX) + i * a.lddx;
         const T *ds = kRms && a.dS ? static_cast<const T *>(a.dS) + i * a.ldds : nullptr;
         const float rstd = a.rstd[i], mean = !kRms && a.X ? a.mean[i] : 0.0f;
-        float s[2] = {0.0f, 0.0f};
-        for (int k = threadIdx.x; k < K; k += kRowThreads) {
+        float s[2];
+        share_sums<true>(K, s, [&](int k, float (&run)[2]) {
             const float g = to_f32(dy[k]) * (a.gamma ? __ldg(a.gamma + k) : 1.0f);
-            s[0] += g;
-            s[1] = fmaf(g, xhat_at<T, kRms>(a, i, k, mean, rstd), s[1]);
-        }
+            run[0] += g;
+            run[1] = fmaf(g, xhat_at<T, kRms>(a, i, k, mean, rstd), run[1]);
+        });
         block_sum(s);
         const float c0 = s[0] * inv_k, c1 = s[1] * inv_k;
         for (int k = threadIdx.x; k < K; k += kRowThreads) {

@@ -40,13 +40,13 @@ struct ForwardArgs {
 // The row's mean and variance from m0, S1 = sum d and S2 = sum d^2: m0 + S1 / K and S2 / K - (S1 / K)^2.
 // The difference cancels only where the spread is below m0's own error, some ulps of the row's
 // level. In a constant row it is what the rounding of the sums leaves, at most 3 (K / 32 + 40) u of
-// S2 (u = 2^-24; rows of 16384 columns: 2^-13.2; the threads of longer ones add K / 256): taken for 0.
-// (A NaN stays one.)
+// S2 (u = 2^-24; rows of 16384 columns: 2^-13.2; the threads of longer ones add K / 256 terms, 256 at a
+// time): taken for 0. (A NaN stays one.)
 __device__ __forceinline__ void finish_moments(float (&s)[2], int K, float inv_k, float &mean,
                                                float &variance) {
     const float c = s[0] * inv_k, left = fmaf(-s[0], c, s[1]);
     mean += c;
-    variance = left < s[1] * fmaf(float(K), 0x1p-29f, 0x1p-13f) ? 0.0f : left * inv_k;
+    variance = left < s[1] * fmaf(float(min(K, kRowThreads * kRun)), 0x1p-29f, 0x1p-13f) ? 0.0f : left * inv_k;
 }
 
 // Rows that do not fit registers (more than 8192 fp32 or 16384 16-bit columns): a block per
@@ -60,15 +60,15 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
     for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
         const T *x = static_cast<const T *>(a.X) + i * a.ldx;
         T *y = static_cast<T *>(a.Y) + i * a.ldy;
-        float s0[1] = {0.0f}, s[2] = {0.0f, 0.0f}, variance;
-        for (int k = threadIdx.x; k < K; k += kRowThreads) s0[0] += to_f32(x[k]);
+        float s0[1], s[2], variance;
+        share_sums<false>(K, s0, [&](int k, float (&run)[1]) { run[0] += to_f32(x[k]); });
         block_sum(s0);
         float mean = s0[0] * inv_k;
-        for (int k = threadIdx.x; k < K; k += kRowThreads) {
+        share_sums<false>(K, s, [&](int k, float (&run)[2]) {
             const float d = to_f32(x[k]) - mean;
-            s[0] += d;
-            s[1] = fmaf(d, d, s[1]);
-        }
+            run[0] += d;
+            run[1] = fmaf(d, d, run[1]);
+        });
         block_sum(s);
         finish_moments(s, K, inv_k, mean, variance);
         const float rstd = 1.0f / sqrtf(variance + a.eps);

@@ -84,23 +84,19 @@ __global__ void __launch_bounds__(kRowThreads) rms_forward_any_kernel(const RmsF
         auto fresh = [&](int k) { return r ? from_f32<T>(to_f32(x[k]) + to_f32(r[k])) : x[k]; };
         // (Once the sum is stored it is read there: it may have taken r's or x's place.)
         auto at = [&](int k) { return to_f32(sum ? sum[k] : fresh(k)); };
-        float s[1] = {0.0f};
-        for (int g = warp; g < groups; g += kWarps) {
-            const int k = g * kGroup + lane;
-            if (k >= K) continue;
+        float s[1];
+        share_sums<false>(K, s, [&](int k, float (&run)[1]) {
             const T v = fresh(k);
             if (sum) sum[k] = v;
-            s[0] = fmaf(to_f32(v), to_f32(v), s[0]);
-        }
+            run[0] = fmaf(to_f32(v), to_f32(v), run[0]);
+        });
         block_sum(s);
         const Rstd r_of = rstd_of(s[0], K, inv_k, a.eps, [&](float f) {
-            float again[1] = {0.0f};
-            for (int g = warp; g < groups; g += kWarps) {
-                const int k = g * kGroup + lane;
-                if (k >= K) continue;
+            float again[1];
+            share_sums<false>(K, again, [&](int k, float (&run)[1]) {
                 const float v = at(k) * f;
-                again[0] = fmaf(v, v, again[0]);
-            }
+                run[0] = fmaf(v, v, run[0]);
+            });
             block_sum(again);
             return again[0];
         });
