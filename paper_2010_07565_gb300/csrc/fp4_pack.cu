@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kFp4Threads, 4)
 fp4_columns_kernel(const T *__restrict__ W, int K, int F, int64_t ldw, bool wide, uint8_t *__restrict__ q,
                    int64_t ldq, uint8_t *__restrict__ exps, int64_t lde) {
     constexpr int V = kPiece<T>, kCols = 8 * V;
-    __shared__ uint32_t codes[kCols][kColumnGroups * 4 + 4];
+    __shared__ __align__(16) uint32_t codes[kCols][kColumnGroups * 4 + 4];      // (read 16 bytes at a time)
     __shared__ uint8_t bytes[kCols][kColumnGroups];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int column = lane % 8 * V, octet = lane / 8;
