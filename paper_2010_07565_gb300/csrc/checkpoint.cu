@@ -89,6 +89,7 @@ pack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
     }
 }
 
+// With gamma, beta or both (values_kernel below: without).
 template <typename T, int A, int J, int R>
 __global__ void __launch_bounds__(kCkThreads)
 unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
@@ -119,10 +120,9 @@ unpack_kernel(const CkArgs a, const int tpr, const unsigned parts) {
             if (at.i[r] >= a.N) continue;
             float2 v[H];
             dequantise_piece<H>(w[r][j], unpack_factor(b[r][j]), v);
-            if (a.gamma || a.beta)
 #pragma unroll
-                for (int e = 0; e < H; ++e)
-                    v[e] = __ffma2_rn(v[e], a.gamma ? g[e] : both(1.0f), a.beta ? c[e] : both(0.0f));
+            for (int e = 0; e < H; ++e)
+                v[e] = __ffma2_rn(v[e], a.gamma ? g[e] : both(1.0f), a.beta ? c[e] : both(0.0f));
             T *out = static_cast<T *>(a.X) + at.i[r] * a.ldx + k;
             store_piece<T, A>(out, pack16<T>(v), n, whole_pieces<A>(out, tpr >= 32));
         }

@@ -34,17 +34,6 @@ __device__ __forceinline__ uint32_t fp4_codes(float v0, float v1, float v2, floa
         : "f"(v0), "f"(v1), "f"(v2), "f"(v3), "f"(v4), "f"(v5), "f"(v6), "f"(v7));
     return r;
 }
-// Four values to the low half of a word.
-__device__ __forceinline__ uint32_t fp4_codes4(float v0, float v1, float v2, float v3) {
-    uint32_t r;
-    asm("{\n.reg .b8 a, b;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
-        "mov.b32 %0, {a, b, a, b};\n}"
-        : "=r"(r)
-        : "f"(v0), "f"(v1), "f"(v2), "f"(v3));
-    return r & 0xFFFFu;
-}
 
 // A word of codes to eight halves (exact), in pairs.
 __device__ __forceinline__ void fp4_halves(uint32_t w, uint32_t (&h)[4]) {

@@ -33,8 +33,7 @@ inline EncodeTiled encoder() {
 // of `parts` parts of `width` elements, box_parts of which are in a box.
 inline bool encode_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t width,
                        int64_t rows, int64_t row_bytes, int box, int box_rows, bool swizzle,
-                       int64_t parts = 1, int64_t part_bytes = 0, int box_parts = 1,
-                       CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_128B) {
+                       int64_t parts = 1, int64_t part_bytes = 0, int box_parts = 1) {
     const EncodeTiled fn = encoder();
     if (!fn) return false;
     const cuuint64_t dims[3] = {cuuint64_t(width), cuuint64_t(rows), cuuint64_t(parts)};
@@ -44,7 +43,7 @@ inline bool encode_map(CUtensorMap *map, CUtensorMapDataType type, const void *b
     return fn(map, type, part_bytes ? 3 : 2, const_cast<void *>(base), dims, strides, boxes, steps,
               CU_TENSOR_MAP_INTERLEAVE_NONE,
               swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-              promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace bigcn
