@@ -798,8 +798,8 @@ bigcn_status bigcn_fp4_unpack(int32_t dtype, const uint8_t *q, int64_t ldq, cons
  * Z     N x F of `dtype`, row stride ldz >= F, rounded once.   bias  F fp32, nullable (0).
  * The operands enter exactly; the sums are fp32, those of 64 columns at a time taken and added by
  * the tensor core, which truncates: within 1.2e-7 of sum_k |a_ik b_jk| for every 64 columns, and half that
- * for the bias. A sum's bits do not depend on the other rows and columns. A group of NaN makes every sum
- * that it is part of NaN; sums past fp32's range are infinities.
+ * for the bias (below 2^-126 a sum may count as 0). A sum's bits do not depend on the other rows and
+ * columns. A group of NaN makes every sum that it is part of NaN; sums past fp32's range are infinities.
  * The kernel waits on shared-memory barriers a bounded number of times: where a wait runs out, the
  * tile's part of Z is NaN (0 waits in correct operation; bigcn_device_timeouts counts them).
  * 0 <= N < 2^31, 1 <= K <= 32768, 1 <= F <= 2^30. Z may not overlap an input.
@@ -819,7 +819,8 @@ size_t bigcn_grad_norm_workspace_bytes(int32_t n);
  *        elements, which lie one behind the other, and how many they are (0: the pointer is not
  *        looked at). They are read before the call returns; a captured call keeps what they said.
  * norm   one fp32, rounded once of 64-bit sums of fp32 sums of at most 32 squares each (relative error
- *        below 2^-20), whatever the elements' range; NaN or an infinity where the tensors hold one.
+ *        below 2^-20, but for a norm that is subnormal), whatever the elements' range; NaN or an infinity where
+ *        the tensors hold one, an infinity also past fp32's range.
  * workspace  >= bigcn_grad_norm_workspace_bytes(n) bytes, 256-byte aligned. Sums are added in a
  *        fixed order: deterministic for tensors of the same alignment to 16 bytes.
  * 0 <= n <= 65536. norm and workspace may not overlap a tensor or each other. Tensors may overlap (an

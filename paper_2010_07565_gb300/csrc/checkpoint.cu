@@ -1,6 +1,6 @@
 // Activations to 8 bits and back (bigcn_checkpoint_pack, bigcn_checkpoint_unpack): the arithmetic
 // is checkpoint.cuh's, a few operations a column; both are bound by memory. 2^20 x 512 bf16: packing
-// 247 us (0.95 of a copy's rate), unpacking 267 us (0.90), 395 with gamma and beta.
+// 255 us (0.95 of a copy's rate), unpacking 267 us (0.90), 398 with gamma and beta.
 #include "norm.cuh"
 
 namespace bigcn {

@@ -22,12 +22,13 @@
 // What bounds it (L2 flushed before each call; floors at a copy's 6754 GB/s):
 //   232,965 x 602 x 128 fp32: 38 us of 28.7. Start and end of 12 tiles a CTA; B stays in shared memory
 //     (46 us when it was copied for every tile).
-//   232,965 x 128 x 602 fp32: 116 us of 85. Stores: Z's rows are aligned to 8 bytes, a store of 256 bytes
-//     touches three lines, L1 at 83 %. x 604: 109, x 640: 103, x 601 (4 bytes a lane): 191.
+//   232,965 x 128 x 602 fp32: 117 us of 85. Stores: Z's rows are aligned to 8 bytes, a store of 256 bytes
+//     touches three lines, L1 at 83 %. x 604: 107, x 640: 103, x 601 (4 bytes a lane): 195.
 //   2^17 x 8192 x 256 bf16: 132 us of 95. A's copies are 128 bytes of rows 4 KB apart, and a stage's boxes and
 //     MMAs wait for each other 40 % of the issuing thread's time; sums are taken out while nothing is
 //     multiplied, 10 to 16 us of all. More of A on its way did not help (six stages of A beside three of
-//     B 159, boxes of two stages at a time 165, prefetches to L2 by a warp of their own 148, all for 142).
+//     B 159, boxes of two stages at a time 165, prefetches to L2 by a warp of their own 148, all for 142). The
+//     16-bit sums held there spill 12 bytes a thread.
 #include "fp4.cuh"
 #include "launch.cuh"
 #include "tc_rows.cuh"
@@ -704,8 +705,8 @@ extern "C" bigcn_status bigcn_fp4_gemm(int32_t dtype, const uint8_t *aq, int64_t
     const int64_t mt = (N + kUmmaM - 1) / kUmmaM;
     // Tiles of 256 columns read A once for twice as many, but leave no room for a second accumulator: only
     // where a tile's MMAs are long beside taking its sums out, and the last tile is more than half full
-    // (2^17 rows, 256 columns of bf16: K = 8192 134 us, by 128 columns 167; K = 4096 97 and 101; K = 1024
-    // fp32 60 and 50; 219,247 x 2106 x 274 fp16 187 and 154).
+    // (2^17 rows, 256 columns of bf16: K = 8192 132 us, by 128 columns 167; K = 4096 79 and 95; K = 2080 72 and
+    // 70; K = 1024 fp32 52 and 44; 219,247 x 2106 x 274 fp16 193 and 154).
     int NT = F > 128 && K > 2048 && (F + 127) / 128 % 2 == 0 ? 256 : F > 64 ? 128 : F > 32 ? 64 : 32;
     while (NT > 32 && mt * ((F + NT - 1) / NT) * 2 <= dev.sm_count) NT /= 2;
     Fp4GemmArgs p;

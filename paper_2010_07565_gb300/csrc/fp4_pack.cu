@@ -4,8 +4,8 @@
 // Rows are taken as one sequence of octets (packing) or 16-byte pieces (reading back), each row up to a
 // whole group, so that every lane has work whatever a row's length: laid over a power of two
 // threads, 602 columns kept 59 of 100 lanes busy. 232,965 x 602 fp32: packing 105 us (131 so; 6.05 TB/s,
-// 0.90 of a copy's rate), reading back to bf16 72 us (101; 4.9 TB/s: rows aligned to 4 bytes), to fp32 99
-// us; 2^20 x 128 fp32 101 and 57 us.
+// 0.90 of a copy's rate), reading back to bf16 68 us (101; 5.2 TB/s: rows aligned to 4 bytes), to fp32 101
+// us; 2^20 x 128 fp32 101 and 56 us. From bf16, 232,965 x 602 76 us (0.69), 2^20 x 256 122 (0.83).
 #include "fp4.cuh"
 #include "norm.cuh"
 
@@ -157,7 +157,8 @@ void launch_fp4(int32_t dtype, const Fp4Args &a, bool pack, cudaStream_t s) {
 // (16 bytes) of eight rows, which are one word of codes each; four lanes hold a column and share its
 // largest magnitude. The eight warps' groups of a column are 128 bytes of its row, put together in
 // shared memory. 8192 x 1024 fp32: 15 us (a column a lane, 32 loads of four bytes: 17), one wave's
-// latency; 4096 x 4096 23 us (29); 8192 x 1024 bf16 17 us (25).
+// latency; 4096 x 4096 23 us (29); 8192 x 1024 bf16 17 us (25), 4096 x 4096 27: a lane holds 64 values of these, 32
+// of fp32, and has the 64 registers of four blocks an SM (132 bytes of spills).
 constexpr int kColumnGroups = kFp4Threads / 32;
 template <typename T>
 __device__ __forceinline__ void load_columns(const T *p, int64_t n, bool wide, float (&v)[kPiece<T>]) {

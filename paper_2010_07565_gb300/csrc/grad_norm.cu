@@ -14,7 +14,7 @@
 // elements scaled by a power of two.
 //
 // Bound by memory: every element is read for the norm, read again, from L2 where it is still there,
-// and written. 48 matrices of 4096 x 1024 bf16 with their vectors: 204 us (the norm alone 68 at 5.9
+// and written. 48 matrices of 4096 x 1024 bf16 with their vectors: 201 us (the norm alone 67 at 6.0
 // TB/s), 1.2 GB at 5.9 TB/s; a copy's rate would take 179 us, 119 if nothing were read twice. A thread's
 // loads of the next chunks ahead, in registers or in a ring in shared memory, and a block's
 // chunks strided through memory instead of a run of it gave nothing.
@@ -116,7 +116,9 @@ struct ClipRun {
 // Places of a chunk: its pieces begin at `piece`, of which piece q holds elements (piece + q) V -
 // shift + 0 .. V - 1 of the tensor, those within [0, count).
 // (kKeep: in L2 as usual. What will not be there any more when the scaling comes to it leaves L2 first: 48
-// x 4096 x 1024 bf16 216 -> 208 us, by evict-first loads behind the first 64 MB from the end.)
+// x 4096 x 1024 bf16 210 -> 202 us, by evict-first loads behind the first 64 MB from the end, of each launch where
+// a call has more than one. The norm alone does the same: 400 MB behind a buffer that was just written 94 -> 82 us,
+// and the same tensors read again 75 and 77, 96 MB 31 -> 30 and 29 -> 25.)
 template <typename T, bool kKeep>
 __device__ __forceinline__ uint4 load_place(const T *in, int64_t first, int64_t count) {
     constexpr int V = kPiece<T>;

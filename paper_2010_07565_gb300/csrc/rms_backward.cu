@@ -4,10 +4,14 @@
 //
 // with shat from the forward's sum or from its 8-bit checkpoint, and ds what comes past the norm. The
 // kernels are layer norm's (norm_backward.cuh) without its mean and without the sums of g and dy,
-// bound by memory like them: 232,965 x 602 fp32 from the sum, with ds, 338 us (6.6 TB/s, 0.98 of a copy's
-// rate); 2^20 x 256 bf16 from the checkpoint, with ds, 350 us (5.4 TB/s: 24 warps an SM of 77
-// registers). 19,717 x 500 fp16 24.6 us: a warp's eight rows one after the other, and 5 us for
+// bound by memory like them: 232,965 x 602 fp32 with ds from the sum 340 us (6.6 TB/s, 0.98 of a copy's
+// rate), from the checkpoint 278 (0.97); 2^20 x 256 bf16 from the checkpoint, with ds, 350 us (5.4 TB/s: 24 warps an
+// SM of 77 registers). 19,717 x 500 fp16 24.6 us: a warp's eight rows one after the other, and 5 us for
 // gamma's sums behind them.
+// Spills: six pieces a thread with ds (fp32 rows of 641 to 768 columns) 36 to 88 bytes, 200,000 x 700 0.83 of a
+// copy's rate from the sum and 0.72 from the checkpoint; one piece a lane of 16-bit rows aligned to 8 bytes without ds,
+// under its bound of four blocks, 32 bytes, 2^20 x 252 bf16 0.62 and 0.54 (aligned to 16, 256 columns: none, 0.81 and
+// 0.72); at most 28 bytes in others.
 #include "norm_args.cuh"
 
 namespace bigcn {

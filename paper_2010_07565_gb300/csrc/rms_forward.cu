@@ -5,9 +5,10 @@
 //
 // Bound by memory: x and r are read once into registers, s, y and the checkpoint written once.
 // What is normalised is the rounded sum, which the next layers and the backward pass read. Rows,
-// pieces and their accesses are norm.cuh's. 232,965 x 602 fp32 with R, S and the checkpoint 340 us, 6.9 TB/s (a
-// copy's rate); 2^20 x 256 bf16 351 us, 6.9 TB/s; 400,000 x 500 fp16 without it 240 us (6.7 TB/s), x 501, rows at odd
-// halves, 396: five accesses a piece.
+// pieces and their accesses are norm.cuh's. 232,965 x 602 fp32 with R, S and the checkpoint 347 us, 6.9 TB/s (a
+// copy's rate); 2^20 x 256 bf16 349 us, 6.9 TB/s; 400,000 x 500 fp16 without it 244 us (6.5 TB/s), x 501, rows at odd
+// halves, 398: five accesses a piece. Eight pieces a thread (fp32 rows of 769 to 1024 columns, aligned to 16 bytes)
+// spill 28 to 60 bytes: 200,000 x 1000 505 us, 0.94 of a copy's rate, with the checkpoint 496.
 #include <cmath>
 
 #include "norm.cuh"
