@@ -404,9 +404,9 @@ __device__ __forceinline__ void row_sum(float (&v)[kN], int tpr, float (*red)[kM
 // terms, whose sums are added in fp64 (one running fp32 sum over 2^24 equal columns is off by 3e-4 of itself). A
 // share of at most kRun terms is a plain fp32 sum. term(k, sums) adds column k's.
 constexpr int kRun = 256;
-// kPlain: rows of one share by a plain loop, others four terms at a time (RMS backward, 4096 x 16400 fp32: from
-// the input 379 -> 290 us, from the checkpoint 329 -> 220; layer norm's from the input, 16 x 2^22 fp32, 24.8 ->
-// 17.0 ms; the RMS forward takes longer so, 374 -> 437 us).
+// kPlain: rows of one share by a plain loop (4096 x 16400 fp32, RMS backward from the input 304 -> 259 us, from the
+// checkpoint 316 -> 214), others four terms at a time (64 x 70001 fp32, layer norm's 238 -> 101 and 181 -> 160). The
+// forward passes take longer so (RMS, 4096 x 16400: 374 -> 437).
 template <bool kPlain, int kN, typename Term>
 __device__ __forceinline__ void share_sums(int K, float (&v)[kN], Term term) {
     constexpr int kShares = kRowThreads * kRun;

@@ -10,17 +10,20 @@ namespace bigcn {
 namespace {
 
 template <typename T, bool kRms>
-__device__ __forceinline__ float xhat_at(const BackwardArgs &a, int64_t i, int k, float mean,
+__device__ __forceinline__ float xhat_at(const BackwardArgs &a, bool kept, int64_t i, int k, float mean,
                                          float rstd) {
-    if (a.X) {
+    if (!kept) {
         const float x = to_f32(static_cast<const T *>(a.X)[i * a.ldx + k]);
         return (kRms ? x : x - mean) * rstd;
     }
     return float(a.q[i * a.ldq + k]) * unpack_factor(a.exps[i * a.lde + k / kGroup]);
 }
 
-// dX of rows that do not fit registers: a block per row, two walks.
-template <typename T, bool kRms>
+// dX of rows that do not fit registers: a block per row, two walks. (kKept: from the checkpoint. With that
+// asked for in the loop the RMS norm's first walk waited for each load: 64 x 70001 fp32 from the input 230 us,
+// from the checkpoint 252, now 130 and 162. Which products join sums is written out: left to the compiler, that
+// changed with the loops around them.)
+template <typename T, bool kRms, bool kKept>
 __global__ void __launch_bounds__(kRowThreads) backward_any_kernel(const BackwardArgs a) {
     const int K = a.K;
     const float inv_k = 1.0f / float(K);
@@ -28,21 +31,21 @@ __global__ void __launch_bounds__(kRowThreads) backward_any_kernel(const Backwar
         const T *dy = static_cast<const T *>(a.dY) + i * a.lddy;
         T *dx = static_cast<T *>(a.dX) + i * a.lddx;
         const T *ds = kRms && a.dS ? static_cast<const T *>(a.dS) + i * a.ldds : nullptr;
-        const float rstd = a.rstd[i], mean = !kRms && a.X ? a.mean[i] : 0.0f;
+        const float rstd = a.rstd[i], mean = !kRms && !kKept ? a.mean[i] : 0.0f;
         float s[2];
         share_sums<true>(K, s, [&](int k, float (&run)[2]) {
-            const float g = to_f32(dy[k]) * (a.gamma ? __ldg(a.gamma + k) : 1.0f);
+            const float g = __fmul_rn(to_f32(dy[k]), a.gamma ? __ldg(a.gamma + k) : 1.0f);
             run[0] += g;
-            run[1] = fmaf(g, xhat_at<T, kRms>(a, i, k, mean, rstd), run[1]);
+            run[1] = fmaf(g, xhat_at<T, kRms>(a, kKept, i, k, mean, rstd), run[1]);
         });
         block_sum(s);
         const float c0 = s[0] * inv_k, c1 = s[1] * inv_k;
         for (int k = threadIdx.x; k < K; k += kRowThreads) {
-            const float g = to_f32(dy[k]) * (a.gamma ? __ldg(a.gamma + k) : 1.0f);
-            const float h = xhat_at<T, kRms>(a, i, k, mean, rstd);
+            const float g = __fmul_rn(to_f32(dy[k]), a.gamma ? __ldg(a.gamma + k) : 1.0f);
+            const float h = xhat_at<T, kRms>(a, kKept, i, k, mean, rstd);
             if constexpr (kRms)
                 dx[k] = from_f32<T>(fmaf(fmaf(h, -c1, g), rstd, ds ? to_f32(ds[k]) : 0.0f));
-            else dx[k] = from_f32<T>(rstd * (g - c0 - h * c1));
+            else dx[k] = from_f32<T>(rstd * fmaf(-h, c1, g - c0));
         }
     }
 }
@@ -59,8 +62,7 @@ __global__ void __launch_bounds__(kRowThreads) param_any_kernel(const BackwardAr
     if (k < a.K)
         for (int64_t i = r0 + warp; i < r1; i += (kRowThreads / 32)) {
             const float dy = to_f32(static_cast<const T *>(a.dY)[i * a.lddy + k]);
-            sg = fmaf(dy, xhat_at<T, kRms>(a, i, int(k), !kRms && a.X ? a.mean[i] : 0.0f, a.rstd[i]),
-                      sg);
+            sg = fmaf(dy, xhat_at<T, kRms>(a, !a.X, i, int(k), !kRms && a.X ? a.mean[i] : 0.0f, a.rstd[i]), sg);
             sb += dy;
         }
     part[0][warp][lane] = sg;
@@ -360,7 +362,9 @@ void launch_backward(BackwardArgs &a, const DeviceInfo &dev, cudaStream_t s) {
     else done = launch_any_alignment<T, kRms, false>(a, A, aligned, dev, s);
     if (done) return;
     const int64_t most = int64_t(dev.sm_count) * 64;
-    if (a.dX) backward_any_kernel<T, kRms><<<unsigned(a.N < most ? a.N : most), kRowThreads, 0, s>>>(a);
+    const unsigned blocks = unsigned(a.N < most ? a.N : most);
+    if (a.dX && a.X) backward_any_kernel<T, kRms, false><<<blocks, kRowThreads, 0, s>>>(a);
+    else if (a.dX) backward_any_kernel<T, kRms, true><<<blocks, kRowThreads, 0, s>>>(a);
     if (!a.partial) return;
     const int64_t strips = (int64_t(a.K) + 31) / 32;
     int64_t chunks = (int64_t(dev.sm_count) * 8 + strips - 1) / strips;
