@@ -165,7 +165,7 @@ class NormedLayer:
         dY  = G W~^T
         dX, dgamma, dbeta                                 the norm's gradients from dY
 
-    ``weight_gradient()`` takes dWb through the sign (Eq. bp-W): the gradient of W itself, which a step
+    ``weight_gradient()`` is dWb taken through the sign (Eq. bp-W): the gradient of W itself, which a step
     subtracts. Once ``gradients()`` has been asked for, ``backward()`` writes it into dW each time."""
 
     def __init__(self, N: int, K: int, F: int, device, eps: float = 1e-5, scratch=None):
@@ -211,7 +211,7 @@ class NormedLayer:
                                        gamma=self.gamma, beta=self.beta, db=self.db)
         # (Ten torch calls, 110 us of the host's time beside 60 for the rest: for those who ask.)
         if self.dW is not None:
-            self.weight_gradient(out=self.dW)
+            self._through_sign(self.dW)
         elif torch.cuda.is_current_stream_capturing():
             self._captured = True
         # dY = (G diag(beta_j)) sign(W)^T: W packed row by row over its F columns.
@@ -228,10 +228,15 @@ class NormedLayer:
         if self.dW is None:
             if self._captured:
                 raise RuntimeError("a captured backward() leaves dW out: ask for gradients() before capturing")
-            self.dW = self.weight_gradient()
+            self.dW = self._through_sign()
         return [self.dW, self.db, self.dgamma, self.dbeta]
 
-    def weight_gradient(self, out=None):
+    def weight_gradient(self):
+        """The gradient of W, a tensor of its own: of dW where ``gradients()`` has been asked for, scaled as that
+        has been since (``GradientClip``), else of dWb as it is."""
+        return self._through_sign() if self.dW is None else self.dW.clone()
+
+    def _through_sign(self, out=None):
         """Eq. bp-W of dWb: sign(W) times the column means of dWb sign(W), and beta_j dWb where
         |W| < 1 (the straight-through estimator of sign)."""
         sign = torch.where(self.W >= 0, 1.0, -1.0)

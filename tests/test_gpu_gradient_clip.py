@@ -102,6 +102,28 @@ def test_captured_with_the_step(cuda_device):
     assert all(torch.equal(a, b) for a, b in zip(want, tensors))
 
 
+def test_weight_gradient_behind_the_clipping_is_clipped(cuda_device):
+    """A step that asks weight_gradient() again gets what the list holds, in a tensor of its own; a layer whose
+    gradients nobody asked for has dWb's."""
+    N, K, F = 300, 64, 8
+    layers = layers_of_both_kinds(N, K, F, cuda_device)
+    X, rowptr, colidx = case(N, K, cuda_device)
+    second = layers[1]
+    step(layers, X, rowptr, colidx)
+    whole = second.weight_gradient()
+    within(whole, *weight_gradient(second), "gradient of W")
+    clip = GradientClip(layers)
+    for limit in (2.0 ** -10, 2.0 ** -12):
+        norm = clip(limit).item()
+        got = second.weight_gradient()
+        assert torch.equal(got, second.dW) and norm > limit
+        assert got.abs().max() < 0.5 * whole.abs().max()
+        got.zero_()
+        assert second.dW.abs().max() > 0
+        step(layers, X, rowptr, colidx)
+        assert torch.equal(second.weight_gradient(), whole)
+
+
 def test_weight_gradient_is_kept_for_those_who_ask(cuda_device):
     """Asked for after a backward pass, gradients() has that pass's and from then on every later one's; a
     graph that was captured before cannot write it, which is refused."""
