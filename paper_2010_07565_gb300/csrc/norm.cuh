@@ -405,9 +405,10 @@ __device__ __forceinline__ void row_sum(float (&v)[kN], int tpr, float (*red)[kM
 // share of at most kRun terms is a plain fp32 sum. term(k, sums) adds column k's.
 constexpr int kRun = 256;
 // kPlain: rows of one share by a plain loop (4096 x 16400 fp32, RMS backward from the input 304 -> 259 us, from the
-// checkpoint 316 -> 214), others four terms at a time (64 x 70001 fp32, layer norm's 238 -> 101 and 181 -> 160). The
-// forward passes take longer so (RMS, 4096 x 16400: 374 -> 437).
-template <bool kPlain, int kN, typename Term>
+// checkpoint 316 -> 214); the forward passes take longer so (RMS, 4096 x 16400: 374 -> 437). kFour: longer rows four
+// terms at a time, as the compiler would not (64 x 70001 fp32, layer norm's 238 -> 101 and 181 -> 160; a 16-bit
+// layer's checkpoint, without, 195 -> 138 by the RMS norm and 195 -> 162, though 4096 x 16400 152 -> 154 and 169).
+template <bool kPlain, bool kFour, int kN, typename Term>
 __device__ __forceinline__ void share_sums(int K, float (&v)[kN], Term term) {
     constexpr int kShares = kRowThreads * kRun;
     if (kPlain && K <= kShares) {
@@ -420,7 +421,7 @@ __device__ __forceinline__ void share_sums(int K, float (&v)[kN], Term term) {
     for (int first = threadIdx.x; first < K; first += kShares) {
         float run[kN] = {};
         const int end = min(K, first + kShares);
-        if constexpr (kPlain) {
+        if constexpr (kFour) {
 #pragma unroll 4
             for (int k = first; k < end; k += kRowThreads) term(k, run);
         } else {

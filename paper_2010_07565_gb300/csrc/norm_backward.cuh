@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kRowThreads) backward_any_kernel(const Backwar
         const T *ds = kRms && a.dS ? static_cast<const T *>(a.dS) + i * a.ldds : nullptr;
         const float rstd = a.rstd[i], mean = !kRms && !kKept ? a.mean[i] : 0.0f;
         float s[2];
-        share_sums<true>(K, s, [&](int k, float (&run)[2]) {
+        share_sums<true, !kKept || sizeof(T) == 4>(K, s, [&](int k, float (&run)[2]) {
             const float g = __fmul_rn(to_f32(dy[k]), a.gamma ? __ldg(a.gamma + k) : 1.0f);
             run[0] += g;
             run[1] = fmaf(g, xhat_at<T, kRms>(a, kKept, i, k, mean, rstd), run[1]);

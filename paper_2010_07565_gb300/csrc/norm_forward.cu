@@ -61,10 +61,10 @@ __global__ void __launch_bounds__(kRowThreads) forward_any_kernel(const ForwardA
         const T *x = static_cast<const T *>(a.X) + i * a.ldx;
         T *y = static_cast<T *>(a.Y) + i * a.ldy;
         float s0[1], s[2], variance;
-        share_sums<false>(K, s0, [&](int k, float (&run)[1]) { run[0] += to_f32(x[k]); });
+        share_sums<false, false>(K, s0, [&](int k, float (&run)[1]) { run[0] += to_f32(x[k]); });
         block_sum(s0);
         float mean = s0[0] * inv_k;
-        share_sums<false>(K, s, [&](int k, float (&run)[2]) {
+        share_sums<false, false>(K, s, [&](int k, float (&run)[2]) {
             const float d = to_f32(x[k]) - mean;
             run[0] += d;
             run[1] = fmaf(d, d, run[1]);

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kRowThreads) rms_forward_any_kernel(const RmsF
         // (Once the sum is stored it is read there: it may have taken r's or x's place.)
         auto at = [&](int k) { return to_f32(sum ? sum[k] : fresh(k)); };
         float s[1];
-        share_sums<false>(K, s, [&](int k, float (&run)[1]) {
+        share_sums<false, false>(K, s, [&](int k, float (&run)[1]) {
             const T v = fresh(k);
             if (sum) sum[k] = v;
             run[0] = fmaf(to_f32(v), to_f32(v), run[0]);
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kRowThreads) rms_forward_any_kernel(const RmsF
         block_sum(s);
         const Rstd r_of = rstd_of(s[0], K, inv_k, a.eps, [&](float f) {
             float again[1];
-            share_sums<false>(K, again, [&](int k, float (&run)[1]) {
+            share_sums<false, false>(K, again, [&](int k, float (&run)[1]) {
                 const float v = at(k) * f;
                 run[0] = fmaf(v, v, run[0]);
             });
